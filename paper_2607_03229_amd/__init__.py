@@ -11,6 +11,10 @@ from ._binding import (  # noqa: F401
     CHECK_NOALLOC_MAX_ROWS,
     op_gemm, op_layernorm_fwd, op_layernorm_bwd, op_rope, op_attention_fwd,
     op_attention_bwd, op_scratch_bytes, op_splitk_reduce, gemm_split, gemm_kernel,
+    op_seam_positions, op_rope_axes, op_qk_norm_rope_fwd, op_qk_norm_rope_bwd,
+    op_qk_norm_rope_scratch_bytes, op_grad_norm, op_grad_clip, op_grad_scratch_bytes,
+    RopeCfg, GradList, ROPE_BLOCKS, ROPE_INTERLEAVED, ROPE_ONE_SPECTRUM, ROPE_AXIS_SPECTRA,
+    ROPE_HALVES, ROPE_ADJACENT,
     F32, BF16, OK, NOOP_FROZEN,
     owner_map, OWNER_GREEDY, OWNER_EXACT, OWNER_REFINED,
     schedule_valid, Derived, EVENT_FIELDS,

@@ -40,6 +40,39 @@ class EncoderCfg(C.Structure):
                    float(cfg.rope_theta))
 
 
+class RopeCfg(C.Structure):
+    """mpipe_rope_cfg: which pairs of a head's columns turn by which axis' position, and how
+    fast.  `sections`: pairs of each axis (their sum is rot_dim / 2); rot_dim defaults to
+    head_dim.  The values are checked by the calls that take it."""
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32),
+                ("section", C.c_int32 * 4), ("order", C.c_int32), ("spectrum", C.c_int32),
+                ("pairing", C.c_int32), ("theta", C.c_double)]
+
+    def __init__(self, head_dim: int, sections: Sequence[int], rot_dim: Optional[int] = None,
+                 theta: float = 10000.0, order: int = 0, spectrum: int = 0, pairing: int = 0):
+        sections = [int(v) for v in sections]
+        if not 1 <= len(sections) <= 4:
+            raise MpipeError(-1, "one to four sections")
+        super().__init__(int(head_dim), int(head_dim if rot_dim is None else rot_dim),
+                         len(sections), (C.c_int32 * 4)(*sections), int(order), int(spectrum),
+                         int(pairing), float(theta))
+
+
+ROPE_BLOCKS, ROPE_INTERLEAVED = 0, 1
+ROPE_ONE_SPECTRUM, ROPE_AXIS_SPECTRA = 0, 1
+ROPE_HALVES, ROPE_ADJACENT = 0, 1
+
+
+class _Heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("heads", C.c_int32)]
+
+
+class _GradTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -86,6 +119,15 @@ def load():
         "mpipe_op_attention_fwd": (st, [i32, P, i64, i32, i32, P, i32, P, P, P, sz, P]),
         "mpipe_op_attention_bwd": (st, [i32, P, P, P, P, i64, i32, i32, P, i32, P, P, sz, P]),
         "mpipe_op_scratch_bytes": (sz, [i64, i32, i32, i32]),
+        "mpipe_op_seam_positions": (st, [P, P, P, i32, P, P, P, i32, i64, P, i64, P, P]),
+        "mpipe_op_rope_axes": (st, [i32, P, i64, P, P, P, i64, i32, P, P, P]),
+        "mpipe_op_qk_norm_rope_fwd": (st, [i32, P, i64, P, P, P, P, C.c_float, P, i64, P, P, P]),
+        "mpipe_op_qk_norm_rope_bwd": (st, [i32, P, i64, P, P, P, P, P, P, C.c_float, P, i64, P, P,
+                                           P, P, i32, P, sz, P]),
+        "mpipe_op_qk_norm_rope_scratch_bytes": (sz, [i64, i32, i32, i32]),
+        "mpipe_op_grad_norm": (st, [P, i32, P, P, P, sz, P]),
+        "mpipe_op_grad_scratch_bytes": (sz, [P, i32]),
+        "mpipe_op_grad_clip": (st, [P, P, i32, P, C.c_double, P, P]),
         "mpipe_encoder_cost": (st, [P, P, i32, P, i32, i32, C.c_double, C.c_double, P]),
         "mpipe_owner_map": (st, [P, i32, P, i32, i32, P, P, P]),
         "mpipe_schedule_valid": (st, [P, i32, i32, P]),
@@ -527,3 +569,237 @@ def op_attention_bwd(dtype, qkv, o, d_o, lse, N, heads, head_dim, cu_seqlens, dq
                                          heads, head_dim, cup, max(len(cu) - 1, 0), _ptr(dqkv),
                                          _ptr(scratch), scratch.numel() * scratch.element_size(),
                                          _stream(stream)))
+
+
+# --------------------------------------------------------------------------
+# The first LLM layer behind the seam, and the end of a trained step
+# --------------------------------------------------------------------------
+
+def _need(ok: bool, msg: str) -> None:
+    if not ok:
+        raise MpipeError(-1, msg)
+
+
+class _Launch:
+    """The device and stream of a call: every tensor on one GPU, made current for the call
+    (a tensor's own GPU need not be); the stream is that GPU's current one unless given."""
+
+    def __init__(self, tensors, stream):
+        import torch
+        self.device = dev = tensors[0].device
+        _need(dev.type == "cuda", "tensors must be on the GPU")
+        for t in tensors:
+            _need(t.device == dev, "tensors on different devices")
+        if stream is None:
+            stream = torch.cuda.current_stream(dev)
+        _need(stream.device == dev, "a stream of another device than the tensors'")
+        self.stream = stream.cuda_stream
+        here = torch.cuda.current_device()
+        self.back = None if here == dev.index else here
+
+    def __enter__(self):
+        if self.back is not None:
+            import torch
+            torch.cuda.set_device(self.device)
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            import torch
+            torch.cuda.set_device(self.back)
+
+
+def _host_i64(a, name: str) -> np.ndarray:
+    arr = np.asarray(a)
+    _need(arr.ndim == 1 and (arr.size == 0 or arr.dtype.kind in "iu"),
+          f"{name}: a list of whole numbers")
+    return np.ascontiguousarray(arr, dtype=np.int64)
+
+
+def _p(arr: Optional[np.ndarray]):
+    return None if arr is None else arr.ctypes.data
+
+
+def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, time_step=None,
+                      stream=None) -> np.ndarray:
+    """pos[:, row] (int32 [3][rows], rows adjacent) = the (time, height, width) position of
+    every row of the sequences [seq_row, seq_row + seq_len); rows of none are left as they
+    were.  Item i's merged rows start at row item_row[i] with the encoder's grid_thw[i].
+    Returns the position behind each sequence's last row, which is `seq_pos` when it goes on."""
+    import torch
+    sr, sl = _host_i64(seq_row, "seq_row"), _host_i64(seq_len, "seq_len")
+    sp = None if seq_pos is None else _host_i64(seq_pos, "seq_pos")
+    ir = _host_i64(item_row, "item_row")
+    g = np.ascontiguousarray(_host_i64(np.asarray(grid_thw).reshape(-1), "grid_thw"))
+    ts = None if time_step is None else _host_i64(time_step, "time_step")
+    _need(sl.size == sr.size and (sp is None or sp.size == sr.size),
+          "seq_row, seq_len and seq_pos differ in length")
+    _need(g.size == 3 * ir.size and (ts is None or ts.size == ir.size),
+          "item_row, grid_thw and time_step differ in length")
+    for a in (g, ts):
+        _need(a is None or a.size == 0 or (a.min() >= -2 ** 31 and a.max() < 2 ** 31),
+              "a grid or time step beyond 32 bits")
+    g, ts = g.astype(np.int32), None if ts is None else ts.astype(np.int32)
+    _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == 3 and
+          (pos.shape[1] <= 1 or pos.stride(1) == 1), "pos: int32 [3][rows], rows adjacent")
+    nxt = np.zeros(sr.size, np.int64)
+    with _Launch((pos,), stream) as s:
+        _check(load().mpipe_op_seam_positions(
+            _p(sr), _p(sl), _p(sp), sr.size, _p(ir), _p(g), _p(ts), ir.size, pos.shape[1],
+            _ptr(pos), pos.stride(0), _p(nxt), s))
+    return nxt
+
+
+def _heads(t, like=None):
+    """mpipe_heads of [rows][heads][head_dim]; None: no heads."""
+    if t is None:
+        return None
+    if like is not None:
+        _need(t.shape == like.shape and t.dtype == like.dtype,
+              "inputs, gradients and outputs differ in shape or dtype")
+    rs, hs, cs = t.stride()
+    _need(cs == 1, "the columns of a head must be adjacent")
+    return C.byref(_Heads(t.data_ptr(), rs, hs, t.shape[1]))
+
+
+def _qk_common(cfg, q, k, pos, others):
+    """(dtype, rows) of q and k [rows][heads][head_dim] (either may be None) and the tensors
+    of the call."""
+    import torch
+    one = q if q is not None else k
+    _need(one is not None, "neither q nor k")
+    for t in (q, k):
+        _need(t is None or (t.dim() == 3 and t.shape[2] == cfg.head_dim and
+                            t.shape[0] == one.shape[0] and t.dtype == one.dtype),
+              "q and k: [rows][heads][head_dim] of one dtype")
+    for x, ys in ((q, others[0]), (k, others[1])):
+        _need(all((y is None) == (x is None) for y in ys), "one of q and k without its output")
+    _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == cfg.axes and
+          pos.shape[1] == one.shape[0] and (pos.shape[1] <= 1 or pos.stride(1) == 1),
+          "pos: int32 [axes][rows], rows adjacent")
+    return _dt(one), one.shape[0], [t for t in (q, k, pos, *others[0], *others[1])
+                                    if t is not None]
+
+
+def _gains(cfg, x, gain, name):
+    if x is None:
+        return
+    _need(gain is not None and gain.dtype == x.dtype and gain.dim() == 1 and
+          gain.shape[0] == cfg.head_dim and gain.is_contiguous(),
+          f"{name}: [head_dim] in the heads' dtype")
+
+
+def op_rope_axes(cfg, q, k, pos, q_out, k_out, inverse: bool = False, stream=None) -> None:
+    """q_out, k_out = q, k ([rows][heads][head_dim], any strides of rows and heads; k and
+    k_out may be None) turned by pos (int32 [axes][rows]); inverse turns back (the gradient).
+    An output may be its own input."""
+    dt, rows, ts = _qk_common(cfg, q, k, pos, ((q_out,), (k_out,)))
+    with _Launch(ts, stream) as s:
+        _check(load().mpipe_op_rope_axes(dt, C.byref(cfg), rows, _heads(q), _heads(k), _ptr(pos),
+                                         pos.stride(0), int(bool(inverse)), _heads(q_out, q),
+                                         _heads(k_out, k), s))
+
+
+def op_qk_norm_rope_fwd(cfg, q, k, q_gain, k_gain, eps: float, pos, q_out, k_out,
+                        stream=None) -> None:
+    """The same behind a root-mean-square norm of every head with a gain [head_dim]."""
+    dt, rows, ts = _qk_common(cfg, q, k, pos, ((q_out,), (k_out,)))
+    _gains(cfg, q, q_gain, "q_gain")
+    _gains(cfg, k, k_gain, "k_gain")
+    ts += [g for g in (q_gain, k_gain) if g is not None]
+    with _Launch(ts, stream) as s:
+        _check(load().mpipe_op_qk_norm_rope_fwd(dt, C.byref(cfg), rows, _heads(q), _heads(k),
+                                                _ptr(q_gain), _ptr(k_gain), eps, _ptr(pos),
+                                                pos.stride(0), _heads(q_out, q),
+                                                _heads(k_out, k), s))
+
+
+def op_qk_norm_rope_scratch_bytes(rows: int, heads_q: int, heads_k: int, head_dim: int) -> int:
+    n = int(load().mpipe_op_qk_norm_rope_scratch_bytes(rows, heads_q, heads_k, head_dim))
+    _need(n > 0, "op_qk_norm_rope_scratch_bytes: argument out of range")
+    return n
+
+
+def op_qk_norm_rope_bwd(cfg, dq, dk, q, k, q_gain, k_gain, eps: float, pos, dq_in, dk_in,
+                        grad_q_gain, grad_k_gain, scratch, accumulate: bool = True,
+                        stream=None) -> None:
+    """Gradients of op_qk_norm_rope_fwd: dq_in, dk_in from dq, dk (they may be the same
+    tensors) and the forward's q, k, gains, eps and positions; grad_q_gain, grad_k_gain (fp32
+    [head_dim], may be None) are added to, or overwritten with accumulate=False.  scratch:
+    op_qk_norm_rope_scratch_bytes."""
+    import torch
+    dt, rows, ts = _qk_common(cfg, q, k, pos, ((dq, dq_in), (dk, dk_in)))
+    _gains(cfg, q, q_gain, "q_gain")
+    _gains(cfg, k, k_gain, "k_gain")
+    for g, x in ((grad_q_gain, q), (grad_k_gain, k)):
+        _need(g is None or (x is not None and g.dtype == torch.float32 and g.dim() == 1 and
+                            g.shape[0] == cfg.head_dim and g.is_contiguous()),
+              "gain gradients: fp32 [head_dim]")
+    _need(scratch is None or scratch.is_contiguous(), "scratch must be contiguous")
+    ts += [t for t in (q_gain, k_gain, grad_q_gain, grad_k_gain, scratch) if t is not None]
+    with _Launch(ts, stream) as s:
+        _check(load().mpipe_op_qk_norm_rope_bwd(
+            dt, C.byref(cfg), rows, _heads(dq, q), _heads(dk, k), _heads(q), _heads(k),
+            _ptr(q_gain), _ptr(k_gain), eps, _ptr(pos), pos.stride(0), _heads(dq_in, q),
+            _heads(dk_in, k), _ptr(grad_q_gain), _ptr(grad_k_gain), int(bool(accumulate)),
+            _ptr(scratch), 0 if scratch is None else scratch.numel() * scratch.element_size(), s))
+
+
+class GradList:
+    """The tensors of a gradient (fp32 or bf16, contiguous, one GPU) as the calls take them;
+    it keeps them alive.  Made once for buffers that stay, or for every call."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        self.array = (_GradTensor * max(n, 1))()
+        for a, t in zip(self.array, self.tensors):
+            _need(t.is_contiguous(), "gradients must be contiguous")
+            _need(t.device == self.tensors[0].device, "tensors on different devices")
+            a.data, a.n, a.dtype = t.data_ptr(), t.numel(), _dt(t)
+        self.n = n
+
+
+def _grad_list(grads) -> GradList:
+    return grads if isinstance(grads, GradList) else GradList(grads)
+
+
+def op_grad_scratch_bytes(grads) -> int:
+    """Scratch of op_grad_norm for these tensors (a GradList or tensors)."""
+    g = _grad_list(grads)
+    n = int(load().mpipe_op_grad_scratch_bytes(g.array, g.n))
+    if n == 0:
+        raise MpipeError(-1, last_error())
+    return n
+
+
+def op_grad_norm(grads, sumsq, norms, scratch, stream=None) -> None:
+    """sumsq (fp64 [1]) = the sum of squares over all of grads (a GradList or tensors);
+    norms (fp32 [tensors], may be None) = each one's L2 norm."""
+    import torch
+    g = _grad_list(grads)
+    _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1, "sumsq: fp64 [1]")
+    _need(norms is None or (norms.dtype == torch.float32 and norms.numel() == g.n and
+                            norms.is_contiguous()), "norms: fp32 [tensors]")
+    _need(scratch.is_contiguous(), "scratch must be contiguous")
+    ts = [sumsq, scratch] + g.tensors[:1] + ([] if norms is None else [norms])
+    with _Launch(ts, stream) as s:
+        _check(load().mpipe_op_grad_norm(g.array, g.n, _ptr(sumsq), _ptr(norms), _ptr(scratch),
+                                         scratch.numel() * scratch.element_size(), s))
+
+
+def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None) -> None:
+    """Scale grads to the norm max_norm where sqrt(sumsq) is above it (and finite): in place,
+    or into `out` (tensors of the same lengths, fp32 or bf16, always written).  norm (fp32
+    [1], may be None) = sqrt(sumsq)."""
+    import torch
+    g = _grad_list(grads)
+    o = None if out is None else _grad_list(out)
+    _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1, "sumsq: fp64 [1]")
+    _need(norm is None or (norm.dtype == torch.float32 and norm.numel() == 1), "norm: fp32 [1]")
+    _need(o is None or o.n == g.n, "grads and out differ in number")
+    ts = [sumsq] + g.tensors[:1] + ([] if norm is None else [norm]) + \
+        ([] if o is None else o.tensors[:1])
+    with _Launch(ts, stream) as s:
+        _check(load().mpipe_op_grad_clip(g.array, None if o is None else o.array, g.n,
+                                         _ptr(sumsq), float(max_norm), _ptr(norm), s))

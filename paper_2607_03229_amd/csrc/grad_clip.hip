@@ -1,0 +1,187 @@
+// The L2 norm of a gradient of several tensors and its scaling to a largest norm
+// (mpipe_op_grad_norm, mpipe_op_grad_clip).
+//
+//   S = sum g^2 (fp64), norm = sqrt(S), out = g * (norm > max ? max / norm : 1)
+// Tensors are cut into chunks; their addresses travel in the kernels' arguments, a hundred or
+// two tensors a launch.  Every chunk's sum goes to its own place and the places are added in
+// order, so the result has the same bits every time.
+#include <algorithm>
+
+#include "common.h"
+#include "layer_kernels.h"
+
+namespace mpipe {
+namespace {
+
+constexpr int kNormTensors = 190, kClipTensors = 130;   // arguments below 4 KB
+
+struct NormArgs {
+  const void* p[kNormTensors];
+  int64_t n[kNormTensors];   // elements * 2 + (1 where bf16)
+  int32_t first[kNormTensors];   // first chunk, from chunk0
+};
+
+// the tensor of chunk c: the last one whose first chunk is not behind it
+__device__ __forceinline__ int tensor_of(const int32_t* first, int n, int c) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= c) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += lds[w];
+  __syncthreads();
+  return s;
+}
+
+template <class T>
+__device__ double chunk_sum(const T* p, int64_t n) {
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 256) {
+    const double v = (double)(float)p[i];
+    s = fma(v, v, s);
+  }
+  return s;
+}
+
+// partial[chunk0 + block] = sum of squares of one chunk; starts[tensor] = its first chunk
+__global__ __launch_bounds__(256) void sumsq_kernel(NormArgs a, int n, int tensor0, int chunk0,
+                                                    int64_t chunk, double* partial,
+                                                    int32_t* starts) {
+  __shared__ double lds[4];
+  const int c = blockIdx.x, t = tensor_of(a.first, n, c), nth = c - a.first[t];
+  const int64_t len = a.n[t] >> 1, at = nth * chunk, m = len - at < chunk ? len - at : chunk;
+  const double s = block_sum((a.n[t] & 1) ? chunk_sum((const bf16*)a.p[t] + at, m)
+                                          : chunk_sum((const float*)a.p[t] + at, m), lds);
+  if (threadIdx.x == 0) {
+    partial[chunk0 + c] = s;
+    if (nth == 0) starts[tensor0 + t] = chunk0 + c;
+  }
+}
+
+// block t: the sum of tensor t's chunks, its norm
+__global__ __launch_bounds__(256) void tensor_sum_kernel(const double* partial,
+                                                         const int32_t* starts, int n, int chunks,
+                                                         double* sums, float* norms) {
+  __shared__ double lds[4];
+  const int t = blockIdx.x, end = t + 1 < n ? starts[t + 1] : chunks;
+  double s = 0.0;
+  for (int c = starts[t] + threadIdx.x; c < end; c += 256) s += partial[c];
+  s = block_sum(s, lds);
+  if (threadIdx.x == 0) {
+    sums[t] = s;
+    if (norms) norms[t] = (float)sqrt(s);
+  }
+}
+
+__global__ __launch_bounds__(256) void total_kernel(const double* sums, int n, double* sumsq) {
+  __shared__ double lds[4];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
+  s = block_sum(s, lds);
+  if (threadIdx.x == 0) *sumsq = s;
+}
+
+struct ClipArgs {
+  const void* p[kClipTensors];
+  void* o[kClipTensors];
+  int64_t n[kClipTensors];   // elements * 4 + (1 where the input is bf16) + (2 where the output is)
+  int32_t first[kClipTensors];
+};
+
+template <class A, class B>
+__device__ void chunk_scale(const A* p, B* o, int64_t n, float f) {
+  for (int64_t i = threadIdx.x; i < n; i += 256) o[i] = (B)((float)p[i] * f);
+}
+
+__global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t chunk,
+                                                   const double* sumsq, double max_norm,
+                                                   float* norm) {
+  const double len2 = sqrt(*sumsq);
+  const bool scales = len2 > max_norm && len2 <= 1.7976931348623157e308;
+  const float f = scales ? (float)(max_norm / len2) : 1.f;
+  const int c = blockIdx.x;
+  if (norm && c == 0 && threadIdx.x == 0) *norm = (float)len2;
+  if (n == 0) return;
+  const int t = tensor_of(a.first, n, c);
+  const int64_t len = a.n[t] >> 2, at = (c - a.first[t]) * chunk;
+  const int64_t m = len - at < chunk ? len - at : chunk;
+  if (a.p[t] == a.o[t] && !scales) return;
+  const bool in16 = a.n[t] & 1, out16 = a.n[t] & 2;
+  if (in16 && out16) chunk_scale((const bf16*)a.p[t] + at, (bf16*)a.o[t] + at, m, f);
+  else if (in16) chunk_scale((const bf16*)a.p[t] + at, (float*)a.o[t] + at, m, f);
+  else if (out16) chunk_scale((const float*)a.p[t] + at, (bf16*)a.o[t] + at, m, f);
+  else chunk_scale((const float*)a.p[t] + at, (float*)a.o[t] + at, m, f);
+}
+
+int chunks_of(int64_t n, int64_t chunk) { return (int)std::max<int64_t>(1, (n + chunk - 1) / chunk); }
+
+}  // namespace
+
+size_t grad_norm_scratch(int n, const GradPlan& p) {   // partials, tensor sums, first chunks
+  return (size_t)p.chunks * 8 + (size_t)n * 8 + (size_t)n * 4 + 256;
+}
+
+hipError_t grad_norm(const mpipe_grad_tensor* t, int n, const GradPlan& p, double* sumsq,
+                     float* norms, char* scratch, hipStream_t s) {
+  double* partial = reinterpret_cast<double*>(scratch);
+  double* sums = partial + p.chunks;
+  int32_t* starts = reinterpret_cast<int32_t*>(sums + n);
+  int chunk0 = 0;
+  for (int i = 0; i < n;) {
+    NormArgs a;
+    const int tensor0 = i;
+    int k = 0, c = 0;
+    for (; i < n && k < kNormTensors; ++i, ++k) {
+      a.p[k] = t[i].data;
+      a.n[k] = t[i].n * 2 + (t[i].dtype == DT_BF16);
+      a.first[k] = c;
+      c += chunks_of(t[i].n, p.chunk);
+    }
+    hipLaunchKernelGGL(sumsq_kernel, dim3(c), dim3(256), 0, s, a, k, tensor0, chunk0, p.chunk,
+                       partial, starts);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    chunk0 += c;
+  }
+  if (n > 0) {
+    hipLaunchKernelGGL(tensor_sum_kernel, dim3(n), dim3(256), 0, s, partial, starts, n,
+                       (int)p.chunks, sums, norms);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(total_kernel, dim3(1), dim3(256), 0, s, sums, n, sumsq);
+  return hipGetLastError();
+}
+
+hipError_t grad_clip(const mpipe_grad_tensor* in, const mpipe_grad_tensor* out, int n,
+                     const GradPlan& p, const double* sumsq, double max_norm, float* norm,
+                     hipStream_t s) {
+  int i = 0;
+  do {
+    ClipArgs a;
+    int k = 0, c = 0;
+    for (; i < n && k < kClipTensors; ++i, ++k) {
+      a.p[k] = in[i].data;
+      a.o[k] = out[i].data;
+      a.n[k] = in[i].n * 4 + (in[i].dtype == DT_BF16) + 2 * (out[i].dtype == DT_BF16);
+      a.first[k] = c;
+      c += chunks_of(in[i].n, p.chunk);
+    }
+    hipLaunchKernelGGL(clip_kernel, dim3(std::max(c, 1)), dim3(256), 0, s, a, k, p.chunk, sumsq,
+                       max_norm, norm);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    norm = nullptr;
+  } while (i < n);
+  return hipSuccess;
+}
+
+}  // namespace mpipe

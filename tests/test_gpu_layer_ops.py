@@ -1,0 +1,748 @@
+"""Operators around the first LLM layer on the GPU, against their float64 forms
+(tests/layer_ref.py).
+
+Tolerances count roundings (fp32 2^-24, bf16 2^-8 relative, half a step each).
+  rotation  cos and sin are off by at most 2^-23 (the angle's rounding and the series'), each
+            product and sum by 2^-24 of itself: below 2^-22 (|a| + |b|) for a pair (a, b).
+  norm      a sum of at most 256 squares through at most 30 roundings, halved by the root,
+            and six more to the normed value: below 2^-19 of it, rotation included.
+  backward  the same two factors on both of its terms: below 2^-18 of their sizes.
+  gains     a term is off by 2^-19 of its size; the sum of N of them in fp32 by less than
+            2^-24 min(N, 1200) of the sum of sizes (no chain of additions is longer).
+  output    bf16 adds 2^-8 of the value."""
+import numpy as np
+import pytest
+
+from tests import layer_ref as R
+from tests.gpu_util import announce, torch_dev
+
+pytestmark = pytest.mark.gpu
+
+OUT = {"bf16": 2.0 ** -8, "f32": 0.0}
+
+CFGS = {
+    "d128_3axes": R.rope_cfg(128, [16, 24, 24], theta=1e6),
+    "d128_interleaved": R.rope_cfg(128, [24, 20, 20], theta=1e6, order=1),
+    "d80_yx": R.rope_cfg(80, [20, 20], spectrum=1),
+    "d64_part_adjacent": R.rope_cfg(64, [4, 6, 6], rot=32, pairing=1),
+    "d64_part_halves": R.rope_cfg(64, [8, 4], rot=24),
+    "d32_4axes": R.rope_cfg(32, [4, 4, 4, 4], order=1, spectrum=1, pairing=1),
+    "d256": R.rope_cfg(256, [128], theta=5e5),
+    "d256_adjacent_part": R.rope_cfg(256, [30, 45, 45], rot=240, pairing=1),
+    "d72": R.rope_cfg(72, [10, 0, 26]),
+    "d8": R.rope_cfg(8, [4]),
+    "d248": R.rope_cfg(248, [62, 62], pairing=1),
+    "d16_part": R.rope_cfg(16, [2, 2], rot=8),
+}
+
+
+def _mp():
+    import paper_2607_03229_amd as mp
+    return mp
+
+
+def _cfg(c):
+    return _mp().RopeCfg(c["head_dim"], c["sections"], rot_dim=c["rot_dim"], theta=c["theta"],
+                         order=c["order"], spectrum=c["spectrum"], pairing=c["pairing"])
+
+
+def _tdt(dtype):
+    import torch
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _rand(gen, shape, dtype):
+    torch, dev = torch_dev()
+    return torch.randn(shape, generator=gen).to(_tdt(dtype)).to(dev)
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _pos(rng, axes, rows, far=False):
+    torch, dev = torch_dev()
+    p = rng.integers(0, 2 ** 31 - 1 if far else 40000, (axes, rows)).astype(np.int32)
+    if far and rows > 1:
+        p[:, 1] = -p[:, 1]
+        p[:, 0] = 2 ** 31 - 1
+    return p, torch.from_numpy(p).to(dev)
+
+
+def _view(shape, dtype, layout):
+    """An empty [rows][heads][d] view in a buffer of NaN, and the buffer."""
+    torch, dev = torch_dev()
+    rows, heads, d = shape
+    nan = dict(dtype=_tdt(dtype), device=dev)
+    if layout == "dense":
+        b = torch.full((rows, heads, d), float("nan"), **nan)
+        return b, b
+    if layout == "head_major":
+        b = torch.full((heads, rows, d), float("nan"), **nan)
+        return b.transpose(0, 1), b
+    if layout == "fused":          # the first columns of a wider row
+        b = torch.full((rows, heads + 2, d), float("nan"), **nan)
+        return b[:, 1:heads + 1], b
+    assert layout == "shifted"     # one element off every larger alignment, ragged strides
+    b = torch.full((rows * (heads * (d + 1) + 3) + 1,), float("nan"), **nan)
+    return b[1:].as_strided((rows, heads, d), (heads * (d + 1) + 3, d + 1, 1)), b
+
+
+def _filled(gen, shape, dtype, layout):
+    v, b = _view(shape, dtype, layout)
+    v.copy_(_rand(gen, shape, dtype))
+    return v, b
+
+
+def _untouched(view, buf):
+    """Only the view's elements of the NaN buffer were written."""
+    import torch
+    n = int(torch.isnan(buf).sum())
+    return n == buf.numel() - view.numel() and not bool(torch.isnan(view).any())
+
+
+def _close(got, ref, scale, tol, dtype, what):
+    err = np.abs(_np(got) - ref)
+    bound = tol * scale + OUT[dtype] * np.abs(ref) + 1e-37
+    bad = err > bound
+    assert not bad.any(), (what, float((err / bound).max()), np.argwhere(bad)[:3].tolist())
+
+
+# ---- positions ----------------------------------------------------------------------------------
+
+def _image(rng, most):
+    return (1, 2 * int(rng.integers(1, most)), 2 * int(rng.integers(1, most)))
+
+
+def _position_cases():
+    rng = np.random.default_rng(11)
+    many, row = [], 3
+    for i in range(700):      # more spans than one launch takes
+        g = _image(rng, 4)
+        many.append((row, g, 1))
+        row += g[1] * g[2] // 4 + int(rng.integers(0, 3))
+    return {
+        "one_token": (8, [(3, 1, 70000)], []),
+        "decode": (40, [(i, 1, 1000 * i) for i in range(40)], []),
+        "text_only": (700, [(0, 700, 0)], []),
+        "image_only": (24, [(0, 24, 5)], [(0, (1, 8, 12), 1)]),
+        "image_first_and_last": (100, [(0, 100, 0)], [(0, (1, 4, 6), 1), (94, (1, 4, 6), 1)]),
+        "adjacent_items": (64, [(0, 64, 0)], [(10, (1, 4, 4), 1), (14, (3, 2, 8), 1), (26, (1, 2, 2), 1)]),
+        "clip_steps": (600, [(0, 600, 9)], [(4, (8, 6, 10), 2), (200, (5, 4, 4), 0), (300, (6, 4, 2), 25)]),
+        "padded": (300, [(0, 60, 0), (100, 100, 7), (200, 31, 0)],
+                   [(30, (1, 6, 8), 1), (110, (2, 8, 8), 1), (225, (1, 4, 6), 1)]),
+        "unordered_with_empty": (300, [(200, 50, 3), (90, 0, 4), (0, 80, 0)],
+                                 [(210, (1, 4, 8), 1), (10, (1, 8, 8), 1), (40, (1, 2, 2), 1)]),
+        "tall_and_wide": (400, [(0, 400, 0)], [(3, (1, 100, 2), 1), (60, (1, 2, 120), 1)]),
+        "largest_position": (20, [(0, 20, 2 ** 31 - 20)], []),
+        "many_items": (row + 50, [(0, row + 20, 1)], many),
+    }
+
+
+@pytest.mark.parametrize("name", _position_cases())
+@pytest.mark.parametrize("wide", [0, 5])
+def test_positions(name, wide):
+    torch, dev = torch_dev()
+    mp = _mp()
+    n, seqs, items = _position_cases()[name]
+    announce(f"seam positions {name}")
+    want = np.full((3, n + wide), -7, np.int32)
+    nxt = R.seam_positions(seqs, items, want)
+    buf = torch.full((3, n + wide), -7, dtype=torch.int32, device=dev)
+    got = mp.op_seam_positions([s[0] for s in seqs], [s[1] for s in seqs], [i[0] for i in items],
+                               [i[1] for i in items], buf[:, :n], seq_pos=[s[2] for s in seqs],
+                               time_step=[i[2] for i in items])
+    assert got.tolist() == nxt
+    assert np.array_equal(buf.cpu().numpy(), want)
+
+
+def test_positions_defaults():
+    """Without first positions and time steps: zeros and ones."""
+    torch, dev = torch_dev()
+    want = np.zeros((3, 90), np.int32)
+    nxt = R.seam_positions([(0, 90, 0)], [(7, (4, 6, 4), 1)], want)
+    pos = torch.zeros((3, 90), dtype=torch.int32, device=dev)
+    got = _mp().op_seam_positions([0], [90], [7], [[4, 6, 4]], pos)
+    assert got.tolist() == nxt and np.array_equal(pos.cpu().numpy(), want)
+
+
+# ---- rotation alone -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", CFGS)
+def test_rope(name, dtype):
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS[name]
+    d, axes = c["head_dim"], len(c["sections"])
+    rng, gen = np.random.default_rng(3), torch.Generator().manual_seed(4)
+    for rows, hq, hk, far in ((1, 4, 2, False), (37, 7, 3, True), (130, 28, 4, False)):
+        announce(f"rope_axes {name} {dtype} rows={rows} heads={hq}+{hk}")
+        p, pos = _pos(rng, axes, rows, far)
+        q, k = _rand(gen, (rows, hq, d), dtype), _rand(gen, (rows, hk, d), dtype)
+        (qo, qb), (ko, kb) = (_view(t.shape, dtype, "fused") for t in (q, k))
+        for inverse in (False, True):
+            mp.op_rope_axes(_cfg(c), q, k, pos, qo, ko, inverse=inverse)
+            for x, y in ((q, qo), (k, ko)):
+                ref = R.rotate(c, _np(x), p, inverse)
+                _close(y, ref, R.partners(c, _np(x)), 2.0 ** -22, dtype, (name, rows, inverse))
+        assert _untouched(qo, qb) and _untouched(ko, kb)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["dense", "head_major", "fused", "shifted"])
+@pytest.mark.parametrize("name", ["d128_3axes", "d64_part_adjacent", "d72"])
+def test_layouts(name, layout, dtype):
+    """Inputs and outputs of any strides and alignment, outputs in place, one side only: the
+    same bits as dense ones."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS[name]
+    cfg, d, axes, rows = _cfg(c), c["head_dim"], len(c["sections"]), 19
+    rng, gen = np.random.default_rng(8), torch.Generator().manual_seed(9)
+    announce(f"layouts {name} {layout} {dtype}")
+    _, pos = _pos(rng, axes, rows)
+    wide = torch.zeros((axes, rows + 3), dtype=torch.int32, device=dev)
+    wide[:, :rows] = pos
+    g = [_rand(gen, (d,), dtype) for _ in range(2)]
+    q, k = _filled(gen, (rows, 5, d), dtype, layout)[0], _filled(gen, (rows, 2, d), dtype, layout)[0]
+    dq, dk = _filled(gen, (rows, 5, d), dtype, layout)[0], _filled(gen, (rows, 2, d), dtype, layout)[0]
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, 5, 2, d), dtype=torch.uint8, device=dev)
+
+    def all_three(q, k, dq, dk, pos, out):
+        r = [out(q), out(k)]
+        mp.op_rope_axes(cfg, q, k, pos, r[0], r[1])
+        r += [out(q), out(k)]
+        mp.op_qk_norm_rope_fwd(cfg, q, k, g[0], g[1], 1e-6, pos, r[2], r[3])
+        r += [out(q), out(k)] + [torch.zeros(d, device=dev) for _ in range(2)]
+        mp.op_qk_norm_rope_bwd(cfg, dq, dk, q, k, g[0], g[1], 1e-6, pos, r[4], r[5], r[6], r[7], scratch)
+        return r
+
+    dense = [t.contiguous() for t in (q, k, dq, dk)]
+    want = all_three(*dense, pos, lambda t: torch.empty(t.shape, dtype=t.dtype, device=dev))
+    bufs = []
+
+    def out(t):
+        v, b = _view(t.shape, dtype, layout)
+        bufs.append((v, b))
+        return v
+
+    got = all_three(q, k, dq, dk, wide[:, :rows], out)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b.contiguous())
+    assert all(_untouched(v, b) for v, b in bufs)
+    # in place; k alone
+    for fwd in (lambda x, y, ko: mp.op_rope_axes(cfg, x, None, pos, y, None),
+                lambda x, y, ko: mp.op_qk_norm_rope_fwd(cfg, x, None, g[0], None, 1e-6, pos, y, None)):
+        x, _ = _view(q.shape, dtype, layout)
+        x.copy_(q)
+        y, _ = _view(q.shape, dtype, layout)
+        fwd(x, y, None)
+        fwd(x, x, None)
+        assert torch.equal(x, y)
+    x = k.clone()
+    mp.op_rope_axes(cfg, None, x, pos, None, x)
+    assert torch.equal(x, want[1])
+    # the backward over its output gradient, and over q
+    for over in (0, 1):
+        a, b = dense[2 - 2 * over].clone(), dense[3 - 2 * over].clone()
+        args = [(a, b, dense[0], dense[1]), (dense[2], dense[3], a, b)][over]
+        mp.op_qk_norm_rope_bwd(cfg, *args, g[0], g[1], 1e-6, pos, a, b, None, None, scratch)
+        assert torch.equal(a, want[4]) and torch.equal(b, want[5])
+
+
+def test_rope_into_one_product():
+    """q, k turned inside rows of q | k | v, in place: v and the rest stay."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d80_yx"]
+    rng, gen = np.random.default_rng(1), torch.Generator().manual_seed(1)
+    rows, h, d = 53, 4, 80
+    announce("rope in place inside a fused product")
+    p, pos = _pos(rng, 2, rows)
+    qkv = _rand(gen, (rows, 3 * h, d), "bf16")
+    old = qkv.clone()
+    mp.op_rope_axes(_cfg(c), qkv[:, :h], qkv[:, h:2 * h], pos, qkv[:, :h], qkv[:, h:2 * h])
+    assert torch.equal(qkv[:, 2 * h:], old[:, 2 * h:])
+    ref = R.rotate(c, _np(old[:, :2 * h]), p)
+    _close(qkv[:, :2 * h], ref, R.partners(c, _np(old[:, :2 * h])), 2.0 ** -22, "bf16", "fused")
+
+
+def test_rope_matches_the_encoder_kernel():
+    """(y, x) of patch rows: what op_rope computes from the grids."""
+    torch, dev = torch_dev()
+    import oracle
+    mp = _mp()
+    grid, h, d = np.array([[1, 6, 8], [2, 4, 4]], np.int32), 4, 64
+    y, x = oracle.positions(grid)
+    rows = len(y)
+    announce("rope against op_rope")
+    qkv = _rand(torch.Generator().manual_seed(6), (rows, 3 * h * d), "f32")
+    want = qkv.clone()
+    scratch = torch.empty(mp.op_scratch_bytes(rows, h, h * d, 2), dtype=torch.uint8, device=dev)
+    mp.op_rope(0, want, rows, h, d, grid, 10000.0, 0, scratch)
+    v = qkv.view(rows, 3 * h, d)
+    pos = torch.from_numpy(np.stack([y, x]).astype(np.int32)).to(dev)
+    mp.op_rope_axes(mp.RopeCfg(d, [16, 16], spectrum=mp.ROPE_AXIS_SPECTRA), v[:, :h], v[:, h:2 * h],
+                    pos, v[:, :h], v[:, h:2 * h])
+    # two roundings of cos, sin apart on values below 6
+    assert float((qkv - want).abs().max()) < 12 * 2.0 ** -22
+
+
+def test_values_stay_in_their_head():
+    """Infinities and NaN of one head, and of columns that do not turn, reach no other."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d64_part_halves"]
+    gen, rows, d = torch.Generator().manual_seed(2), 9, 64
+    announce("non-finite heads")
+    _, pos = _pos(np.random.default_rng(2), 2, rows)
+    q = _rand(gen, (rows, 3, d), "bf16")
+    bad = q.clone()
+    bad[4, 1, 50] = float("inf")     # a tail column
+    bad[6, 2, 3] = float("nan")
+    g = _rand(gen, (d,), "bf16")
+    for f in (lambda x, y: mp.op_rope_axes(_cfg(c), x, None, pos, y, None),
+              lambda x, y: mp.op_qk_norm_rope_fwd(_cfg(c), x, None, g, None, 1e-6, pos, y, None)):
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        f(q, a)
+        f(bad, b)
+        keep = torch.ones((rows, 3), dtype=torch.bool)
+        keep[4, 1] = keep[6, 2] = False
+        assert torch.equal(a[keep.to(dev)], b[keep.to(dev)])
+    mp.op_rope_axes(_cfg(c), bad, None, pos, b, None)
+    assert int((~torch.isfinite(b[4, 1])).sum()) == 1 and int(torch.isnan(b[6, 2]).sum()) == 2
+
+
+# ---- with the norm ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", CFGS)
+def test_norm_rope(name, dtype):
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS[name]
+    d, axes = c["head_dim"], len(c["sections"])
+    rng, gen = np.random.default_rng(13), torch.Generator().manual_seed(14)
+    for rows, hq, hk in ((1, 4, 2), (37, 7, 3), (130, 28, 4), (700, 3, 1)):
+        announce(f"norm_rope {name} {dtype} rows={rows} heads={hq}+{hk}")
+        p, pos = _pos(rng, axes, rows)
+        x = [_rand(gen, (rows, h, d), dtype) for h in (hq, hk)]
+        x[0][rows // 2] *= 1e-3       # small and zero heads: eps counts
+        x[0][0, 0] = 0
+        g = [1 + 0.2 * _rand(gen, (d,), dtype) for _ in range(2)]
+        outs = [_view(t.shape, dtype, "fused") for t in x]
+        mp.op_qk_norm_rope_fwd(_cfg(c), x[0], x[1], g[0], g[1], 1e-6, pos, outs[0][0], outs[1][0])
+        for z in range(2):
+            xn = _np(x[z])
+            r = 1.0 / np.sqrt((xn * xn).mean(-1, keepdims=True) + 1e-6)
+            eps32 = float(np.float32(1e-6))
+            ref = R.norm_rope(c, xn, _np(g[z]), eps32, p)
+            _close(outs[z][0], ref, R.partners(c, xn * r * _np(g[z])), 2.0 ** -19, dtype, (name, rows))
+            assert _untouched(*outs[z])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", CFGS)
+def test_norm_rope_backward(name, dtype):
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS[name]
+    d, axes = c["head_dim"], len(c["sections"])
+    rng, gen = np.random.default_rng(23), torch.Generator().manual_seed(24)
+    for rows, hq, hk in ((1, 4, 2), (37, 7, 3), (130, 28, 4), (1500, 3, 1)):
+        announce(f"norm_rope_bwd {name} {dtype} rows={rows} heads={hq}+{hk}")
+        p, pos = _pos(rng, axes, rows)
+        x = [_rand(gen, (rows, h, d), dtype) for h in (hq, hk)]
+        dy = [_rand(gen, (rows, h, d), dtype) for h in (hq, hk)]
+        x[0][0, 0] = 0
+        g = [1 + 0.2 * _rand(gen, (d,), dtype) for _ in range(2)]
+        outs = [_view(t.shape, dtype, "fused") for t in x]
+        base = [torch.randn(d, generator=gen).to(dev) for _ in range(2)]
+        grad = [b.clone() for b in base]
+        scratch = torch.full((mp.op_qk_norm_rope_scratch_bytes(rows, hq, hk, d) + 64,), 0xA5,
+                             dtype=torch.uint8, device=dev)
+        args = (_cfg(c), dy[0], dy[1], x[0], x[1], g[0], g[1], 1e-6, pos, outs[0][0], outs[1][0])
+        mp.op_qk_norm_rope_bwd(*args, grad[0], grad[1], scratch[:-64])
+        assert bool((scratch[-64:] == 0xA5).all())
+        over = [torch.full((d,), float("nan"), device=dev) for _ in range(2)]
+        first = [o[0].clone() for o in outs]
+        mp.op_qk_norm_rope_bwd(*args, over[0], over[1], scratch, accumulate=False)
+        for z in range(2):
+            dx, dg, sx, sg = R.norm_rope_bwd(c, _np(dy[z]), _np(x[z]), _np(g[z]),
+                                             float(np.float32(1e-6)), p)
+            _close(outs[z][0], dx, sx, 2.0 ** -18, dtype, (name, rows, "dx"))
+            n = min(rows * x[z].shape[1], 1200)
+            _close(over[z], dg, sg, 2.0 ** -19 + n * 2.0 ** -24, "f32", (name, rows, "dg"))
+            # accumulate: one more rounding of the sum
+            assert torch.equal(grad[z], base[z] + over[z])
+            assert torch.equal(first[z], outs[z][0]) and _untouched(*outs[z])
+
+
+def test_norm_rope_backward_of_nothing():
+    """No rows: overwritten gains are zero, accumulated ones stay; one side and no gains."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d128_3axes"]
+    announce("norm_rope_bwd of no rows")
+    e = torch.empty((0, 4, 128), dtype=torch.bfloat16, device=dev)
+    g = torch.ones(128, dtype=torch.bfloat16, device=dev)
+    pos = torch.empty((3, 0), dtype=torch.int32, device=dev)
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(0, 4, 4, 128), dtype=torch.uint8, device=dev)
+    for acc, want in ((True, 3.0), (False, 0.0)):
+        grad = [torch.full((128,), 3.0, device=dev) for _ in range(2)]
+        mp.op_qk_norm_rope_bwd(_cfg(c), e, e, e, e, g, g, 1e-6, pos, e, e, grad[0], grad[1], scratch,
+                               accumulate=acc)
+        assert all(bool((t == want).all()) for t in grad)
+    mp.op_rope_axes(_cfg(c), e, e, pos, e, e)
+    mp.op_qk_norm_rope_fwd(_cfg(c), e, None, g, None, 1e-6, pos, e, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_rope_gradient_by_differences(dtype):
+    """The backward's directional derivative against the kernel's own forward in fp32, and on
+    bf16 values against the fp32 backward."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d64_part_adjacent"]
+    cfg, rows, h, d = _cfg(c), 11, 3, 64
+    gen = torch.Generator().manual_seed(31)
+    announce(f"norm_rope differences {dtype}")
+    _, pos = _pos(np.random.default_rng(3), 3, rows)
+    x, dy = _rand(gen, (rows, h, d), dtype), _rand(gen, (rows, h, d), dtype)
+    g = _rand(gen, (d,), dtype)
+    grad, gg = torch.empty_like(x), torch.empty(d, device=dev)
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, h, 0, d), dtype=torch.uint8, device=dev)
+    mp.op_qk_norm_rope_bwd(cfg, dy, None, x, None, g, None, 1e-3, pos, grad, None, gg, None, scratch,
+                           accumulate=False)
+    xf, gf, dyf = x.float(), g.float(), dy.float()
+
+    def loss(x, g):
+        y = torch.empty_like(x)
+        mp.op_qk_norm_rope_fwd(cfg, x, None, g, None, 1e-3, pos, y, None)
+        return float((y.double() * dyf.double()).sum())
+
+    h_ = 2.0 ** -7
+    for var, got in ((xf, grad.double()), (gf, gg.double())):
+        v = _rand(gen, tuple(var.shape), "f32")
+        a = (var + h_ * v, gf) if var is xf else (xf, var + h_ * v)
+        b = (var - h_ * v, gf) if var is xf else (xf, var - h_ * v)
+        diff = (loss(*a) - loss(*b)) / (2 * h_)
+        dot = float((got * v.double()).sum())
+        # 2112 outputs of size below 4, each off by 2^-19 |dy| y / h_: sum in quadrature below
+        # 0.2, and the h_^2 term of x (third derivatives of order |x / rms|^3 |dy|) below 0.5;
+        # bf16 gradients are off by 2^-8 each: 2^-8 sqrt(2112) * 2 below 0.4
+        assert abs(diff - dot) < 1.1, (diff, dot)
+
+
+def test_norm_rope_far_rows():
+    """Offsets past 32 bits: rows 2^20 elements apart, the last at 2^32."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d128_3axes"]
+    rows, d = 4100, 128
+    announce("norm_rope past 32-bit offsets")
+    buf = torch.empty(((rows - 1) << 20) + 256, dtype=torch.bfloat16, device=dev)
+    x = buf.as_strided((rows, 2, d), (1 << 20, d, 1))
+    gen = torch.Generator().manual_seed(5)
+    dense = _rand(gen, (rows, 2, d), "bf16")
+    x.copy_(dense)
+    g = _rand(gen, (d,), "bf16")
+    _, pos = _pos(np.random.default_rng(4), 3, rows)
+    want = torch.empty_like(dense)
+    mp.op_qk_norm_rope_fwd(_cfg(c), dense, None, g, None, 1e-6, pos, want, None)
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, 2, 0, d), dtype=torch.uint8, device=dev)
+    dw, dx = torch.empty_like(dense), torch.empty_like(dense)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dense, None, dense, None, g, None, 1e-6, pos, dw, None, None, None, scratch)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dense, None, x, None, g, None, 1e-6, pos, dx, None, None, None, scratch)
+    assert torch.equal(dx, dw)
+    mp.op_qk_norm_rope_fwd(_cfg(c), x, None, g, None, 1e-6, pos, x, None)
+    assert torch.equal(x.contiguous(), want)
+
+
+# ---- gradients' norm and clip --------------------------------------------------------------------------
+
+LISTS = {
+    "one_element": [1],
+    "one": [100003],
+    "empties": [0, 5, 0, 0, 4097, 0],
+    "odd": [1, 2, 3, 7, 8, 9, 255, 256, 257, 4095, 4096, 4097, 8193, 12289],
+    "many": [(7 * i * i) % 1031 for i in range(450)],     # several launches' worth
+    "long": [9_000_001, 13],
+}
+
+
+def _grads(gen, sizes, dtype, shift, scale=1.0):
+    """Views of one buffer that starts `shift` elements off alignment, three elements apart."""
+    torch, dev = torch_dev()
+    buf = _rand(gen, (sum(sizes) + 3 * len(sizes) + shift,), dtype) * scale
+    out, at = [], shift
+    for n in sizes:
+        out.append(buf[at:at + n])
+        at += n + 3
+    return out, buf
+
+
+def _norm_call(ts):
+    torch, dev = torch_dev()
+    mp = _mp()
+    sumsq = torch.full((1,), float("nan"), dtype=torch.float64, device=dev)
+    norms = torch.full((len(ts),), float("nan"), device=dev)
+    nbytes = mp.op_grad_scratch_bytes(ts)
+    scratch = torch.full((nbytes + 64,), 0xA5, dtype=torch.uint8, device=dev)
+    mp.op_grad_norm(ts, sumsq, norms, scratch[:nbytes])
+    assert bool((scratch[nbytes:] == 0xA5).all())
+    return sumsq, norms
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("name", LISTS)
+def test_grad_clip(name, dtype, out):
+    torch, dev = torch_dev()
+    mp = _mp()
+    sizes, gen = LISTS[name], torch.Generator().manual_seed(41)
+    for shift in (0, 1):
+        announce(f"grad clip {name} {dtype}->{out} shift={shift}")
+        ts, buf = _grads(gen, sizes, dtype, shift)
+        ref = [_np(t) for t in ts]
+        want = np.sqrt([float((r * r).sum()) for r in ref])
+        total = float(np.sqrt((want ** 2).sum()))
+        sumsq, norms = _norm_call(ts)
+        # fp64 sums of exact squares, one rounding to fp32
+        assert abs(float(sumsq) ** 0.5 - total) <= 1e-12 * total
+        assert np.all(np.abs(_np(norms) - want) <= 2.0 ** -24 * want)
+        again, _ = _norm_call(ts)
+        assert torch.equal(sumsq, again)
+        for max_norm in (0.5 * total, 2.0 * total):
+            f = min(1.0, max_norm / total)
+            os, obuf = _grads(gen, sizes, out, 1 - shift)
+            before = obuf.clone()
+            norm = torch.zeros(1, device=dev)
+            mp.op_grad_clip(ts, sumsq, max_norm, norm, out=os)
+            assert abs(float(norm) - total) <= 2.0 ** -24 * total
+            for r, o in zip(ref, os):
+                _close(o, r * f, np.abs(r * f), 2.0 ** -23, out, (name, max_norm))
+                if f == 1.0 and dtype == out:
+                    assert np.array_equal(_np(o), r)
+            # what lies between the outputs stays
+            for o in os:
+                o.zero_()
+            at = 1 - shift
+            for n in sizes:
+                before[at:at + n] = 0
+                at += n + 3
+            assert torch.equal(before, obuf)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_grad_clip_in_place(dtype):
+    torch, dev = torch_dev()
+    mp, gen = _mp(), torch.Generator().manual_seed(43)
+    announce(f"grad clip in place {dtype}")
+    ts, buf = _grads(gen, LISTS["odd"], dtype, 3)
+    keep = buf.clone()
+    sumsq, _ = _norm_call(ts)
+    total = float(sumsq) ** 0.5
+    mp.op_grad_clip(ts, sumsq, 2 * total)
+    assert torch.equal(buf, keep)
+    other = [torch.empty_like(t) for t in ts]
+    mp.op_grad_clip(ts, sumsq, 0.3 * total, out=other)
+    assert torch.equal(buf, keep)
+    # some in place, some not; then all of them
+    mixed = [t if i % 2 else torch.empty_like(t) for i, t in enumerate(ts)]
+    mp.op_grad_clip(ts, sumsq, 0.3 * total, out=mixed)
+    assert all(torch.equal(a, b) for a, b in zip(mixed, other))
+    buf.copy_(keep)
+    mp.op_grad_clip(ts, sumsq, 0.3 * total)
+    assert all(torch.equal(a, b) for a, b in zip(ts, other))
+    at = 3
+    for t in ts:       # only the tensors' elements changed
+        buf[at:at + t.numel()] = keep[at:at + t.numel()]
+        at += t.numel() + 3
+    assert torch.equal(buf, keep)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_grad_clip_not_finite(value):
+    """The norm shows it; gradients in place stay, outputs are copies."""
+    torch, dev = torch_dev()
+    mp, gen = _mp(), torch.Generator().manual_seed(44)
+    announce(f"grad clip with {value}")
+    ts, buf = _grads(gen, [1000, 77], "f32", 0)
+    ts[0][500] = value
+    keep = buf.clone()
+    sumsq, norms = _norm_call(ts)
+    norm = torch.zeros(1, device=dev)
+    out = [torch.zeros_like(t) for t in ts]
+    mp.op_grad_clip(ts, sumsq, 1e-3, norm)
+    mp.op_grad_clip(ts, sumsq, 1e-3, None, out=out)
+    same = lambda a, b: bool(((a == b) | (a.isnan() & b.isnan())).all())
+    assert same(buf, keep) and all(same(a, b) for a, b in zip(ts, out))
+    want = float("nan") if value != value else float("inf")
+    assert str(float(norm)) == str(want) and str(float(norms[0])) == str(want)
+    assert np.isfinite(float(norms[1]))
+
+
+def test_grad_norm_extremes():
+    """Squares beyond fp32's range at both ends; all zeros; nothing at all; max_norm 0 and
+    infinity."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce("grad norm extremes")
+    big = [torch.full((3,), 3e38, device=dev)]
+    sumsq, norms = _norm_call(big)
+    assert abs(float(sumsq) ** 0.5 / (3 ** 0.5 * float(np.float32(3e38))) - 1) < 1e-12
+    assert float(norms[0]) == float("inf")          # beyond fp32, but the clip knows better
+    out = [torch.zeros(3, device=dev)]
+    mp.op_grad_clip(big, sumsq, 1.0, out=out)
+    assert np.allclose(_np(out[0]), 3 ** -0.5, rtol=2.0 ** -22)
+    small = [torch.full((4,), 1e-38, device=dev)]
+    sumsq, norms = _norm_call(small)
+    assert abs(float(norms[0]) / 2e-38 - 1) < 2.0 ** -22
+    zero = [torch.zeros(5000, device=dev)]
+    sumsq, norms = _norm_call(zero)
+    norm = torch.ones(1, device=dev)
+    mp.op_grad_clip(zero, sumsq, 0.0, norm)
+    assert float(sumsq) == 0 and float(norm) == 0 and bool((zero[0] == 0).all())
+    t = [torch.ones(100, device=dev)]
+    sumsq, _ = _norm_call(t)
+    mp.op_grad_clip(t, sumsq, float("inf"))
+    assert bool((t[0] == 1).all())
+    mp.op_grad_clip(t, sumsq, 0.0)
+    assert bool((t[0] == 0).all())
+    sumsq = torch.ones(1, dtype=torch.float64, device=dev)
+    scratch = torch.empty(mp.op_grad_scratch_bytes([]), dtype=torch.uint8, device=dev)
+    mp.op_grad_norm([], sumsq, None, scratch)
+    mp.op_grad_clip([], sumsq, 1.0, norm)
+    assert float(sumsq) == 0 and float(norm) == 0
+
+
+# ---- streams, graphs, all of them together ----------------------------------------------------------------
+
+def test_other_stream_and_graph():
+    """On a stream of its own, captured with two graphs, replayed with new inputs and eager
+    calls between; every replay has the bits of the eager call."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d128_3axes"]
+    cfg, rows, d = _cfg(c), 300, 128
+    gen = torch.Generator().manual_seed(51)
+    announce("layer operators on a stream and in graphs")
+    pos = torch.zeros((3, rows), dtype=torch.int32, device=dev)
+    q, k, dq, dk = (_rand(gen, (rows, h, d), "bf16") for h in (6, 2, 6, 2))
+    g = [_rand(gen, (d,), "bf16") for _ in range(2)]
+    out = [torch.empty_like(t) for t in (q, k, dq, dk)]
+    gg = [torch.zeros(d, device=dev) for _ in range(2)]
+    sc = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, 6, 2, d), dtype=torch.uint8, device=dev)
+    sumsq, norm = torch.empty(1, dtype=torch.float64, device=dev), torch.empty(1, device=dev)
+    gs = torch.empty(mp.op_grad_scratch_bytes(gg), dtype=torch.uint8, device=dev)
+    clipped = [torch.empty_like(t) for t in gg]
+
+    def step(stream=None):
+        mp.op_seam_positions([0], [rows], [20], [[2, 12, 16]], pos, stream=stream)
+        mp.op_qk_norm_rope_fwd(cfg, q, k, *g, 1e-6, pos, out[0], out[1], stream=stream)
+        mp.op_qk_norm_rope_bwd(cfg, dq, dk, q, k, *g, 1e-6, pos, out[2], out[3], *gg, sc,
+                               accumulate=False, stream=stream)
+        mp.op_grad_norm(gg, sumsq, None, gs, stream=stream)
+        mp.op_grad_clip(gg, sumsq, 1.0, norm, out=clipped, stream=stream)
+
+    def snapshot():
+        torch.cuda.synchronize()
+        return [t.clone() for t in out + gg + clipped + [pos, sumsq, norm]]
+
+    def wipe():
+        for t in out + gg + clipped + [pos, sumsq, norm]:
+            t.zero_()
+        torch.cuda.synchronize()
+
+    step()
+    want = snapshot()
+    s = torch.cuda.Stream()
+    wipe()
+    step(stream=s)
+    assert all(torch.equal(a, b) for a, b in zip(snapshot(), want))
+    graphs = []
+    for _ in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step()
+        graphs.append(gr)
+    for i in range(4):
+        q.copy_(_rand(gen, q.shape, "bf16"))
+        step()
+        want = snapshot()
+        wipe()
+        graphs[i % 2].replay()
+        assert all(torch.equal(a, b) for a, b in zip(snapshot(), want)), i
+
+
+def test_a_trained_step_together():
+    """The tiny encoder's merged rows through the seam into a layer's q and k: positions, the
+    product, norm and rotation, back to the embeddings, the encoder's backward, and the whole
+    gradient's norm and clip -- each against its float64 form on the values it was given."""
+    torch, dev = torch_dev()
+    import workload as W
+    mp = _mp()
+    announce("a trained step through the layer operators")
+    wl = W.make_workload("c1_tiny_fp32", 3)
+    cfg, H, rows = wl.cfg, wl.cfg.llm_hidden, wl.emb_rows
+    enc = mp.Encoder(cfg)
+    s = enc.sizes(wl.cu_seqlens, wl.grid_thw, True)
+    f = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(dev)
+    w, x = f(wl.weights()), f(wl.patches())
+    merged = torch.empty((s["n_merged"], H), device=dev)
+    tape, ws = (torch.empty(s[n], dtype=torch.uint8, device=dev) for n in ("tape", "workspace"))
+    enc.fwd(w, x, wl.cu_seqlens, wl.grid_thw, True, merged, tape, ws)
+    place = wl.placeholders()
+    idx, emb = torch.from_numpy(place).to(dev), f(wl.emb_init())
+    mp.merge_scatter(merged, idx, emb)
+    # positions of the two sequences, items where their first merged row lies
+    first = np.concatenate([[0], np.cumsum(wl.merged_per_item)[:-1]])
+    S = wl.spec.emb_seq_len
+    pos = torch.empty((3, rows), dtype=torch.int32, device=dev)
+    nxt = mp.op_seam_positions([0, S], [S, S], place[first], wl.grid_thw, pos)
+    want = np.zeros((3, rows), np.int32)
+    assert nxt.tolist() == R.seam_positions(
+        [(0, S, 0), (S, S, 0)],
+        [(int(place[i]), tuple(int(v) for v in g), 1) for i, g in zip(first, wl.grid_thw)], want)
+    assert np.array_equal(pos.cpu().numpy(), want)
+    # q and k of a layer: one product, norm, rotation
+    hq, hk, d = 6, 2, 64
+    c = R.rope_cfg(d, [8, 12, 12], theta=1e6)
+    gen = torch.Generator().manual_seed(61)
+    wqk = _rand(gen, ((hq + hk) * d, H), "f32") * 0.05
+    qk = torch.empty((rows, hq + hk, d), device=dev)
+    n = (hq + hk) * d
+    mp.op_gemm(0, 0, 0, rows, n, H, emb, H, wqk, H, qk, n)
+    gains = [1 + 0.1 * _rand(gen, (d,), "f32") for _ in range(2)]
+    out = torch.empty_like(qk)
+    sides = ((slice(0, hq), gains[0]), (slice(hq, hq + hk), gains[1]))
+    mp.op_qk_norm_rope_fwd(_cfg(c), qk[:, :hq], qk[:, hq:], *gains, 1e-6, pos, out[:, :hq], out[:, hq:])
+    for sl, g in sides:
+        v = _np(qk[:, sl])
+        r = 1.0 / np.sqrt((v * v).mean(-1, keepdims=True) + 1e-6)
+        _close(out[:, sl], R.norm_rope(c, v, _np(g), float(np.float32(1e-6)), want),
+               R.partners(c, v * r * _np(g)), 2.0 ** -19, "f32", "forward")
+    # back: rotation and norm, the product, the gather, the encoder
+    dout = _rand(gen, tuple(out.shape), "f32")
+    dqk = torch.empty_like(qk)
+    ggain = [torch.zeros(d, device=dev) for _ in range(2)]
+    sc = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, hq, hk, d), dtype=torch.uint8, device=dev)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dout[:, :hq], dout[:, hq:], qk[:, :hq], qk[:, hq:], *gains, 1e-6,
+                           pos, dqk[:, :hq], dqk[:, hq:], *ggain, sc)
+    for (sl, g), gg in zip(sides, ggain):
+        dx, dg, sx, sg = R.norm_rope_bwd(c, _np(dout[:, sl]), _np(qk[:, sl]), _np(g),
+                                         float(np.float32(1e-6)), want)
+        _close(dqk[:, sl], dx, sx, 2.0 ** -18, "f32", "backward")
+        _close(gg, dg, sg, 2.0 ** -19 + 1200 * 2.0 ** -24, "f32", "gains")
+    demb = torch.empty_like(emb)
+    mp.op_gemm(0, 1, 0, rows, H, n, dqk, n, wqk, H, demb, H)
+    dwqk = torch.empty_like(wqk)
+    mp.op_gemm(0, 2, 4, n, H, rows, dqk, n, emb, H, dwqk, H)
+    dm = torch.empty_like(merged)
+    mp.merge_gather(demb, idx, dm)
+    dw = torch.zeros(w.numel(), device=dev)
+    enc.bwd(w, x, wl.cu_seqlens, wl.grid_thw, True, tape, dm, dw, None, ws)
+    # the whole gradient: the encoder's tensors as views of its flat buffer, the layer's
+    grads = [dw[o:o + r * cc] for _, o, r, cc in enc.param_table()] + [dwqk] + ggain
+    gl = mp.GradList(grads)
+    sumsq, norm = torch.empty(1, dtype=torch.float64, device=dev), torch.empty(1, device=dev)
+    norms = torch.empty(gl.n, device=dev)
+    mp.op_grad_norm(gl, sumsq, norms, torch.empty(mp.op_grad_scratch_bytes(gl), dtype=torch.uint8, device=dev))
+    ref = [_np(t) for t in grads]
+    total = float(np.sqrt(sum((r * r).sum() for r in ref)))
+    mp.op_grad_clip(gl, sumsq, 0.1 * total, norm)
+    assert abs(float(norm) / total - 1) <= 2.0 ** -24
+    for r, t in zip(ref, grads):
+        _close(t, 0.1 * r, np.abs(0.1 * r), 2.0 ** -23, "f32", "clip")
+    enc.close()
