@@ -95,27 +95,31 @@ template <int V, bool ADJ> struct Lane {
   static __device__ __forceinline__ constexpr int second(int i) { return ADJ ? 2 * i + 1 : V + i; }
 };
 
-template <class T, int V, bool ADJ>
-__device__ __forceinline__ void load_head(const T* p, const Lane<V, ADJ>& l, bool on,
-                                          Words<T, V> (&r)[2]) {
+// Lanes that are off keep whatever their registers held: what they compute is not stored, and
+// columns past the head are set to zero before a sum.  (Zeroing the registers first would
+// make every load wait for the one before.)
+template <class T, int V>
+__device__ __forceinline__ void load_head(const T* p, const int64_t (&off)[2], const bool (&on)[2],
+                                          bool head, Words<T, V> (&r)[2]) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    r[k] = 0;
-    if (on && l.on[k]) r[k] = *reinterpret_cast<const typename Vec<T, V>::At*>(p + l.col[k]);
+    r[k] = __builtin_nondeterministic_value(r[k]);
+    if (head && on[k]) r[k] = *reinterpret_cast<const typename Vec<T, V>::At*>(p + off[k]);
   }
 }
 template <class T, int V>
-__device__ __forceinline__ void widen(const Words<T, V> (&r)[2], float (&v)[2 * V]) {
+__device__ __forceinline__ void widen(const Words<T, V> (&r)[2], const bool (&on)[2],
+                                      float (&v)[2 * V]) {
   constexpr int E = 4 / sizeof(T);   // elements of a word
 #pragma unroll
   for (int i = 0; i < 2 * V; ++i) {
     const uint32_t w = r[i / V][i % V / E];
-    v[i] = __uint_as_float(E == 1 ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
+    v[i] = on[i / V] ? __uint_as_float(E == 1 ? w : i % 2 ? w & 0xFFFF0000u : w << 16) : 0.f;
   }
 }
-template <class T, int V, bool ADJ>
-__device__ __forceinline__ void store_head(T* p, const Lane<V, ADJ>& l, bool on,
-                                           const float (&v)[2 * V]) {
+template <class T, int V>
+__device__ __forceinline__ void store_head(T* p, const int64_t (&off)[2], const bool (&on)[2],
+                                           bool head, const float (&v)[2 * V]) {
   constexpr int E = 4 / sizeof(T);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -130,7 +134,7 @@ __device__ __forceinline__ void store_head(T* p, const Lane<V, ADJ>& l, bool on,
         r[i] = __builtin_bit_cast(uint32_t, t);
       }
     }
-    if (on && l.on[k]) *reinterpret_cast<typename Vec<T, V>::At*>(p + l.col[k]) = r;
+    if (head && on[k]) *reinterpret_cast<typename Vec<T, V>::At*>(p + off[k]) = r;
   }
 }
 
@@ -191,37 +195,49 @@ struct Place {
 };
 constexpr int kTrig = 512;   // pairs of a wave's rows: at most 64 lanes * 8
 
+// A view as a wave walks it: the lane's offsets from the wave's first row and head, and the
+// (scalar) way to those.
+template <class T> struct Walk {
+  const T* base;
+  int64_t row, head, off[2];
+  __device__ __forceinline__ Walk(const void* p, int64_t row_stride, int64_t head_stride,
+                                  const Place& at, const int (&col)[2])
+      : base(reinterpret_cast<const T*>(p)), row(row_stride), head(head_stride) {
+    for (int k = 0; k < 2; ++k) off[k] = at.rs * row + at.hs * head + col[k];
+  }
+  __device__ __forceinline__ const T* at(int64_t r, int h) const { return base + r * row + h * head; }
+};
+
 template <class T, int V, bool ADJ, bool NORM>
-__global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a) {
-  constexpr int U = 4;
+__global__ __launch_bounds__(256, 4) void qk_fwd_kernel(QkArgs a) {
+  constexpr int U = 2;   // heads loaded ahead
   __shared__ float trig[4][2][kTrig];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int z = (int)blockIdx.x >= a.side[0].blocks;
   const SideArgs& sd = a.side[z];
   const int log_c = a.log_c, log_h = sd.log_h, block = blockIdx.x - (z ? a.side[0].blocks : 0);
   const Place at(lane, log_c, log_h);
   const Lane<V, ADJ> l(at.c, a.half, a.d);
+  const Walk<T> x(sd.x, sd.x_row, sd.x_head, at, l.col), y(sd.y, sd.y_row, sd.y_head, at, l.col);
   float* cs = trig[wave][0];
   float* sn = trig[wave][1];
   float g[2 * V];
   if (NORM) {
     Words<T, V> r[2];
-    load_head<T, V, ADJ>(reinterpret_cast<const T*>(sd.gain), l, true, r);
-    widen<T, V>(r, g);
+    const int64_t off[2] = {l.col[0], l.col[1]};
+    load_head<T, V>(reinterpret_cast<const T*>(sd.gain), off, l.on, true, r);
+    widen<T, V>(r, l.on, g);
   }
   for (int item = block * 4 + wave; item < sd.items; item += sd.blocks * 4) {
     const int rg = item / sd.head_groups, hg = item - rg * sd.head_groups;
-    const int64_t row = ((int64_t)rg << (6 - log_c - log_h)) + at.rs;
-    const int head0 = ((hg * sd.iters) << log_h) + at.hs;
-    const T* x = reinterpret_cast<const T*>(sd.x) + row * sd.x_row + head0 * sd.x_head;
-    T* y = reinterpret_cast<T*>(sd.y) + row * sd.y_row + head0 * sd.y_head;
-    const int64_t x_step = sd.x_head << log_h, y_step = sd.y_head << log_h;
-    const int left = row < a.rows ? sd.heads - head0 : 0;   // heads from here on
+    const int64_t row0 = (int64_t)rg << (6 - log_c - log_h);
+    const int head0 = (hg * sd.iters) << log_h, n = min(sd.iters << log_h, sd.heads - head0);
+    const int left = row0 + at.rs < a.rows ? n - at.hs : 0;   // heads from the lane's first on
     Words<T, V> r[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (u < sd.iters) load_head<T, V, ADJ>(x + u * x_step, l, (u << log_h) < left, r[u]);
-    wave_trig(a, cs, sn, row, at.rs, at.sub, 1 << (log_c + log_h));
+      load_head<T, V>(x.at(row0, head0 + (u << log_h)), x.off, l.on, (u << log_h) < left, r[u]);
+    wave_trig(a, cs, sn, row0 + at.rs, at.rs, at.sub, 1 << (log_c + log_h));
     float c[V], s[V];
     if (l.turns) {
 #pragma unroll
@@ -231,18 +247,13 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a) {
       }
     }
     __builtin_amdgcn_wave_barrier();
-    for (int it = 0; it < sd.iters; it += U) {
-      if (it > 0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (it + u < sd.iters)
-            load_head<T, V, ADJ>(x + (it + u) * x_step, l, ((it + u) << log_h) < left, r[u]);
-      }
+    for (int h = 0;;) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (it + u >= sd.iters) break;
+        if (h + (u << log_h) >= n) break;
+        __builtin_amdgcn_sched_barrier(0);   // one head at a time, or registers run out
         float v[2 * V];
-        widen<T, V>(r[u], v);
+        widen<T, V>(r[u], l.on, v);
         if (NORM) {
           float ss = 0.f;
 #pragma unroll
@@ -252,50 +263,54 @@ __global__ __launch_bounds__(256) void qk_fwd_kernel(QkArgs a) {
           for (int i = 0; i < 2 * V; ++i) v[i] = v[i] * k * g[i];
         }
         turn<V, ADJ>(l, c, s, v);
-        store_head<T, V, ADJ>(y + (it + u) * y_step, l, ((it + u) << log_h) < left, v);
+        store_head<T, V>(const_cast<T*>(y.at(row0, head0 + h + (u << log_h))), y.off, l.on,
+                         h + (u << log_h) < left, v);
       }
+      h += U << log_h;
+      if (h >= n) break;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        load_head<T, V>(x.at(row0, head0 + h + (u << log_h)), x.off, l.on,
+                        h + (u << log_h) < left, r[u]);
     }
   }
 }
 
 template <class T, int V, bool ADJ>
-__global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a) {
+__global__ __launch_bounds__(256, 3) void qk_bwd_kernel(QkArgs a) {
   constexpr int U = 2;
   __shared__ float trig[4][2][kTrig];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int z = (int)blockIdx.x >= a.side[0].blocks;
   const SideArgs& sd = a.side[z];
   const int log_c = a.log_c, log_h = sd.log_h, block = blockIdx.x - (z ? a.side[0].blocks : 0);
   const Place at(lane, log_c, log_h);
   const Lane<V, ADJ> l(at.c, a.half, a.d);
+  const Walk<T> x(sd.x, sd.x_row, sd.x_head, at, l.col), dy(sd.dy, sd.dy_row, sd.dy_head, at, l.col),
+      y(sd.y, sd.y_row, sd.y_head, at, l.col);
   float* cs = trig[wave][0];
   float* sn = trig[wave][1];
   float g[2 * V], dg[2 * V];
   {
     Words<T, V> r[2];
-    load_head<T, V, ADJ>(reinterpret_cast<const T*>(sd.gain), l, true, r);
-    widen<T, V>(r, g);
+    const int64_t off[2] = {l.col[0], l.col[1]};
+    load_head<T, V>(reinterpret_cast<const T*>(sd.gain), off, l.on, true, r);
+    widen<T, V>(r, l.on, g);
   }
 #pragma unroll
   for (int i = 0; i < 2 * V; ++i) dg[i] = 0.f;
   for (int item = block * 4 + wave; item < sd.items; item += sd.blocks * 4) {
     const int rg = item / sd.head_groups, hg = item - rg * sd.head_groups;
-    const int64_t row = ((int64_t)rg << (6 - log_c - log_h)) + at.rs;
-    const int head0 = ((hg * sd.iters) << log_h) + at.hs;
-    const T* x = reinterpret_cast<const T*>(sd.x) + row * sd.x_row + head0 * sd.x_head;
-    const T* dy = reinterpret_cast<const T*>(sd.dy) + row * sd.dy_row + head0 * sd.dy_head;
-    T* y = reinterpret_cast<T*>(sd.y) + row * sd.y_row + head0 * sd.y_head;
-    const int64_t x_step = sd.x_head << log_h, dy_step = sd.dy_head << log_h,
-                  y_step = sd.y_head << log_h;
-    const int left = row < a.rows ? sd.heads - head0 : 0;
+    const int64_t row0 = (int64_t)rg << (6 - log_c - log_h);
+    const int head0 = (hg * sd.iters) << log_h, n = min(sd.iters << log_h, sd.heads - head0);
+    const int left = row0 + at.rs < a.rows ? n - at.hs : 0;
     Words<T, V> rx[U][2], rd[U][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (u < sd.iters) {
-        load_head<T, V, ADJ>(x + u * x_step, l, (u << log_h) < left, rx[u]);
-        load_head<T, V, ADJ>(dy + u * dy_step, l, (u << log_h) < left, rd[u]);
-      }
-    wave_trig(a, cs, sn, row, at.rs, at.sub, 1 << (log_c + log_h));
+    for (int u = 0; u < U; ++u) {
+      load_head<T, V>(x.at(row0, head0 + (u << log_h)), x.off, l.on, (u << log_h) < left, rx[u]);
+      load_head<T, V>(dy.at(row0, head0 + (u << log_h)), dy.off, l.on, (u << log_h) < left, rd[u]);
+    }
+    wave_trig(a, cs, sn, row0 + at.rs, at.rs, at.sub, 1 << (log_c + log_h));
     float c[V], s[V];
     if (l.turns) {
 #pragma unroll
@@ -305,21 +320,15 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a) {
       }
     }
     __builtin_amdgcn_wave_barrier();
-    for (int it = 0; it < sd.iters; it += U) {
-      if (it > 0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (it + u < sd.iters) {
-            load_head<T, V, ADJ>(x + (it + u) * x_step, l, ((it + u) << log_h) < left, rx[u]);
-            load_head<T, V, ADJ>(dy + (it + u) * dy_step, l, ((it + u) << log_h) < left, rd[u]);
-          }
-      }
+    for (int h = 0;;) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (it + u >= sd.iters) break;
+        if (h + (u << log_h) >= n) break;
+        __builtin_amdgcn_sched_barrier(0);   // one head at a time, or registers run out
+        const bool head = h + (u << log_h) < left, on[2] = {head && l.on[0], head && l.on[1]};
         float v[2 * V], w[2 * V];
-        widen<T, V>(rx[u], v);
-        widen<T, V>(rd[u], w);
+        widen<T, V>(rx[u], on, v);
+        widen<T, V>(rd[u], on, w);
         turn<V, ADJ>(l, c, s, w);
         float ss = 0.f, sw = 0.f;
 #pragma unroll
@@ -334,7 +343,16 @@ __global__ __launch_bounds__(256) void qk_bwd_kernel(QkArgs a) {
           dg[i] = fmaf(w[i], v[i] * k, dg[i]);
           w[i] = k * fmaf(w[i], g[i], -v[i] * m);
         }
-        store_head<T, V, ADJ>(y + (it + u) * y_step, l, ((it + u) << log_h) < left, w);
+        store_head<T, V>(const_cast<T*>(y.at(row0, head0 + h + (u << log_h))), y.off, l.on, head, w);
+      }
+      h += U << log_h;
+      if (h >= n) break;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        load_head<T, V>(x.at(row0, head0 + h + (u << log_h)), x.off, l.on,
+                        h + (u << log_h) < left, rx[u]);
+        load_head<T, V>(dy.at(row0, head0 + h + (u << log_h)), dy.off, l.on,
+                        h + (u << log_h) < left, rd[u]);
       }
     }
   }
@@ -392,7 +410,7 @@ int lanes_log2(int v, int half, int d) {   // lanes of a head
 }
 
 constexpr int kWaves = 4096;    // enough waves for 256 compute units
-constexpr int kMaxBlocks = 1 << 20;
+constexpr int kFwdBlocks = 4096;
 
 // Heads a wave holds at once: as few idle slots over a row's heads as can be, then as many
 // heads as can be (a row's angles are worked out once per wave).  Few rows are spread over
@@ -418,7 +436,7 @@ void divide(SideArgs& s, int64_t rows, int log_c, int max_blocks) {
   s.blocks = std::min((s.items + 3) / 4, max_blocks);
 }
 
-constexpr int kBwdBlocks = 1024;
+constexpr int kBwdBlocks = 512;
 
 QkArgs device_args(const QkProblem& p, int v) {
   QkArgs a;
@@ -446,7 +464,7 @@ hipError_t qk_rope_fwd(const QkProblem& p, hipStream_t s) {
   if (p.rows == 0) return hipSuccess;
   const int v = vector_of(p.dtype, p.rot_dim / 2, p.head_dim);
   QkArgs a = device_args(p, v);
-  for (SideArgs& sd : a.side) divide(sd, p.rows, a.log_c, kMaxBlocks);
+  for (SideArgs& sd : a.side) divide(sd, p.rows, a.log_c, kFwdBlocks);
   const dim3 grid(a.side[0].blocks + a.side[1].blocks);
   if (grid.x == 0) return hipSuccess;
 #define MPIPE_QK(T, V)                                                                            \
