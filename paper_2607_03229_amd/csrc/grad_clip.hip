@@ -21,14 +21,18 @@ struct NormArgs {
   int32_t first[kNormTensors];   // first chunk, from chunk0
 };
 
-// the tensor of chunk c: the last one whose first chunk is not behind it
-__device__ __forceinline__ int tensor_of(const int32_t* first, int n, int c) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= c) lo = mid; else hi = mid;
+// The tensor of chunk c: how many first chunks are not behind it, less one.  All of them are
+// compared at once, 64 a step.
+template <int N>
+__device__ __forceinline__ int tensor_of(const int32_t (&first)[N], int n, int c) {
+  const int lane = threadIdx.x & 63;
+  int t = -1;
+#pragma unroll
+  for (int k = 0; k < N; k += 64) {
+    const bool before = k + lane < n && first[min(k + lane, N - 1)] <= c;
+    t += __popcll(__ballot(before));
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(t);
 }
 
 __device__ __forceinline__ double block_sum(double v, double* lds) {
@@ -41,14 +45,70 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return s;
 }
 
-template <class T>
-__device__ double chunk_sum(const T* p, int64_t n) {
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
-    const double v = (double)(float)p[i];
-    s = fma(v, v, s);
+// E elements in words, aligned to one element: wide accesses take any alignment.
+template <class T, int E> struct Group {
+  static constexpr int kWords = E * sizeof(T) / 4;
+  typedef uint32_t W __attribute__((ext_vector_type(kWords)));
+  typedef W At __attribute__((aligned(sizeof(T))));
+  W w;
+  __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const At*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<At*>(p) = w; }
+  __device__ __forceinline__ float get(int i) const {
+    if (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
   }
-  return s;
+};
+template <class T, int E>
+__device__ __forceinline__ Group<T, E> pack(const float (&v)[E]) {
+  Group<T, E> g;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) g.w[i] = __float_as_uint(v[i]);
+  } else {
+    typedef __bf16 Two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < E; i += 2) {
+      const Two t = {(bf16)v[i], (bf16)v[i + 1]};
+      g.w[i / 2] = __builtin_bit_cast(uint32_t, t);
+    }
+  }
+  return g;
+}
+
+constexpr int kAhead = 8;   // 16-byte loads of a thread in flight
+
+template <class T>
+__device__ __forceinline__ double chunk_sum(const T* p, int n) {
+  constexpr int E = 16 / sizeof(T);
+  double s[2] = {0.0, 0.0};
+  const int groups = n / E;
+  int i = threadIdx.x;
+  for (; i + (kAhead - 1) * 256 < groups; i += kAhead * 256) {
+    Group<T, E> g[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) g[u].load(p + (int64_t)(i + u * 256) * E);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const double v = (double)g[u].get(e);
+        s[e % 2] = fma(v, v, s[e % 2]);
+      }
+  }
+  for (; i < groups; i += 256) {
+    Group<T, E> g;
+    g.load(p + (int64_t)i * E);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const double v = (double)g.get(e);
+      s[e % 2] = fma(v, v, s[e % 2]);
+    }
+  }
+  if (groups * E + (int)threadIdx.x < n) {
+    const double v = (double)(float)p[groups * E + threadIdx.x];
+    s[0] = fma(v, v, s[0]);
+  }
+  return s[0] + s[1];
 }
 
 // partial[chunk0 + block] = sum of squares of one chunk; starts[tensor] = its first chunk
@@ -57,7 +117,8 @@ __global__ __launch_bounds__(256) void sumsq_kernel(NormArgs a, int n, int tenso
                                                     int32_t* starts) {
   __shared__ double lds[4];
   const int c = blockIdx.x, t = tensor_of(a.first, n, c), nth = c - a.first[t];
-  const int64_t len = a.n[t] >> 1, at = nth * chunk, m = len - at < chunk ? len - at : chunk;
+  const int64_t len = a.n[t] >> 1, at = nth * chunk;
+  const int m = (int)(len - at < chunk ? len - at : chunk);
   const double s = block_sum((a.n[t] & 1) ? chunk_sum((const bf16*)a.p[t] + at, m)
                                           : chunk_sum((const float*)a.p[t] + at, m), lds);
   if (threadIdx.x == 0) {
@@ -89,6 +150,31 @@ __global__ __launch_bounds__(256) void total_kernel(const double* sums, int n, d
   if (threadIdx.x == 0) *sumsq = s;
 }
 
+// both steps in one block, where there are few tensors and chunks: a wave a tensor
+constexpr int kFewTensors = 64, kFewChunks = 4096;
+__global__ __launch_bounds__(1024) void few_sums_kernel(const double* partial,
+                                                        const int32_t* starts, int n, int chunks,
+                                                        float* norms, double* sumsq) {
+  __shared__ double lds[kFewTensors];
+  const int lane = threadIdx.x & 63;
+  for (int t = threadIdx.x >> 6; t < n; t += 16) {
+    const int end = t + 1 < n ? starts[t + 1] : chunks;
+    double s = 0.0;
+    for (int c = starts[t] + lane; c < end; c += 64) s += partial[c];
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) {
+      lds[t] = s;
+      if (norms) norms[t] = (float)sqrt(s);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    double s = lane < n ? lds[lane] : 0.0;
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) *sumsq = s;
+  }
+}
+
 struct ClipArgs {
   const void* p[kClipTensors];
   void* o[kClipTensors];
@@ -97,8 +183,32 @@ struct ClipArgs {
 };
 
 template <class A, class B>
-__device__ void chunk_scale(const A* p, B* o, int64_t n, float f) {
-  for (int64_t i = threadIdx.x; i < n; i += 256) o[i] = (B)((float)p[i] * f);
+__device__ __forceinline__ void chunk_scale(const A* p, B* o, int n, float f) {
+  constexpr int E = sizeof(A) + sizeof(B) == 4 ? 8 : 4, U = 4;
+  const int groups = n / E;
+  int i = threadIdx.x;
+  for (; i + (U - 1) * 256 < groups; i += U * 256) {
+    Group<A, E> g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) g[u].load(p + (int64_t)(i + u * 256) * E);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = g[u].get(e) * f;
+      pack<B, E>(v).store(o + (int64_t)(i + u * 256) * E);
+    }
+  }
+  for (; i < groups; i += 256) {
+    Group<A, E> g;
+    g.load(p + (int64_t)i * E);
+    float v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = g.get(e) * f;
+    pack<B, E>(v).store(o + (int64_t)i * E);
+  }
+  i = groups * E + threadIdx.x;
+  if (i < n) o[i] = (B)((float)p[i] * f);
 }
 
 __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t chunk,
@@ -107,12 +217,12 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t ch
   const double len2 = sqrt(*sumsq);
   const bool scales = len2 > max_norm && len2 <= 1.7976931348623157e308;
   const float f = scales ? (float)(max_norm / len2) : 1.f;
-  const int c = blockIdx.x;
+  const int c = gridDim.x - 1 - blockIdx.x;   // what the norm read last is cached still
   if (norm && c == 0 && threadIdx.x == 0) *norm = (float)len2;
   if (n == 0) return;
   const int t = tensor_of(a.first, n, c);
   const int64_t len = a.n[t] >> 2, at = (c - a.first[t]) * chunk;
-  const int64_t m = len - at < chunk ? len - at : chunk;
+  const int m = (int)(len - at < chunk ? len - at : chunk);
   if (a.p[t] == a.o[t] && !scales) return;
   const bool in16 = a.n[t] & 1, out16 = a.n[t] & 2;
   if (in16 && out16) chunk_scale((const bf16*)a.p[t] + at, (bf16*)a.o[t] + at, m, f);
@@ -151,6 +261,11 @@ hipError_t grad_norm(const mpipe_grad_tensor* t, int n, const GradPlan& p, doubl
     if (e != hipSuccess) return e;
     chunk0 += c;
   }
+  if (n <= kFewTensors && p.chunks <= kFewChunks) {
+    hipLaunchKernelGGL(few_sums_kernel, dim3(1), dim3(1024), 0, s, partial, starts, n,
+                       (int)p.chunks, norms, sumsq);
+    return hipGetLastError();
+  }
   if (n > 0) {
     hipLaunchKernelGGL(tensor_sum_kernel, dim3(n), dim3(256), 0, s, partial, starts, n,
                        (int)p.chunks, sums, norms);
@@ -164,23 +279,27 @@ hipError_t grad_norm(const mpipe_grad_tensor* t, int n, const GradPlan& p, doubl
 hipError_t grad_clip(const mpipe_grad_tensor* in, const mpipe_grad_tensor* out, int n,
                      const GradPlan& p, const double* sumsq, double max_norm, float* norm,
                      hipStream_t s) {
-  int i = 0;
+  // from the last tensors to the first, as within a launch
+  int end = n;
   do {
     ClipArgs a;
-    int k = 0, c = 0;
-    for (; i < n && k < kClipTensors; ++i, ++k) {
+    const int begin = std::max(0, end - kClipTensors);
+    int c = 0;
+    for (int i = begin; i < end; ++i) {
+      const int k = i - begin;
       a.p[k] = in[i].data;
       a.o[k] = out[i].data;
       a.n[k] = in[i].n * 4 + (in[i].dtype == DT_BF16) + 2 * (out[i].dtype == DT_BF16);
       a.first[k] = c;
       c += chunks_of(in[i].n, p.chunk);
     }
-    hipLaunchKernelGGL(clip_kernel, dim3(std::max(c, 1)), dim3(256), 0, s, a, k, p.chunk, sumsq,
-                       max_norm, norm);
+    hipLaunchKernelGGL(clip_kernel, dim3(std::max(c, 1)), dim3(256), 0, s, a, end - begin, p.chunk,
+                       sumsq, max_norm, norm);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     norm = nullptr;
-  } while (i < n);
+    end = begin;
+  } while (end > 0);
   return hipSuccess;
 }
 
