@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -61,11 +62,6 @@ class RopeCfg(C.Structure):
 ROPE_BLOCKS, ROPE_INTERLEAVED = 0, 1
 ROPE_ONE_SPECTRUM, ROPE_AXIS_SPECTRA = 0, 1
 ROPE_HALVES, ROPE_ADJACENT = 0, 1
-
-
-class _Heads(C.Structure):
-    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
-                ("heads", C.c_int32)]
 
 
 class _GradTensor(C.Structure):
@@ -580,36 +576,34 @@ def _need(ok: bool, msg: str) -> None:
         raise MpipeError(-1, msg)
 
 
-class _Launch:
-    """The device and stream of a call: every tensor on one GPU, made current for the call
-    (a tensor's own GPU need not be); the stream is that GPU's current one unless given."""
-
-    def __init__(self, tensors, stream):
-        import torch
-        self.device = dev = tensors[0].device
-        _need(dev.type == "cuda", "tensors must be on the GPU")
-        for t in tensors:
-            _need(t.device == dev, "tensors on different devices")
-        if stream is None:
-            stream = torch.cuda.current_stream(dev)
-        _need(stream.device == dev, "a stream of another device than the tensors'")
-        self.stream = stream.cuda_stream
-        here = torch.cuda.current_device()
-        self.back = None if here == dev.index else here
-
-    def __enter__(self):
-        if self.back is not None:
-            import torch
-            torch.cuda.set_device(self.device)
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.back is not None:
-            import torch
-            torch.cuda.set_device(self.back)
+def _launch(fn, tensors, stream, *args) -> None:
+    """fn(*args, stream) with every tensor on one GPU, which is current for the call (it need
+    not be before); the stream is that GPU's current one unless given."""
+    import torch
+    dev = tensors[0].device
+    if dev.type != "cuda":
+        raise MpipeError(-1, "tensors must be on the GPU")
+    for t in tensors:
+        if t.device != dev:
+            raise MpipeError(-1, "tensors on different devices")
+    if stream is None:
+        stream = torch.cuda.current_stream(dev.index)
+    elif stream.device != dev:
+        raise MpipeError(-1, "a stream of another device than the tensors'")
+    here = torch.cuda.current_device()
+    if here == dev.index:
+        _check(fn(*args, stream.cuda_stream))
+        return
+    torch.cuda.set_device(dev)
+    try:
+        _check(fn(*args, stream.cuda_stream))
+    finally:
+        torch.cuda.set_device(here)
 
 
 def _host_i64(a, name: str) -> np.ndarray:
+    if type(a) is np.ndarray and a.dtype == np.int64 and a.ndim == 1 and a.flags.c_contiguous:
+        return a
     arr = np.asarray(a)
     _need(arr.ndim == 1 and (arr.size == 0 or arr.dtype.kind in "iu"),
           f"{name}: a list of whole numbers")
@@ -617,7 +611,7 @@ def _host_i64(a, name: str) -> np.ndarray:
 
 
 def _p(arr: Optional[np.ndarray]):
-    return None if arr is None else arr.ctypes.data
+    return None if arr is None else arr.__array_interface__["data"][0]
 
 
 def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, time_step=None,
@@ -643,42 +637,46 @@ def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, t
     _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == 3 and
           (pos.shape[1] <= 1 or pos.stride(1) == 1), "pos: int32 [3][rows], rows adjacent")
     nxt = np.zeros(sr.size, np.int64)
-    with _Launch((pos,), stream) as s:
-        _check(load().mpipe_op_seam_positions(
-            _p(sr), _p(sl), _p(sp), sr.size, _p(ir), _p(g), _p(ts), ir.size, pos.shape[1],
-            _ptr(pos), pos.stride(0), _p(nxt), s))
+    _launch(load().mpipe_op_seam_positions, (pos,), stream, _p(sr), _p(sl), _p(sp), sr.size,
+            _p(ir), _p(g), _p(ts), ir.size, pos.shape[1], pos.data_ptr(), pos.stride(0), _p(nxt))
     return nxt
+
+
+_HEADS = struct.Struct("PqqiI")    # mpipe_heads
 
 
 def _heads(t, like=None):
     """mpipe_heads of [rows][heads][head_dim]; None: no heads."""
     if t is None:
         return None
-    if like is not None:
-        _need(t.shape == like.shape and t.dtype == like.dtype,
-              "inputs, gradients and outputs differ in shape or dtype")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise MpipeError(-1, "inputs, gradients and outputs differ in shape or dtype")
     rs, hs, cs = t.stride()
-    _need(cs == 1, "the columns of a head must be adjacent")
-    return C.byref(_Heads(t.data_ptr(), rs, hs, t.shape[1]))
+    if cs != 1:
+        raise MpipeError(-1, "the columns of a head must be adjacent")
+    return _HEADS.pack(t.data_ptr(), rs, hs, t.shape[1], 0)
 
 
-def _qk_common(cfg, q, k, pos, others):
+def _qk_common(cfg, q, k, pos, outs):
     """(dtype, rows) of q and k [rows][heads][head_dim] (either may be None) and the tensors
     of the call."""
     import torch
     one = q if q is not None else k
     _need(one is not None, "neither q nor k")
-    for t in (q, k):
-        _need(t is None or (t.dim() == 3 and t.shape[2] == cfg.head_dim and
-                            t.shape[0] == one.shape[0] and t.dtype == one.dtype),
-              "q and k: [rows][heads][head_dim] of one dtype")
-    for x, ys in ((q, others[0]), (k, others[1])):
-        _need(all((y is None) == (x is None) for y in ys), "one of q and k without its output")
+    rows, dtype, ts = one.shape[0], one.dtype, [pos]
+    for x, ys in ((q, outs[0]), (k, outs[1])):
+        if x is None:
+            _need(all(y is None for y in ys), "one of q and k without its input")
+            continue
+        _need(x.dim() == 3 and x.shape[2] == cfg.head_dim and x.shape[0] == rows and
+              x.dtype == dtype, "q and k: [rows][heads][head_dim] of one dtype")
+        _need(all(y is not None for y in ys), "one of q and k without its output")
+        ts.append(x)
+        ts.extend(ys)
     _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == cfg.axes and
-          pos.shape[1] == one.shape[0] and (pos.shape[1] <= 1 or pos.stride(1) == 1),
+          pos.shape[1] == rows and (rows <= 1 or pos.stride(1) == 1),
           "pos: int32 [axes][rows], rows adjacent")
-    return _dt(one), one.shape[0], [t for t in (q, k, pos, *others[0], *others[1])
-                                    if t is not None]
+    return _dt(one), rows, ts
 
 
 def _gains(cfg, x, gain, name):
@@ -694,10 +692,9 @@ def op_rope_axes(cfg, q, k, pos, q_out, k_out, inverse: bool = False, stream=Non
     k_out may be None) turned by pos (int32 [axes][rows]); inverse turns back (the gradient).
     An output may be its own input."""
     dt, rows, ts = _qk_common(cfg, q, k, pos, ((q_out,), (k_out,)))
-    with _Launch(ts, stream) as s:
-        _check(load().mpipe_op_rope_axes(dt, C.byref(cfg), rows, _heads(q), _heads(k), _ptr(pos),
-                                         pos.stride(0), int(bool(inverse)), _heads(q_out, q),
-                                         _heads(k_out, k), s))
+    _launch(load().mpipe_op_rope_axes, ts, stream, dt, C.byref(cfg), rows, _heads(q), _heads(k),
+            pos.data_ptr(), pos.stride(0), int(bool(inverse)), _heads(q_out, q),
+            _heads(k_out, k))
 
 
 def op_qk_norm_rope_fwd(cfg, q, k, q_gain, k_gain, eps: float, pos, q_out, k_out,
@@ -707,11 +704,9 @@ def op_qk_norm_rope_fwd(cfg, q, k, q_gain, k_gain, eps: float, pos, q_out, k_out
     _gains(cfg, q, q_gain, "q_gain")
     _gains(cfg, k, k_gain, "k_gain")
     ts += [g for g in (q_gain, k_gain) if g is not None]
-    with _Launch(ts, stream) as s:
-        _check(load().mpipe_op_qk_norm_rope_fwd(dt, C.byref(cfg), rows, _heads(q), _heads(k),
-                                                _ptr(q_gain), _ptr(k_gain), eps, _ptr(pos),
-                                                pos.stride(0), _heads(q_out, q),
-                                                _heads(k_out, k), s))
+    _launch(load().mpipe_op_qk_norm_rope_fwd, ts, stream, dt, C.byref(cfg), rows, _heads(q),
+            _heads(k), _ptr(q_gain), _ptr(k_gain), eps, pos.data_ptr(), pos.stride(0),
+            _heads(q_out, q), _heads(k_out, k))
 
 
 def op_qk_norm_rope_scratch_bytes(rows: int, heads_q: int, heads_k: int, head_dim: int) -> int:
@@ -737,12 +732,11 @@ def op_qk_norm_rope_bwd(cfg, dq, dk, q, k, q_gain, k_gain, eps: float, pos, dq_i
               "gain gradients: fp32 [head_dim]")
     _need(scratch is None or scratch.is_contiguous(), "scratch must be contiguous")
     ts += [t for t in (q_gain, k_gain, grad_q_gain, grad_k_gain, scratch) if t is not None]
-    with _Launch(ts, stream) as s:
-        _check(load().mpipe_op_qk_norm_rope_bwd(
-            dt, C.byref(cfg), rows, _heads(dq, q), _heads(dk, k), _heads(q), _heads(k),
-            _ptr(q_gain), _ptr(k_gain), eps, _ptr(pos), pos.stride(0), _heads(dq_in, q),
-            _heads(dk_in, k), _ptr(grad_q_gain), _ptr(grad_k_gain), int(bool(accumulate)),
-            _ptr(scratch), 0 if scratch is None else scratch.numel() * scratch.element_size(), s))
+    _launch(load().mpipe_op_qk_norm_rope_bwd, ts, stream, dt, C.byref(cfg), rows, _heads(dq, q),
+            _heads(dk, k), _heads(q), _heads(k), _ptr(q_gain), _ptr(k_gain), eps, pos.data_ptr(),
+            pos.stride(0), _heads(dq_in, q), _heads(dk_in, k), _ptr(grad_q_gain),
+            _ptr(grad_k_gain), int(bool(accumulate)), _ptr(scratch),
+            0 if scratch is None else scratch.numel() * scratch.element_size())
 
 
 class GradList:
@@ -783,9 +777,8 @@ def op_grad_norm(grads, sumsq, norms, scratch, stream=None) -> None:
                             norms.is_contiguous()), "norms: fp32 [tensors]")
     _need(scratch.is_contiguous(), "scratch must be contiguous")
     ts = [sumsq, scratch] + g.tensors[:1] + ([] if norms is None else [norms])
-    with _Launch(ts, stream) as s:
-        _check(load().mpipe_op_grad_norm(g.array, g.n, _ptr(sumsq), _ptr(norms), _ptr(scratch),
-                                         scratch.numel() * scratch.element_size(), s))
+    _launch(load().mpipe_op_grad_norm, ts, stream, g.array, g.n, _ptr(sumsq), _ptr(norms),
+            _ptr(scratch), scratch.numel() * scratch.element_size())
 
 
 def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None) -> None:
@@ -800,6 +793,5 @@ def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None
     _need(o is None or o.n == g.n, "grads and out differ in number")
     ts = [sumsq] + g.tensors[:1] + ([] if norm is None else [norm]) + \
         ([] if o is None else o.tensors[:1])
-    with _Launch(ts, stream) as s:
-        _check(load().mpipe_op_grad_clip(g.array, None if o is None else o.array, g.n,
-                                         _ptr(sumsq), float(max_norm), _ptr(norm), s))
+    _launch(load().mpipe_op_grad_clip, ts, stream, g.array, None if o is None else o.array, g.n,
+            _ptr(sumsq), float(max_norm), _ptr(norm))

@@ -80,11 +80,11 @@ def test_positions_of_nothing(L):
 # ---- rotary configurations and head views -----------------------------------------------------
 
 def _heads(p=FAKE, row=1024, head=128, heads=8):
-    return B._Heads(p, row, head, heads)
+    return B._HEADS.pack(p or 0, row, head, heads, 0)
 
 
 def _rope(L, cfg=None, dtype=1, rows=4, q=None, k=None, qo=None, ko=None, pos=FAKE * 2, ld=4):
-    ref = lambda h: None if h is None else C.byref(h)
+    ref = lambda h: h
     cfg = mp.RopeCfg(128, [16, 24, 24]) if cfg is None else cfg
     q = _heads() if q is None else q
     qo = _heads(FAKE * 16) if qo is None else qo
@@ -165,7 +165,7 @@ def test_nothing_to_turn(L):
 
 def _norm(L, eps=1e-6, gains=(FAKE * 3, FAKE * 3), bwd=False, scratch=FAKE * 64, nbytes=1 << 30,
           grads=(FAKE * 5, FAKE * 5 + 1024), rows=4, dq_out=FAKE * 16):
-    ref = lambda h: None if h is None else C.byref(h)
+    ref = lambda h: h
     cfg = mp.RopeCfg(128, [16, 24, 24])
     q, k, qo, ko = _heads(), _heads(FAKE * 8), _heads(dq_out), _heads(FAKE * 24)
     common = (gains[0], gains[1], eps, FAKE * 2, 4, ref(qo), ref(ko))
