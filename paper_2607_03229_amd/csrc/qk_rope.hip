@@ -20,9 +20,9 @@ struct SideArgs {
   const void* gain;
   float* part;   // backward: [blocks][head_dim]
   int heads, blocks;
-  // heads a wave holds at once (log2), its walks over a row's heads, waves per row group,
-  // row groups times those
-  int log_h, iters, head_groups, items;
+  // heads a wave holds at once (log2), its steps over a row's heads, waves that share a row,
+  // groups of as many rows as a wave holds
+  int log_h, iters, head_groups, groups;
 };
 
 struct QkArgs {
@@ -31,7 +31,7 @@ struct QkArgs {
   int64_t ld_pos, rows;
   float eps, inv_d;
   int d, half, inverse;
-  int log_c;   // lanes of a head (log2)
+  int lanes, log_c;   // lanes of a head that hold columns; the power of two above (log2)
   RopeTable table;
 };
 
@@ -57,6 +57,10 @@ __device__ __forceinline__ void turn_cos_sin(uint64_t f, int32_t p, float& c, fl
   s = (q >= 2) ? -b : b;
 }
 
+// Pointers that came through a table of views: known to be global memory, so that loads are
+// counted apart from LDS accesses.
+#define MPIPE_GLOBAL __attribute__((address_space(1)))
+
 // V elements as words, aligned to one element: global accesses of 16 bytes take any alignment.
 template <class T, int V> struct Vec;
 template <> struct Vec<float, 4> {
@@ -74,11 +78,11 @@ template <> struct Vec<bf16, 4> {
 template <class T, int V> using Words = typename Vec<T, V>::W;
 
 // What a lane does in every head it takes: V pairs (2 V columns) or, behind the rotated
-// columns, 2 V columns that pass through.  col[0] and col[1] each start V adjacent columns;
-// with halves they are rot / 2 apart.
+// columns, 2 V columns that pass through (V where `two` is off: the second V repeat them).
+// col[0] and col[1] each start V adjacent columns; with halves they are rot / 2 apart.
 template <int V, bool ADJ> struct Lane {
   int col[2];
-  bool on[2], turns;
+  bool two, turns;
   __device__ __forceinline__ Lane(int c, int half, int d) {
     turns = c * V < half;
     if (turns && !ADJ) {
@@ -88,38 +92,29 @@ template <int V, bool ADJ> struct Lane {
       col[0] = 2 * c * V;
       col[1] = 2 * c * V + V;
     }
-    on[0] = col[0] < d;
-    on[1] = col[1] < d;
+    two = col[1] < d;
+    if (!two) col[1] = col[0];
   }
   static __device__ __forceinline__ constexpr int first(int i) { return ADJ ? 2 * i : i; }
   static __device__ __forceinline__ constexpr int second(int i) { return ADJ ? 2 * i + 1 : V + i; }
 };
 
-// Lanes that are off keep whatever their registers held: what they compute is not stored, and
-// columns past the head are set to zero before a sum.  (Zeroing the registers first would
-// make every load wait for the one before.)
 template <class T, int V>
-__device__ __forceinline__ void load_head(const T* p, const int64_t (&off)[2], const bool (&on)[2],
-                                          bool head, Words<T, V> (&r)[2]) {
+__device__ __forceinline__ void load_head(const T* const (&p)[2], Words<T, V> (&r)[2]) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    r[k] = __builtin_nondeterministic_value(r[k]);
-    if (head && on[k]) r[k] = *reinterpret_cast<const typename Vec<T, V>::At*>(p + off[k]);
-  }
+  for (int k = 0; k < 2; ++k) r[k] = *(const MPIPE_GLOBAL typename Vec<T, V>::At*)p[k];
 }
 template <class T, int V>
-__device__ __forceinline__ void widen(const Words<T, V> (&r)[2], const bool (&on)[2],
-                                      float (&v)[2 * V]) {
+__device__ __forceinline__ void widen(const Words<T, V> (&r)[2], float (&v)[2 * V]) {
   constexpr int E = 4 / sizeof(T);   // elements of a word
 #pragma unroll
   for (int i = 0; i < 2 * V; ++i) {
     const uint32_t w = r[i / V][i % V / E];
-    v[i] = on[i / V] ? __uint_as_float(E == 1 ? w : i % 2 ? w & 0xFFFF0000u : w << 16) : 0.f;
+    v[i] = __uint_as_float(E == 1 ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
   }
 }
 template <class T, int V>
-__device__ __forceinline__ void store_head(T* p, const int64_t (&off)[2], const bool (&on)[2],
-                                           bool head, const float (&v)[2 * V]) {
+__device__ __forceinline__ void store_head(const T* const (&p)[2], const float (&v)[2 * V]) {
   constexpr int E = 4 / sizeof(T);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -134,7 +129,7 @@ __device__ __forceinline__ void store_head(T* p, const int64_t (&off)[2], const 
         r[i] = __builtin_bit_cast(uint32_t, t);
       }
     }
-    if (head && on[k]) *reinterpret_cast<typename Vec<T, V>::At*>(p + off[k]) = r;
+    *(MPIPE_GLOBAL typename Vec<T, V>::At*)const_cast<T*>(p[k]) = r;
   }
 }
 
@@ -143,30 +138,20 @@ template <int CTRL> __device__ __forceinline__ float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float head_sum(float v, int log_c) {
-  if (log_c > 0) v = dpp_add<0xB1>(v);    // lane ^ 1
-  if (log_c > 1) v = dpp_add<0x4E>(v);    // lane ^ 2
-  if (log_c > 2) v = dpp_add<0x141>(v);   // mirrored within 8
-  if (log_c > 3) v = dpp_add<0x140>(v);   // mirrored within 16
+  float w = dpp_add<0xB1>(v);     // lane ^ 1
+  v = log_c > 0 ? w : v;
+  w = dpp_add<0x4E>(v);           // lane ^ 2
+  v = log_c > 1 ? w : v;
+  w = dpp_add<0x141>(v);          // mirrored within 8
+  v = log_c > 2 ? w : v;
+  w = dpp_add<0x140>(v);          // mirrored within 16
+  v = log_c > 3 ? w : v;
   if (log_c > 4) v += __shfl_xor(v, 16);
   return v;
 }
 __device__ __forceinline__ float inv_rms(float ss, float inv_d, float eps) {
   const float m = fmaf(ss, inv_d, eps), r = __builtin_amdgcn_rsqf(m);
   return fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r);   // one Newton step: the root to half a step
-}
-
-// cos and sin of a wave's rows: each row's lanes share its rot / 2 pairs and meet in LDS
-__device__ __forceinline__ void wave_trig(const QkArgs& a, float* cs, float* sn, int64_t row,
-                                          int rs, int sub, int width) {
-  if (row < a.rows)
-    for (int j = sub; j < a.half; j += width) {
-      float c, s;
-      turn_cos_sin(a.table.turn[j], a.pos[a.table.axis[j] * a.ld_pos + row], c, s);
-      cs[rs * a.half + j] = c;
-      sn[rs * a.half + j] = a.inverse ? -s : s;
-    }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 template <int V, bool ADJ>
@@ -183,187 +168,297 @@ __device__ __forceinline__ void turn(const Lane<V, ADJ>& l, const float (&c)[V],
 }
 
 // A wave is (rows) x (heads) x (lanes of a head), powers of two: 64 >> (log_c + log_h) rows,
-// 1 << log_h heads, walked `iters` times over a row's heads.
+// 1 << log_h heads.  It walks its share of a row's heads, then the next rows of its stride,
+// `kRing` steps of loads ahead of the arithmetic.
+//
+// Every lane of a step loads and stores, so that the loads in flight can be counted and only
+// the oldest waited for: lanes past the last row, head or column repeat the last one, with the
+// same values to the same place, and are left out of the sums.
 struct Place {
   int c, hs, rs, sub;
-  __device__ __forceinline__ Place(int lane, int log_c, int log_h) {
-    c = lane & ((1 << log_c) - 1);
+  bool extra;   // a column lane past the head's last
+  __device__ __forceinline__ Place(int lane, int log_c, int log_h, int lanes) {
+    const int l = lane & ((1 << log_c) - 1);
+    c = min(l, lanes - 1);
+    extra = l >= lanes;
     hs = (lane >> log_c) & ((1 << log_h) - 1);
     rs = lane >> (log_c + log_h);
     sub = lane & ((1 << (log_c + log_h)) - 1);
   }
 };
-constexpr int kTrig = 512;   // pairs of a wave's rows: at most 64 lanes * 8
 
-// A view as a wave walks it: the lane's offsets from the wave's first row and head, and the
-// (scalar) way to those.
-template <class T> struct Walk {
-  const T* base;
-  int64_t row, head, off[2];
-  __device__ __forceinline__ Walk(const void* p, int64_t row_stride, int64_t head_stride,
-                                  const Place& at, const int (&col)[2])
-      : base(reinterpret_cast<const T*>(p)), row(row_stride), head(head_stride) {
-    for (int k = 0; k < 2; ++k) off[k] = at.rs * row + at.hs * head + col[k];
+// Where a wave is in its rows and heads.
+struct Cursor {
+  int rg, h;
+  __device__ __forceinline__ void next(int h_step, int n, int rg_step) {
+    h += h_step;
+    if (h >= n) {
+      h = 0;
+      rg += rg_step;
+    }
   }
-  __device__ __forceinline__ const T* at(int64_t r, int h) const { return base + r * row + h * head; }
 };
 
-template <class T, int V, bool ADJ, bool NORM>
-__global__ __launch_bounds__(256, 4) void qk_fwd_kernel(QkArgs a) {
-  constexpr int U = 2;   // heads loaded ahead
-  __shared__ float trig[4][2][kTrig];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int z = (int)blockIdx.x >= a.side[0].blocks;
-  const SideArgs& sd = a.side[z];
-  const int log_c = a.log_c, log_h = sd.log_h, block = blockIdx.x - (z ? a.side[0].blocks : 0);
-  const Place at(lane, log_c, log_h);
-  const Lane<V, ADJ> l(at.c, a.half, a.d);
-  const Walk<T> x(sd.x, sd.x_row, sd.x_head, at, l.col), y(sd.y, sd.y_row, sd.y_head, at, l.col);
-  float* cs = trig[wave][0];
-  float* sn = trig[wave][1];
-  float g[2 * V];
-  if (NORM) {
-    Words<T, V> r[2];
-    const int64_t off[2] = {l.col[0], l.col[1]};
-    load_head<T, V>(reinterpret_cast<const T*>(sd.gain), off, l.on, true, r);
-    widen<T, V>(r, l.on, g);
+// A view as a wave walks it: the lane's offsets from the step's first row and head.
+template <class T> struct Walk {
+  const T* base;   // first row, the wave's first head
+  int64_t row, head, off[2];
+  __device__ __forceinline__ Walk(const void* p, int64_t row_stride, int64_t head_stride,
+                                  const Place& at, int head0, const int (&col)[2])
+      : base(reinterpret_cast<const T*>(p) + head0 * head_stride), row(row_stride),
+        head(head_stride) {
+    for (int k = 0; k < 2; ++k) off[k] = at.rs * row + at.hs * head + col[k];
   }
-  for (int item = block * 4 + wave; item < sd.items; item += sd.blocks * 4) {
-    const int rg = item / sd.head_groups, hg = item - rg * sd.head_groups;
-    const int64_t row0 = (int64_t)rg << (6 - log_c - log_h);
-    const int head0 = (hg * sd.iters) << log_h, n = min(sd.iters << log_h, sd.heads - head0);
-    const int left = row0 + at.rs < a.rows ? n - at.hs : 0;   // heads from the lane's first on
-    Words<T, V> r[U][2];
+  // the lane's two vectors at `row0` and head h; `drs`, `dhs`: how far it is past the last
+  __device__ __forceinline__ void at(int64_t row0, int h, int drs, int dhs, bool edge,
+                                     const T* (&p)[2]) const {
+    const T* b = base + row0 * row + h * head;
+    p[0] = b + off[0];
+    p[1] = b + off[1];
+    if (edge) {
+      const int64_t back = drs * row + dhs * head;
+      p[0] -= back;
+      p[1] -= back;
+    }
+  }
+};
+
+constexpr int kTrig = 512;   // pairs of a wave's rows: at most 64 lanes * 8
+
+// What both kernels keep of a wave's walk.
+template <class T, int V, bool ADJ, int KP> struct Wave {
+  const QkArgs& a;
+  const int log_c, log_h, rs_log;
+  const Place at;
+  const Lane<V, ADJ> l;
+  int rg0, rg_step, groups, head0, n;
+  bool idle;
+  float *cs, *sn;
+  const uint64_t* turns;
+  const int32_t* pos[KP];
+
+  __device__ __forceinline__ Wave(const QkArgs& a, const SideArgs& sd, int w, float* trig,
+                                  const uint64_t* turn_table, const uint8_t* axis_table)
+      : a(a), log_c(a.log_c), log_h(sd.log_h), rs_log(6 - a.log_c - sd.log_h),
+        at(threadIdx.x & 63, a.log_c, sd.log_h, a.lanes), l(at.c, a.half, a.d) {
+    const int hg = w % sd.head_groups;
+    rg0 = w / sd.head_groups;
+    rg_step = sd.blocks * 4 / sd.head_groups;
+    groups = sd.groups;
+    idle = rg0 >= min(rg_step, groups);   // a grid's last waves may have no rows of their own
+    rg0 = min(rg0, groups - 1);
+    head0 = (hg * sd.iters) << log_h;
+    n = min(sd.iters << log_h, sd.heads - head0);
+    cs = trig;
+    sn = trig + kTrig;
+    turns = turn_table;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      load_head<T, V>(x.at(row0, head0 + (u << log_h)), x.off, l.on, (u << log_h) < left, r[u]);
-    wave_trig(a, cs, sn, row0 + at.rs, at.rs, at.sub, 1 << (log_c + log_h));
-    float c[V], s[V];
-    if (l.turns) {
+    for (int k = 0; k < KP; ++k) {
+      const int j = min(at.sub + (k << (log_c + log_h)), a.half - 1);
+      pos[k] = a.pos + axis_table[j] * a.ld_pos + at.rs;
+    }
+  }
+  __device__ __forceinline__ int64_t row0(int rg) const { return (int64_t)rg << rs_log; }
+  // how far the lane is past the last row / head of a step
+  __device__ __forceinline__ int past_rows(int rg) const {
+    return max(0, at.rs - (int)min((int64_t)64, a.rows - 1 - row0(rg)));
+  }
+  __device__ __forceinline__ int past_heads(int h) const { return max(0, at.hs - (n - 1 - h)); }
+  __device__ __forceinline__ bool edge(const Cursor& c) const {
+    return row0(c.rg + 1) > a.rows || c.h + (1 << log_h) > n;
+  }
+  __device__ __forceinline__ void load_pos(int rg, int32_t (&p)[KP]) const {
+    const int64_t r = row0(rg) - past_rows(rg);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        c[i] = cs[at.rs * a.half + at.c * V + i];
-        s[i] = sn[at.rs * a.half + at.c * V + i];
+    for (int k = 0; k < KP; ++k) p[k] = *(const MPIPE_GLOBAL int32_t*)(pos[k] + r);
+  }
+  // cos and sin of the step's rows: each row's lanes share its rot / 2 pairs and meet in LDS
+  __device__ __forceinline__ void angles(const int32_t (&p)[KP], float (&c)[V], float (&s)[V]) const {
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < KP; ++k) {
+      const int j = at.sub + (k << (log_c + log_h));
+      if (j < a.half) {
+        float x, y;
+        turn_cos_sin(turns[j], p[k], x, y);
+        cs[at.rs * a.half + j] = x;
+        sn[at.rs * a.half + j] = a.inverse ? -y : y;
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
-    for (int h = 0;;) {
+    const int j0 = at.rs * a.half + (l.turns ? at.c * V : 0);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (h + (u << log_h) >= n) break;
-        __builtin_amdgcn_sched_barrier(0);   // one head at a time, or registers run out
-        float v[2 * V];
-        widen<T, V>(r[u], l.on, v);
-        if (NORM) {
-          float ss = 0.f;
+    for (int i = 0; i < V; ++i) {
+      c[i] = cs[j0 + i];
+      s[i] = sn[j0 + i];
+    }
+  }
+};
+
+// the tables to LDS, where a step's branch reads them without touching the loads in flight
+__device__ __forceinline__ void copy_tables(const QkArgs& a, uint64_t* turns) {
+  for (int i = threadIdx.x; i < a.half; i += 256) turns[i] = a.table.turn[i];
+  __syncthreads();
+}
+
+template <class T, int V, bool ADJ, bool NORM, int KP>
+__global__ __launch_bounds__(256, KP == 2 ? 4 : 2) void qk_fwd_kernel(QkArgs a) {
+  constexpr int kRing = 3;
+  __shared__ float trig[4][2 * kTrig];
+  __shared__ uint64_t turns[kMaxPairs];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int z = (int)blockIdx.x >= a.side[0].blocks;
+  const SideArgs& sd = a.side[z];
+  const int block = blockIdx.x - (z ? a.side[0].blocks : 0);
+  const Wave<T, V, ADJ, KP> w(a, sd, block * 4 + wave, trig[wave], turns, a.table.axis);
+  const Walk<T> x(sd.x, sd.x_row, sd.x_head, w.at, w.head0, w.l.col),
+      y(sd.y, sd.y_row, sd.y_head, w.at, w.head0, w.l.col);
+  float g[2 * V];
+  if (NORM) {
+    const T* gain = reinterpret_cast<const T*>(sd.gain);
+    const T* const p[2] = {gain + w.l.col[0], gain + w.l.col[1]};
+    Words<T, V> r[2];
+    load_head<T, V>(p, r);
+    widen<T, V>(r, g);
+  }
+  Words<T, V> r[kRing][2];
+  int32_t pos[kRing][KP];
+  Cursor ahead = {w.rg0, 0}, now = ahead;
+  auto load = [&](Words<T, V> (&r)[2], int32_t (&p)[KP]) {
+    const T* at[2];
+    x.at(w.row0(ahead.rg), ahead.h, w.past_rows(ahead.rg), w.past_heads(ahead.h), w.edge(ahead), at);
+    load_head<T, V>(at, r);
+    w.load_pos(ahead.rg, p);
+    Cursor c = ahead;
+    c.next(1 << w.log_h, w.n, w.rg_step);
+    if (c.rg < w.groups) ahead = c;   // at the end: once more the last
+  };
 #pragma unroll
-          for (int i = 0; i < 2 * V; ++i) ss = fmaf(v[i], v[i], ss);
-          const float k = inv_rms(head_sum(ss, log_c), a.inv_d, a.eps);
+  for (int i = 0; i < kRing; ++i) load(r[i], pos[i]);
+  copy_tables(a, turns);
+  if (w.idle) return;
+  float c[V], s[V];
+  for (;;) {
 #pragma unroll
-          for (int i = 0; i < 2 * V; ++i) v[i] = v[i] * k * g[i];
+    for (int i = 0; i < kRing; ++i) {
+      if (now.h == 0) w.angles(pos[i], c, s);
+      float v[2 * V];
+      widen<T, V>(r[i], v);
+      if (NORM) {
+        float ss = 0.f, st = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          ss = fmaf(v[e], v[e], ss);
+          st = fmaf(v[V + e], v[V + e], st);
         }
-        turn<V, ADJ>(l, c, s, v);
-        store_head<T, V>(const_cast<T*>(y.at(row0, head0 + h + (u << log_h))), y.off, l.on,
-                         h + (u << log_h) < left, v);
-      }
-      h += U << log_h;
-      if (h >= n) break;
+        ss = w.at.extra ? 0.f : ss + (w.l.two ? st : 0.f);
+        const float k = inv_rms(head_sum(ss, w.log_c), a.inv_d, a.eps);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        load_head<T, V>(x.at(row0, head0 + h + (u << log_h)), x.off, l.on,
-                        h + (u << log_h) < left, r[u]);
+        for (int e = 0; e < 2 * V; ++e) v[e] = v[e] * k * g[e];
+      }
+      turn<V, ADJ>(w.l, c, s, v);
+      const T* at[2];
+      y.at(w.row0(now.rg), now.h, w.past_rows(now.rg), w.past_heads(now.h), w.edge(now), at);
+      store_head<T, V>(at, v);
+      load(r[i], pos[i]);
+      now.next(1 << w.log_h, w.n, w.rg_step);
+      if (now.rg >= w.groups) return;
     }
   }
 }
 
-template <class T, int V, bool ADJ>
-__global__ __launch_bounds__(256, 3) void qk_bwd_kernel(QkArgs a) {
-  constexpr int U = 2;
-  __shared__ float trig[4][2][kTrig];
+template <class T, int V, bool ADJ, int KP>
+__global__ __launch_bounds__(256, KP == 2 ? 3 : 2) void qk_bwd_kernel(QkArgs a) {
+  constexpr int kRing = 2;
+  __shared__ float trig[4][2 * kTrig];
+  __shared__ uint64_t turns[kMaxPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int z = (int)blockIdx.x >= a.side[0].blocks;
   const SideArgs& sd = a.side[z];
-  const int log_c = a.log_c, log_h = sd.log_h, block = blockIdx.x - (z ? a.side[0].blocks : 0);
-  const Place at(lane, log_c, log_h);
-  const Lane<V, ADJ> l(at.c, a.half, a.d);
-  const Walk<T> x(sd.x, sd.x_row, sd.x_head, at, l.col), dy(sd.dy, sd.dy_row, sd.dy_head, at, l.col),
-      y(sd.y, sd.y_row, sd.y_head, at, l.col);
-  float* cs = trig[wave][0];
-  float* sn = trig[wave][1];
-  float g[2 * V], dg[2 * V];
+  const int block = blockIdx.x - (z ? a.side[0].blocks : 0);
+  const Wave<T, V, ADJ, KP> w(a, sd, block * 4 + wave, trig[wave], turns, a.table.axis);
+  float dg[2 * V];
+#pragma unroll
+  for (int e = 0; e < 2 * V; ++e) dg[e] = 0.f;
   {
-    Words<T, V> r[2];
-    const int64_t off[2] = {l.col[0], l.col[1]};
-    load_head<T, V>(reinterpret_cast<const T*>(sd.gain), off, l.on, true, r);
-    widen<T, V>(r, l.on, g);
-  }
-#pragma unroll
-  for (int i = 0; i < 2 * V; ++i) dg[i] = 0.f;
-  for (int item = block * 4 + wave; item < sd.items; item += sd.blocks * 4) {
-    const int rg = item / sd.head_groups, hg = item - rg * sd.head_groups;
-    const int64_t row0 = (int64_t)rg << (6 - log_c - log_h);
-    const int head0 = (hg * sd.iters) << log_h, n = min(sd.iters << log_h, sd.heads - head0);
-    const int left = row0 + at.rs < a.rows ? n - at.hs : 0;
-    Words<T, V> rx[U][2], rd[U][2];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      load_head<T, V>(x.at(row0, head0 + (u << log_h)), x.off, l.on, (u << log_h) < left, rx[u]);
-      load_head<T, V>(dy.at(row0, head0 + (u << log_h)), dy.off, l.on, (u << log_h) < left, rd[u]);
+    const Walk<T> x(sd.x, sd.x_row, sd.x_head, w.at, w.head0, w.l.col),
+        dy(sd.dy, sd.dy_row, sd.dy_head, w.at, w.head0, w.l.col),
+        y(sd.y, sd.y_row, sd.y_head, w.at, w.head0, w.l.col);
+    float g[2 * V];
+    {
+      const T* gain = reinterpret_cast<const T*>(sd.gain);
+      const T* const p[2] = {gain + w.l.col[0], gain + w.l.col[1]};
+      Words<T, V> r[2];
+      load_head<T, V>(p, r);
+      widen<T, V>(r, g);
     }
-    wave_trig(a, cs, sn, row0 + at.rs, at.rs, at.sub, 1 << (log_c + log_h));
+    Words<T, V> rx[kRing][2], rd[kRing][2];
+    int32_t pos[kRing][KP];
+    Cursor ahead = {w.rg0, 0}, now = ahead;
+    auto load = [&](Words<T, V> (&rx)[2], Words<T, V> (&rd)[2], int32_t (&p)[KP]) {
+      const T* at[2];
+      const bool edge = w.edge(ahead);
+      const int64_t row0 = w.row0(ahead.rg);
+      const int drs = w.past_rows(ahead.rg), dhs = w.past_heads(ahead.h);
+      x.at(row0, ahead.h, drs, dhs, edge, at);
+      load_head<T, V>(at, rx);
+      dy.at(row0, ahead.h, drs, dhs, edge, at);
+      load_head<T, V>(at, rd);
+      w.load_pos(ahead.rg, p);
+      Cursor c = ahead;
+      c.next(1 << w.log_h, w.n, w.rg_step);
+      if (c.rg < w.groups) ahead = c;
+    };
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) load(rx[i], rd[i], pos[i]);
+    copy_tables(a, turns);
     float c[V], s[V];
-    if (l.turns) {
+    for (bool more = !w.idle; more;) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        c[i] = cs[at.rs * a.half + at.c * V + i];
-        s[i] = sn[at.rs * a.half + at.c * V + i];
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    for (int h = 0;;) {
+      for (int i = 0; i < kRing; ++i) {
+        if (!more) break;
+        if (now.h == 0) w.angles(pos[i], c, s);
+        float v[2 * V], u[2 * V];
+        widen<T, V>(rx[i], v);
+        widen<T, V>(rd[i], u);
+        turn<V, ADJ>(w.l, c, s, u);
+        float ss = 0.f, st = 0.f, gs = 0.f, gt = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (h + (u << log_h) >= n) break;
-        __builtin_amdgcn_sched_barrier(0);   // one head at a time, or registers run out
-        const bool head = h + (u << log_h) < left, on[2] = {head && l.on[0], head && l.on[1]};
-        float v[2 * V], w[2 * V];
-        widen<T, V>(rx[u], on, v);
-        widen<T, V>(rd[u], on, w);
-        turn<V, ADJ>(l, c, s, w);
-        float ss = 0.f, sw = 0.f;
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) {
-          ss = fmaf(v[i], v[i], ss);
-          sw = fmaf(w[i] * g[i], v[i], sw);
+        for (int e = 0; e < V; ++e) {
+          ss = fmaf(v[e], v[e], ss);
+          st = fmaf(v[V + e], v[V + e], st);
+          gs = fmaf(u[e] * g[e], v[e], gs);
+          gt = fmaf(u[V + e] * g[V + e], v[V + e], gt);
         }
-        const float k = inv_rms(head_sum(ss, log_c), a.inv_d, a.eps);
-        const float m = k * k * head_sum(sw, log_c) * a.inv_d;
+        ss = w.at.extra ? 0.f : ss + (w.l.two ? st : 0.f);
+        gs = w.at.extra ? 0.f : gs + (w.l.two ? gt : 0.f);
+        const float k = inv_rms(head_sum(ss, w.log_c), a.inv_d, a.eps);
+        const float m = k * k * head_sum(gs, w.log_c) * a.inv_d;
+        const int drs = w.past_rows(now.rg), dhs = w.past_heads(now.h);
+        const float kd = drs + dhs > 0 || w.at.extra ? 0.f : k;   // repeats add nothing
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) {
-          dg[i] = fmaf(w[i], v[i] * k, dg[i]);
-          w[i] = k * fmaf(w[i], g[i], -v[i] * m);
+        for (int e = 0; e < 2 * V; ++e) {
+          dg[e] = fmaf(u[e], v[e] * kd, dg[e]);
+          u[e] = k * fmaf(u[e], g[e], -v[e] * m);
         }
-        store_head<T, V>(const_cast<T*>(y.at(row0, head0 + h + (u << log_h))), y.off, l.on, head, w);
-      }
-      h += U << log_h;
-      if (h >= n) break;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        load_head<T, V>(x.at(row0, head0 + h + (u << log_h)), x.off, l.on,
-                        h + (u << log_h) < left, rx[u]);
-        load_head<T, V>(dy.at(row0, head0 + h + (u << log_h)), dy.off, l.on,
-                        h + (u << log_h) < left, rd[u]);
+        const T* at[2];
+        y.at(w.row0(now.rg), now.h, drs, dhs, w.edge(now), at);
+        store_head<T, V>(at, u);
+        load(rx[i], rd[i], pos[i]);
+        now.next(1 << w.log_h, w.n, w.rg_step);
+        more = now.rg < w.groups;
       }
     }
   }
   if (!sd.part) return;
   // the lanes of one column: over the wave, then over the block's waves through LDS
   __syncthreads();
-  float* cols = &trig[0][0][0];
+  float* cols = &trig[0][0];
 #pragma unroll
-  for (int i = 0; i < 2 * V; ++i) {
-    for (int o = 1 << log_c; o < 64; o <<= 1) dg[i] += __shfl_xor(dg[i], o);
-    if (lane < (1 << log_c) && l.on[i / V]) cols[wave * kMaxHeadDim + l.col[i / V] + i % V] = dg[i];
+  for (int e = 0; e < 2 * V; ++e) {
+    for (int o = 1 << w.log_c; o < 64; o <<= 1) dg[e] += __shfl_xor(dg[e], o);
+    if (lane < a.lanes && (e < V || w.l.two)) cols[wave * kMaxHeadDim + w.l.col[e / V] + e % V] = dg[e];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < a.d; i += 256)
@@ -378,17 +473,17 @@ struct GainArgs {
   int blocks[2];
   int d, accumulate;
 };
-// 8 columns x 32 lanes of blocks; blocks of a lane in order, then the lanes
-__global__ __launch_bounds__(256) void gain_reduce_kernel(GainArgs a) {
-  __shared__ float lds[32][9];
+// 8 columns x 128 lanes of blocks; blocks of a lane in order, then the lanes
+__global__ __launch_bounds__(1024) void gain_reduce_kernel(GainArgs a) {
+  __shared__ float lds[128][9];
   const int z = blockIdx.y, cl = threadIdx.x & 7, bl = threadIdx.x >> 3, c = blockIdx.x * 8 + cl;
   if (!a.grad[z]) return;
   float s = 0.f;
-#pragma unroll 4
-  for (int b = bl; b < a.blocks[z]; b += 32) s += a.part[z][(int64_t)b * a.d + c];
+#pragma unroll 8
+  for (int b = bl; b < a.blocks[z]; b += 128) s += a.part[z][(int64_t)b * a.d + c];
   lds[bl][cl] = s;
   __syncthreads();
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = 64; o > 0; o >>= 1) {
     if (bl < o) lds[bl][cl] += lds[bl + o][cl];
     __syncthreads();
   }
@@ -405,38 +500,66 @@ int log2_up(int n) {
 int vector_of(int dtype, int half, int d) {
   return dtype == DT_BF16 && half % 8 == 0 && (d - 2 * half) % 8 == 0 ? 8 : 4;
 }
-int lanes_log2(int v, int half, int d) {   // lanes of a head
-  return log2_up(half / v + (d - 2 * half + 2 * v - 1) / (2 * v));
-}
-
 constexpr int kWaves = 4096;    // enough waves for 256 compute units
-constexpr int kFwdBlocks = 4096;
+constexpr int kMaxBlocks = 4096, kMaxBwdBlocks = 1536;
 
-// Heads a wave holds at once: as few idle slots over a row's heads as can be, then as many
-// heads as can be (a row's angles are worked out once per wave).  Few rows are spread over
-// the heads too.
-void divide(SideArgs& s, int64_t rows, int log_c, int max_blocks) {
-  if (s.heads == 0 || rows == 0) return;   // no items, no blocks
-  int best = 0, idle = 1 << 30;
-  for (int h = 0; h <= 6 - log_c; ++h) {
+// Heads a wave holds at once: the most (a row's angles are worked out once per wave) that
+// leave at most an eighth of the slots over a row's heads idle, or the fewest idle.  Few
+// rows are spread over the heads too.
+void divide(SideArgs& s, int64_t rows, int log_c, int min_log_h, int max_blocks) {
+  if (s.heads == 0 || rows == 0) return;   // no blocks
+  int best = min_log_h, idle = 1 << 30;
+  for (int h = min_log_h; h <= 6 - log_c; ++h) {
     const int n = (s.heads + (1 << h) - 1) >> h, waste = (n << h) - s.heads;
-    if (waste <= idle) {
+    if (waste <= idle || waste * 8 <= n << h) {
       idle = waste;
       best = h;
     }
   }
-  const int rs = 6 - log_c - best;
-  const int64_t groups = (rows + (1 << rs) - 1) >> rs;
-  const int iters = (s.heads + (1 << best) - 1) >> best;
+  const int rs = 6 - log_c - best, iters = (s.heads + (1 << best) - 1) >> best;
   s.log_h = best;
-  s.head_groups = (int)std::max<int64_t>(1, std::min<int64_t>(iters, kWaves / groups));
+  s.groups = (int)((rows + (1 << rs) - 1) >> rs);
+  s.head_groups = std::max(1, std::min(iters, std::min(kWaves, 4 * max_blocks) / s.groups));
   s.iters = (iters + s.head_groups - 1) / s.head_groups;
   s.head_groups = (iters + s.iters - 1) / s.iters;
-  s.items = (int)(groups * s.head_groups);
-  s.blocks = std::min((s.items + 3) / 4, max_blocks);
+  s.blocks = (int)std::min<int64_t>(((int64_t)s.groups * s.head_groups + 3) / 4, max_blocks);
 }
 
-constexpr int kBwdBlocks = 512;
+// Slots of heads a wave must hold so that its lanes work out a row's angles two each at most.
+// A side with fewer heads leaves the others idle: a launch of its own with eight angles a lane
+// took 52 us against 46 (rotation of 40000 rows, 8 + 1 heads of 128), and 133 against 120 in
+// the norm's backward with 16 + 2.
+int min_slots_log2(const QkArgs& a) {
+  int h = 0;
+  while ((2 << (a.log_c + h)) < a.half) ++h;
+  return h;
+}
+// The sides of a launch.  Blocks: as many as are resident at once (`resident`: four waves a
+// SIMD forward, three backward), or `many` where each of their waves would take `long_walk`
+// steps and more.  Each side's share of them is its share of the steps, a row's angles
+// counted as another.  Returns the position loads of a step (2 or 8).
+int divide(QkArgs& a, int resident, int many, int long_walk) {
+  const int min_log_h = min_slots_log2(a);
+  const bool few = std::max(a.side[0].heads, a.side[1].heads) < 1 << min_log_h;
+  double steps[2] = {0.0, 0.0};
+  int max_blocks = resident;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int z = 0; z < 2; ++z) {
+      const SideArgs& s = a.side[z];
+      divide(a.side[z], a.rows, a.log_c, few ? 0 : min_log_h, max_blocks);
+      steps[z] = (double)s.groups * s.head_groups * (s.iters + 1);
+    }
+    if (steps[0] + steps[1] < 4.0 * resident * long_walk) break;
+    max_blocks = many;
+  }
+  if (a.side[0].blocks + a.side[1].blocks > max_blocks)
+    for (SideArgs& s : a.side)
+      if (s.blocks > 0) {
+        const double share = steps[&s - a.side] / (steps[0] + steps[1]);
+        s.blocks = std::max((s.head_groups + 3) / 4, std::min(s.blocks, (int)(max_blocks * share)));
+      }
+  return few ? 8 : 2;
+}
 
 QkArgs device_args(const QkProblem& p, int v) {
   QkArgs a;
@@ -453,75 +576,71 @@ QkArgs device_args(const QkProblem& p, int v) {
   a.d = p.head_dim;
   a.half = p.rot_dim / 2;
   a.inverse = p.inverse;
-  a.log_c = lanes_log2(v, a.half, a.d);
+  a.lanes = a.half / v + (a.d - 2 * a.half + 2 * v - 1) / (2 * v);
+  a.log_c = log2_up(a.lanes);
   a.table = p.table;
   return a;
 }
 
-}  // namespace
+template <class T, int V, bool ADJ, int KP>
+void launch_fwd(const QkArgs& a, bool norm, hipStream_t s) {
+  const dim3 grid(a.side[0].blocks + a.side[1].blocks);
+  if (norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, true, KP>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, false, KP>), grid, dim3(256), 0, s, a);
+}
+template <class T, int V, bool ADJ, int KP>
+void launch_bwd(const QkArgs& a, hipStream_t s) {
+  const dim3 grid(a.side[0].blocks + a.side[1].blocks);
+  hipLaunchKernelGGL((qk_bwd_kernel<T, V, ADJ, KP>), grid, dim3(256), 0, s, a);
+}
+template <class T, int V>
+void launch(const QkArgs& a, const QkProblem& p, bool bwd, int kp, hipStream_t s) {
+  if (bwd) {
+    if (kp == 2) p.adjacent ? launch_bwd<T, V, true, 2>(a, s) : launch_bwd<T, V, false, 2>(a, s);
+    else p.adjacent ? launch_bwd<T, V, true, 8>(a, s) : launch_bwd<T, V, false, 8>(a, s);
+  } else {
+    if (kp == 2) p.adjacent ? launch_fwd<T, V, true, 2>(a, p.norm, s) : launch_fwd<T, V, false, 2>(a, p.norm, s);
+    else p.adjacent ? launch_fwd<T, V, true, 8>(a, p.norm, s) : launch_fwd<T, V, false, 8>(a, p.norm, s);
+  }
+}
 
-hipError_t qk_rope_fwd(const QkProblem& p, hipStream_t s) {
-  if (p.rows == 0) return hipSuccess;
+// `gain`: a backward, whose blocks leave their sums in scratch.
+hipError_t run(const QkProblem& p, GainArgs* gain, float* scratch, hipStream_t s) {
   const int v = vector_of(p.dtype, p.rot_dim / 2, p.head_dim);
   QkArgs a = device_args(p, v);
-  for (SideArgs& sd : a.side) divide(sd, p.rows, a.log_c, kFwdBlocks);
-  const dim3 grid(a.side[0].blocks + a.side[1].blocks);
-  if (grid.x == 0) return hipSuccess;
-#define MPIPE_QK(T, V)                                                                            \
-  do {                                                                                            \
-    if (p.adjacent) {                                                                             \
-      if (p.norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, true, true>), grid, dim3(256), 0, s, a); \
-      else hipLaunchKernelGGL((qk_fwd_kernel<T, V, true, false>), grid, dim3(256), 0, s, a);      \
-    } else {                                                                                      \
-      if (p.norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, false, true>), grid, dim3(256), 0, s, a); \
-      else hipLaunchKernelGGL((qk_fwd_kernel<T, V, false, false>), grid, dim3(256), 0, s, a);     \
-    }                                                                                             \
-  } while (0)
-  if (p.dtype == DT_F32) MPIPE_QK(float, 4);
-  else if (v == 8) MPIPE_QK(bf16, 8);
-  else MPIPE_QK(bf16, 4);
-#undef MPIPE_QK
+  const int kp = gain ? divide(a, 768, kMaxBwdBlocks, 48) : divide(a, 1024, kMaxBlocks, 16);
+  if (a.side[0].blocks + a.side[1].blocks == 0) return hipSuccess;
+  if (gain)
+    for (int z = 0; z < 2; ++z) {
+      a.side[z].part = gain->grad[z] ? scratch : nullptr;
+      gain->part[z] = scratch;
+      gain->blocks[z] = a.side[z].blocks;
+      scratch += (int64_t)a.side[z].blocks * p.head_dim;
+    }
+  if (p.dtype == DT_F32) launch<float, 4>(a, p, gain, kp, s);
+  else if (v == 8) launch<bf16, 8>(a, p, gain, kp, s);
+  else launch<bf16, 4>(a, p, gain, kp, s);
   return hipGetLastError();
 }
 
+}  // namespace
+
+hipError_t qk_rope_fwd(const QkProblem& p, hipStream_t s) { return run(p, nullptr, nullptr, s); }
+
+// at most kMaxBwdBlocks blocks a side, and no more than it has heads
 size_t qk_norm_rope_bwd_scratch(int64_t rows, int heads_q, int heads_k, int head_dim) {
-  const auto blocks = [&](int heads) { return (size_t)std::min<int64_t>(rows * heads, kBwdBlocks); };
+  const auto blocks = [&](int heads) { return (size_t)std::min<int64_t>(rows * heads, kMaxBwdBlocks); };
   return (blocks(heads_q) + blocks(heads_k)) * head_dim * 4 + 256;
 }
 
 hipError_t qk_norm_rope_bwd(const QkProblem& p, bool accumulate, float* scratch, hipStream_t s) {
-  const int v = vector_of(p.dtype, p.rot_dim / 2, p.head_dim);
-  QkArgs a = device_args(p, v);
-  GainArgs r;
-  bool any = false;
-  for (int z = 0; z < 2; ++z) {
-    SideArgs& sd = a.side[z];
-    divide(sd, p.rows, a.log_c, kBwdBlocks);
-    sd.part = p.side[z].grad ? scratch : nullptr;
-    r.part[z] = scratch;
-    r.grad[z] = p.side[z].grad;
-    r.blocks[z] = sd.blocks;
-    scratch += (int64_t)sd.blocks * p.head_dim;
-    any |= p.side[z].grad != nullptr;
-  }
-  const dim3 grid(a.side[0].blocks + a.side[1].blocks);
-  if (grid.x > 0) {
-#define MPIPE_QK(T, V)                                                                            \
-  do {                                                                                            \
-    if (p.adjacent) hipLaunchKernelGGL((qk_bwd_kernel<T, V, true>), grid, dim3(256), 0, s, a);    \
-    else hipLaunchKernelGGL((qk_bwd_kernel<T, V, false>), grid, dim3(256), 0, s, a);              \
-  } while (0)
-    if (p.dtype == DT_F32) MPIPE_QK(float, 4);
-    else if (v == 8) MPIPE_QK(bf16, 8);
-    else MPIPE_QK(bf16, 4);
-#undef MPIPE_QK
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (!any) return hipSuccess;
+  GainArgs r = {};
+  for (int z = 0; z < 2; ++z) r.grad[z] = p.side[z].grad;
+  const hipError_t e = run(p, &r, scratch, s);
+  if (e != hipSuccess || (!r.grad[0] && !r.grad[1])) return e;
   r.d = p.head_dim;
   r.accumulate = accumulate;
-  hipLaunchKernelGGL(gain_reduce_kernel, dim3(p.head_dim / 8, 2), dim3(256), 0, s, r);
+  hipLaunchKernelGGL(gain_reduce_kernel, dim3(p.head_dim / 8, 2), dim3(1024), 0, s, r);
   return hipGetLastError();
 }
 

@@ -746,3 +746,56 @@ def test_a_trained_step_together():
     for r, t in zip(ref, grads):
         _close(t, 0.1 * r, np.abs(0.1 * r), 2.0 ** -23, "f32", "clip")
     enc.close()
+
+
+# ---- how the work is divided -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,rows,hq,hk,name", [
+    ("bf16", 1, 300, 1, "d128_3axes"), ("f32", 3, 65, 64, "d256"), ("bf16", 5000, 1, 1, "d128_3axes"),
+    ("bf16", 33000, 28, 4, "d128_3axes"), ("bf16", 9000, 47, 2, "d80_yx"), ("f32", 5000, 2, 1, "d8"),
+    ("f32", 30000, 9, 9, "d72"), ("bf16", 2, 9000, 33, "d16_part"), ("bf16", 4097, 3, 3, "d248"),
+])
+def test_rows_do_not_depend_on_each_other(dtype, rows, hq, hk, name):
+    """Few rows and many heads, many rows and few heads, long walks: a row's results have the
+    same bits as in a call of its own part, and the gains' gradient is the parts' sum."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS[name]
+    cfg, d, axes = _cfg(c), c["head_dim"], len(c["sections"])
+    announce(f"division of {rows} rows, {hq}+{hk} heads of {d} {dtype}")
+    g = torch.Generator(device=dev).manual_seed(rows)
+    rand = lambda *s: torch.randn(s, device=dev, generator=g).to(_tdt(dtype))
+    q, k, dq, dk = rand(rows, hq, d), rand(rows, hk, d), rand(rows, hq, d), rand(rows, hk, d)
+    gain = [rand(d), rand(d)]
+    pos = torch.randint(0, 100000, (axes, rows), device=dev, dtype=torch.int32, generator=g)
+
+    def call(rs, hs):
+        a = [t[rs, hs if t.shape[1] == hq else slice(None)] for t in (q, k, dq, dk)]
+        if hs != slice(None):
+            a[1] = a[3] = None
+        n = a[0].shape[0]
+        out = [None if t is None else torch.full_like(t, float("nan")) for t in (a[0], a[1]) * 3]
+        gg = [torch.empty(d, device=dev), None if a[1] is None else torch.empty(d, device=dev)]
+        sc = torch.empty(mp.op_qk_norm_rope_scratch_bytes(n, a[0].shape[1], hk, d),
+                         dtype=torch.uint8, device=dev)
+        p = pos[:, rs]
+        mp.op_rope_axes(cfg, a[0], a[1], p, out[0], out[1], inverse=True)
+        mp.op_qk_norm_rope_fwd(cfg, a[0], a[1], *gain, 1e-6, p, out[2], out[3])
+        mp.op_qk_norm_rope_bwd(cfg, a[2], a[3], a[0], a[1], *gain, 1e-6, p, out[4], out[5], *gg, sc,
+                               accumulate=False)
+        return out, gg
+
+    whole, gg = call(slice(None), slice(None))
+    edges = sorted({0, rows // 3, rows // 2, rows})
+    total = [torch.zeros(d, dtype=torch.float64, device=dev) for _ in range(2)]
+    for lo, hi in zip(edges, edges[1:]):
+        part, pg = call(slice(lo, hi), slice(None))
+        assert all(torch.equal(w[lo:hi], p) for w, p in zip(whole, part)), (lo, hi)
+        total = [t + x.double() for t, x in zip(total, pg)]
+    if hq != hk:
+        part, _ = call(slice(None), slice(hq // 2, hq // 2 + 1))     # one head alone
+        assert all(torch.equal(whole[i][:, hq // 2:hq // 2 + 1], part[i]) for i in (0, 2, 4))
+    # sums of N terms in two orders, each off by less than 2^-24 min(N, 1200) of their sizes,
+    # which for normal values are below 2 N
+    n = rows * max(hq, hk)
+    for a, b in zip(gg, total):
+        assert float((a.double() - b).abs().max()) <= 2 * 2.0 ** -24 * min(n, 1200) * 2 * n
