@@ -113,7 +113,7 @@ __device__ __forceinline__ void widen(const Words<T, V> (&r)[2], float (&v)[2 * 
     v[i] = __uint_as_float(E == 1 ? w : i % 2 ? w & 0xFFFF0000u : w << 16);
   }
 }
-template <class T, int V>
+template <class T, int V, bool PAST>
 __device__ __forceinline__ void store_head(const T* const (&p)[2], const float (&v)[2 * V]) {
   constexpr int E = 4 / sizeof(T);
 #pragma unroll
@@ -129,7 +129,9 @@ __device__ __forceinline__ void store_head(const T* const (&p)[2], const float (
         r[i] = __builtin_bit_cast(uint32_t, t);
       }
     }
-    *(MPIPE_GLOBAL typename Vec<T, V>::At*)const_cast<T*>(p[k]) = r;
+    const auto to = (MPIPE_GLOBAL typename Vec<T, V>::At*)const_cast<T*>(p[k]);
+    if constexpr (PAST) __builtin_nontemporal_store(r, to);
+    else *to = r;
   }
 }
 
@@ -302,7 +304,8 @@ __device__ __forceinline__ void copy_tables(const QkArgs& a, uint64_t* turns) {
   __syncthreads();
 }
 
-template <class T, int V, bool ADJ, bool NORM, int KP>
+// KP: position loads of a step (2 or 8); PAST: outputs that no cache would hold for a reader
+template <class T, int V, bool ADJ, bool NORM, int KP, bool PAST>
 __global__ __launch_bounds__(256, KP == 2 ? 4 : 2) void qk_fwd_kernel(QkArgs a) {
   constexpr int kRing = 3;
   __shared__ float trig[4][2 * kTrig];
@@ -360,7 +363,7 @@ __global__ __launch_bounds__(256, KP == 2 ? 4 : 2) void qk_fwd_kernel(QkArgs a) 
       turn<V, ADJ>(w.l, c, s, v);
       const T* at[2];
       y.at(w.row0(now.rg), now.h, w.past_rows(now.rg), w.past_heads(now.h), w.edge(now), at);
-      store_head<T, V>(at, v);
+      store_head<T, V, PAST>(at, v);
       load(r[i], pos[i]);
       now.next(1 << w.log_h, w.n, w.rg_step);
       if (now.rg >= w.groups) return;
@@ -368,7 +371,7 @@ __global__ __launch_bounds__(256, KP == 2 ? 4 : 2) void qk_fwd_kernel(QkArgs a) 
   }
 }
 
-template <class T, int V, bool ADJ, int KP>
+template <class T, int V, bool ADJ, int KP, bool PAST>
 __global__ __launch_bounds__(256, KP == 2 ? 3 : 2) void qk_bwd_kernel(QkArgs a) {
   constexpr int kRing = 2;
   __shared__ float trig[4][2 * kTrig];
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(256, KP == 2 ? 3 : 2) void qk_bwd_kernel(QkArgs a) 
         }
         const T* at[2];
         y.at(w.row0(now.rg), now.h, drs, dhs, w.edge(now), at);
-        store_head<T, V>(at, u);
+        store_head<T, V, PAST>(at, u);
         load(rx[i], rd[i], pos[i]);
         now.next(1 << w.log_h, w.n, w.rg_step);
         more = now.rg < w.groups;
@@ -582,25 +585,42 @@ QkArgs device_args(const QkProblem& p, int v) {
   return a;
 }
 
-template <class T, int V, bool ADJ, int KP>
-void launch_fwd(const QkArgs& a, bool norm, hipStream_t s) {
-  const dim3 grid(a.side[0].blocks + a.side[1].blocks);
-  if (norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, true, KP>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, false, KP>), grid, dim3(256), 0, s, a);
+// Outputs of more than the 256 MB of last-level cache are stored past the caches where every
+// store fills whole 128-byte lines (half a head each): 65536 rows, 28 + 4 heads of 128, rotation
+// 201 -> 192 us, norm backward 321 -> 312 us.  Stores that share a line lose by it (45956 rows,
+// 8 + 8 heads of 256 that turn half, rotation: 155 -> 197 us), and a smaller output is still
+// cached for its reader.
+bool past_caches(const QkProblem& p) {
+  if (p.adjacent || p.rot_dim < p.head_dim) return false;
+  const int esz = p.dtype == DT_BF16 ? 2 : 4;
+  uint64_t at = (uint64_t)p.head_dim / 2 * esz;
+  int64_t heads = 0;
+  for (const QkSide& s : p.side)
+    if (s.y.heads > 0) {
+      heads += s.y.heads;
+      at |= (uintptr_t)s.y.p | (uint64_t)(s.y.row * esz) | (uint64_t)(s.y.head * esz);
+    }
+  return at % 128 == 0 && p.rows * heads * p.head_dim * esz > int64_t(256) << 20;
 }
-template <class T, int V, bool ADJ, int KP>
-void launch_bwd(const QkArgs& a, hipStream_t s) {
+
+template <class T, int V, bool ADJ, int KP, bool PAST>
+void launch(const QkArgs& a, bool norm, bool bwd, hipStream_t s) {
   const dim3 grid(a.side[0].blocks + a.side[1].blocks);
-  hipLaunchKernelGGL((qk_bwd_kernel<T, V, ADJ, KP>), grid, dim3(256), 0, s, a);
+  if (bwd) hipLaunchKernelGGL((qk_bwd_kernel<T, V, ADJ, KP, PAST>), grid, dim3(256), 0, s, a);
+  else if (norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, true, KP, PAST>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((qk_fwd_kernel<T, V, ADJ, false, KP, PAST>), grid, dim3(256), 0, s, a);
 }
 template <class T, int V>
 void launch(const QkArgs& a, const QkProblem& p, bool bwd, int kp, hipStream_t s) {
-  if (bwd) {
-    if (kp == 2) p.adjacent ? launch_bwd<T, V, true, 2>(a, s) : launch_bwd<T, V, false, 2>(a, s);
-    else p.adjacent ? launch_bwd<T, V, true, 8>(a, s) : launch_bwd<T, V, false, 8>(a, s);
+  // (eight angles a lane: few heads, far from filling a cache)
+  const bool past = kp == 2 && past_caches(p);
+  if (p.adjacent) {
+    if (kp == 8) launch<T, V, true, 8, false>(a, p.norm, bwd, s);
+    else launch<T, V, true, 2, false>(a, p.norm, bwd, s);
   } else {
-    if (kp == 2) p.adjacent ? launch_fwd<T, V, true, 2>(a, p.norm, s) : launch_fwd<T, V, false, 2>(a, p.norm, s);
-    else p.adjacent ? launch_fwd<T, V, true, 8>(a, p.norm, s) : launch_fwd<T, V, false, 8>(a, p.norm, s);
+    if (kp == 8) launch<T, V, false, 8, false>(a, p.norm, bwd, s);
+    else if (past) launch<T, V, false, 2, true>(a, p.norm, bwd, s);
+    else launch<T, V, false, 2, false>(a, p.norm, bwd, s);
   }
 }
 
