@@ -106,7 +106,8 @@ size_t mpipe_op_scratch_bytes(int64_t N, int32_t heads, int32_t n, int32_t n_seg
  * mpipe_encoder_bwd accumulated.  None of these calls synchronizes, allocates device memory
  * or keeps anything: metadata and tables travel in the kernels' arguments, so every call can
  * be captured into a graph, and a replay reads the buffers anew (host arguments stay as
- * captured).  The current device has to be that of the stream and the buffers. */
+ * captured).  The current device has to be that of the stream and the buffers.  Calls that
+ * overlap need scratch and results of their own. */
 
 /* Positions of the LLM's input rows on three axes (time, height, width): pos[axis * ld_pos
  * + row], device int32, for every row of the sequences; other rows are not written.

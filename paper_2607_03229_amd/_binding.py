@@ -601,13 +601,17 @@ def _launch(fn, tensors, stream, *args) -> None:
         torch.cuda.set_device(here)
 
 
-def _host_i64(a, name: str) -> np.ndarray:
-    if type(a) is np.ndarray and a.dtype == np.int64 and a.ndim == 1 and a.flags.c_contiguous:
+def _host_ints(a, name: str, dtype=np.int64) -> np.ndarray:
+    """A list of whole numbers as the library reads it."""
+    if type(a) is np.ndarray and a.dtype == dtype and a.ndim == 1 and a.flags.c_contiguous:
         return a
     arr = np.asarray(a)
-    _need(arr.ndim == 1 and (arr.size == 0 or arr.dtype.kind in "iu"),
-          f"{name}: a list of whole numbers")
-    return np.ascontiguousarray(arr, dtype=np.int64)
+    if arr.ndim != 1 or not (arr.size == 0 or arr.dtype.kind in "iu"):
+        raise MpipeError(-1, f"{name}: a list of whole numbers")
+    lim = np.iinfo(dtype)
+    if arr.size and (int(arr.min()) < lim.min or int(arr.max()) > lim.max):
+        raise MpipeError(-1, f"{name}: a value beyond {lim.bits} bits")
+    return np.ascontiguousarray(arr, dtype=dtype)
 
 
 def _p(arr: Optional[np.ndarray]):
@@ -621,19 +625,15 @@ def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, t
     were.  Item i's merged rows start at row item_row[i] with the encoder's grid_thw[i].
     Returns the position behind each sequence's last row, which is `seq_pos` when it goes on."""
     import torch
-    sr, sl = _host_i64(seq_row, "seq_row"), _host_i64(seq_len, "seq_len")
-    sp = None if seq_pos is None else _host_i64(seq_pos, "seq_pos")
-    ir = _host_i64(item_row, "item_row")
-    g = np.ascontiguousarray(_host_i64(np.asarray(grid_thw).reshape(-1), "grid_thw"))
-    ts = None if time_step is None else _host_i64(time_step, "time_step")
+    sr, sl = _host_ints(seq_row, "seq_row"), _host_ints(seq_len, "seq_len")
+    sp = None if seq_pos is None else _host_ints(seq_pos, "seq_pos")
+    ir = _host_ints(item_row, "item_row")
+    g = _host_ints(np.asarray(grid_thw).reshape(-1), "grid_thw", np.int32)
+    ts = None if time_step is None else _host_ints(time_step, "time_step", np.int32)
     _need(sl.size == sr.size and (sp is None or sp.size == sr.size),
           "seq_row, seq_len and seq_pos differ in length")
     _need(g.size == 3 * ir.size and (ts is None or ts.size == ir.size),
           "item_row, grid_thw and time_step differ in length")
-    for a in (g, ts):
-        _need(a is None or a.size == 0 or (a.min() >= -2 ** 31 and a.max() < 2 ** 31),
-              "a grid or time step beyond 32 bits")
-    g, ts = g.astype(np.int32), None if ts is None else ts.astype(np.int32)
     _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == 3 and
           (pos.shape[1] <= 1 or pos.stride(1) == 1), "pos: int32 [3][rows], rows adjacent")
     nxt = np.zeros(sr.size, np.int64)

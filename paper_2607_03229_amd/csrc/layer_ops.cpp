@@ -88,7 +88,7 @@ mpipe_status check_qk(QkProblem& p, int32_t dtype, const mpipe_rope_cfg* cfg, in
       return set_error(MPIPE_ERR_INVALID_ARG, "the outputs of q and k share memory");
     for (int w = 0; w < 2; ++w)
       for (const HeadView* v : {&p.side[w].x, &p.side[w].dy})
-        if (!(w == z && same_view(y, *v)) && views_meet(y, *v, rows, d, esz))
+        if (!(w == z && same_view(y, *v, rows)) && views_meet(y, *v, rows, d, esz))
           return set_error(MPIPE_ERR_INVALID_ARG, "an output shares memory with another view");
   }
   return MPIPE_OK;
@@ -233,6 +233,8 @@ mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad
       if (mpipe_status st = grad_outputs_ok(grads, out, n, why)) return set_error(st, why);
     if (!sumsq || (uintptr_t)sumsq % 8 || (uintptr_t)norm % 4)
       return set_error(MPIPE_ERR_INVALID_ARG, "null sumsq, or a misaligned result");
+    if (norm && (uintptr_t)norm < (uintptr_t)(sumsq + 1) && (uintptr_t)(norm + 1) > (uintptr_t)sumsq)
+      return set_error(MPIPE_ERR_INVALID_ARG, "norm inside sumsq");
     if (!(max_norm >= 0.0)) return set_error(MPIPE_ERR_INVALID_ARG, "max_norm must be 0 or more");
     return hip_status(grad_clip(grads, out, n, p, sumsq, max_norm, norm,
                                 reinterpret_cast<hipStream_t>(stream)));

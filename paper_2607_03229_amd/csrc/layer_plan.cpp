@@ -184,8 +184,9 @@ bool view_ok(const HeadView& v, int64_t rows, int32_t d, int esz, bool written, 
   return true;
 }
 
-bool same_view(const HeadView& a, const HeadView& b) {
-  return a.p == b.p && a.row == b.row && a.head == b.head && a.heads == b.heads;
+bool same_view(const HeadView& a, const HeadView& b, int64_t rows) {
+  return a.p == b.p && a.heads == b.heads && (a.row == b.row || rows == 1) &&
+         (a.head == b.head || a.heads == 1);
 }
 
 bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, int esz) {

@@ -49,7 +49,8 @@ struct HeadView {
 // A view that can be read: non-null, strides >= 0, no overflow.  `written`: also no element
 // of it twice.
 bool view_ok(const HeadView& v, int64_t rows, int32_t d, int esz, bool written, std::string& why);
-bool same_view(const HeadView& a, const HeadView& b);
+// the same elements (a stride over one row or head does not count)
+bool same_view(const HeadView& a, const HeadView& b, int64_t rows);
 // Whether two (valid) views may share an element: not if their ranges are apart, or if they
 // are apart inside rows of one stride.
 bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, int esz);

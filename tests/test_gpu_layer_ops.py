@@ -249,6 +249,22 @@ def test_layouts(name, layout, dtype):
         assert torch.equal(a, want[4]) and torch.equal(b, want[5])
 
 
+def test_in_place_over_one_row_or_head():
+    """A stride over one row, or one head, does not make a view another one."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), CFGS["d64_part_halves"]
+    gen = torch.Generator().manual_seed(12)
+    announce("in place over one row or head")
+    for rows, heads in ((1, 3), (5, 1), (1, 1)):
+        _, pos = _pos(np.random.default_rng(1), 2, rows)
+        x = _rand(gen, (rows, heads, 64), "bf16")
+        y = x.as_strided(x.shape, (heads * 64 if rows > 1 else 7, 64 if heads > 1 else 9, 1))
+        want = torch.empty_like(x)
+        mp.op_rope_axes(_cfg(c), x, None, pos, want, None)
+        mp.op_rope_axes(_cfg(c), x, None, pos, y, None)
+        assert torch.equal(x, want)
+
+
 def test_rope_into_one_product():
     """q, k turned inside rows of q | k | v, in place: v and the rest stay."""
     torch, dev = torch_dev()
@@ -553,6 +569,31 @@ def test_grad_clip_in_place(dtype):
     assert torch.equal(buf, keep)
 
 
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+def test_grad_clip_of_many_elements(dtype, out):
+    """Outputs larger than the last-level cache, off alignment by one element."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    n = 140_000_003
+    announce(f"grad clip of {n} elements {dtype}->{out}")
+    gen = torch.Generator(device=dev).manual_seed(3)
+    g = torch.randn(n + 1, device=dev, generator=gen).to(_tdt(dtype))[1:]
+    o = torch.empty(n + 2, dtype=_tdt(out), device=dev)
+    o[0] = o[-1] = 7
+    sumsq, norms = _norm_call([g])
+    want = float((g.double() ** 2).sum())
+    assert abs(float(sumsq) - want) <= 1e-12 * want
+    mp.op_grad_clip([g], sumsq, 100.0, None, out=[o[1:-1]])
+    f = 100.0 / want ** 0.5
+    ref = g.double() * f
+    err = (o[1:-1].double() - ref).abs()
+    assert bool((err <= (2.0 ** -23 + OUT[out]) * ref.abs() + 1e-37).all())
+    assert float(o[0]) == 7 and float(o[-1]) == 7
+    if dtype == out:
+        mp.op_grad_clip([g], sumsq, 100.0)
+        assert torch.equal(g, o[1:-1])
+
+
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
 def test_grad_clip_not_finite(value):
     """The norm shows it; gradients in place stay, outputs are copies."""
@@ -752,7 +793,7 @@ def test_a_trained_step_together():
 
 @pytest.mark.parametrize("dtype,rows,hq,hk,name", [
     ("bf16", 1, 300, 1, "d128_3axes"), ("f32", 3, 65, 64, "d256"), ("bf16", 5000, 1, 1, "d128_3axes"),
-    ("bf16", 33000, 28, 4, "d128_3axes"), ("bf16", 9000, 47, 2, "d80_yx"), ("f32", 5000, 2, 1, "d8"),
+    ("bf16", 33000, 28, 4, "d128_3axes"), ("f32", 17000, 28, 4, "d128_interleaved"), ("bf16", 9000, 47, 2, "d80_yx"), ("f32", 5000, 2, 1, "d8"),
     ("f32", 30000, 9, 9, "d72"), ("bf16", 2, 9000, 33, "d16_part"), ("bf16", 4097, 3, 3, "d248"),
 ])
 def test_rows_do_not_depend_on_each_other(dtype, rows, hq, hk, name):

@@ -255,6 +255,7 @@ def test_clip_arguments_refused(L):
     assert L.mpipe_op_grad_norm(a, n, FAKE * 8, None, None, 1 << 30, None) == -3
     assert L.mpipe_op_grad_norm(a, n, FAKE * 8, None, FAKE * 9 + 4, 1 << 30, None) == -1
     assert L.mpipe_op_grad_clip(a, None, n, None, 1.0, None, None) == -1
+    assert L.mpipe_op_grad_clip(a, None, n, FAKE * 8, 1.0, FAKE * 8 + 4, None) == -1
     assert L.mpipe_op_grad_clip(a, None, n, FAKE * 8, -1.0, None, None) == -1
     assert L.mpipe_op_grad_clip(a, None, n, FAKE * 8, math.nan, None, None) == -1
     assert L.mpipe_op_grad_norm(None, 3, FAKE * 8, None, FAKE * 9, 1 << 30, None) == -1
