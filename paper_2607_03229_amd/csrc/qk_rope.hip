@@ -153,7 +153,8 @@ __device__ __forceinline__ float head_sum(float v, int log_c) {
 }
 __device__ __forceinline__ float inv_rms(float ss, float inv_d, float eps) {
   const float m = fmaf(ss, inv_d, eps), r = __builtin_amdgcn_rsqf(m);
-  return fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r);   // one Newton step: the root to half a step
+  // one Newton step: the root to half a step (an infinite mean keeps its 0)
+  return m < __builtin_inff() ? fmaf(0.5f * r, fmaf(-m * r, r, 1.f), r) : r;
 }
 
 template <int V, bool ADJ>
@@ -613,16 +614,15 @@ void launch(const QkArgs& a, bool norm, bool bwd, hipStream_t s) {
 }
 template <class T, int V>
 void launch(const QkArgs& a, const QkProblem& p, bool bwd, int kp, hipStream_t s) {
-  // (eight angles a lane: few heads, far from filling a cache)
-  const bool past = kp == 2 && past_caches(p);
   if (p.adjacent) {
     if (kp == 8) launch<T, V, true, 8, false>(a, p.norm, bwd, s);
     else launch<T, V, true, 2, false>(a, p.norm, bwd, s);
-  } else {
-    if (kp == 8) launch<T, V, false, 8, false>(a, p.norm, bwd, s);
-    else if (past) launch<T, V, false, 2, true>(a, p.norm, bwd, s);
-    else launch<T, V, false, 2, false>(a, p.norm, bwd, s);
+    return;
   }
+  if constexpr (V * sizeof(T) == 16)   // (whole lines have 16-byte vectors)
+    if (kp == 2 && past_caches(p)) return launch<T, V, false, 2, true>(a, p.norm, bwd, s);
+  if (kp == 8) launch<T, V, false, 8, false>(a, p.norm, bwd, s);
+  else launch<T, V, false, 2, false>(a, p.norm, bwd, s);
 }
 
 // `gain`: a backward, whose blocks leave their sums in scratch.

@@ -326,6 +326,22 @@ def test_values_stay_in_their_head():
     assert int((~torch.isfinite(b[4, 1])).sum()) == 1 and int(torch.isnan(b[6, 2]).sum()) == 2
 
 
+def test_norm_of_an_infinite_head():
+    """An infinity makes its own column not a number and the rest of its head zero, as the
+    formula has it; a NaN takes the whole head."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce("norm of infinite heads")
+    cfg = mp.RopeCfg(32, [4], rot_dim=8)
+    x = _rand(torch.Generator().manual_seed(3), (2, 2, 32), "f32")
+    x[0, 1, 20], x[1, 0, 9] = float("inf"), float("nan")
+    pos = torch.zeros((1, 2), dtype=torch.int32, device=dev)
+    g, y = torch.ones(32, device=dev), torch.empty_like(x)
+    mp.op_qk_norm_rope_fwd(cfg, x, None, g, None, 1e-6, pos, y, None)
+    assert bool(y[0, 1, 20].isnan()) and int((y[0, 1] == 0).sum()) == 31
+    assert bool(y[1, 0].isnan().all()) and bool(torch.isfinite(y[0, 0]).all() and torch.isfinite(y[1, 1]).all())
+
+
 # ---- with the norm ------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
