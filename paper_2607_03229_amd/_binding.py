@@ -571,27 +571,22 @@ def op_attention_bwd(dtype, qkv, o, d_o, lse, N, heads, head_dim, cu_seqlens, dq
 # The first LLM layer behind the seam, and the end of a trained step
 # --------------------------------------------------------------------------
 
-def _need(ok: bool, msg: str) -> None:
-    if not ok:
-        raise MpipeError(-1, msg)
+def _bad(msg: str) -> None:
+    raise MpipeError(-1, msg)
 
 
-def _launch(fn, tensors, stream, *args) -> None:
-    """fn(*args, stream) with every tensor on one GPU, which is current for the call (it need
-    not be before); the stream is that GPU's current one unless given."""
+def _launch(fn, dev: int, stream, *args) -> None:
+    """fn(*args, stream) with GPU `dev` (of every tensor of the call) current, which it need
+    not be before; the stream is that GPU's current one unless given."""
     import torch
-    dev = tensors[0].device
-    if dev.type != "cuda":
-        raise MpipeError(-1, "tensors must be on the GPU")
-    for t in tensors:
-        if t.device != dev:
-            raise MpipeError(-1, "tensors on different devices")
+    if dev < 0:
+        _bad("tensors must be on the GPU")
     if stream is None:
-        stream = torch.cuda.current_stream(dev.index)
-    elif stream.device != dev:
-        raise MpipeError(-1, "a stream of another device than the tensors'")
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device_index != dev:
+        _bad("a stream of another device than the tensors'")
     here = torch.cuda.current_device()
-    if here == dev.index:
+    if here == dev:
         _check(fn(*args, stream.cuda_stream))
         return
     torch.cuda.set_device(dev)
@@ -603,19 +598,15 @@ def _launch(fn, tensors, stream, *args) -> None:
 
 def _host_ints(a, name: str, dtype=np.int64) -> np.ndarray:
     """A list of whole numbers as the library reads it."""
-    if type(a) is np.ndarray and a.dtype == dtype and a.ndim == 1 and a.flags.c_contiguous:
+    if type(a) is np.ndarray and a.dtype == dtype and a.ndim == 1:
         return a
     arr = np.asarray(a)
     if arr.ndim != 1 or not (arr.size == 0 or arr.dtype.kind in "iu"):
-        raise MpipeError(-1, f"{name}: a list of whole numbers")
+        _bad(f"{name}: a list of whole numbers")
     lim = np.iinfo(dtype)
     if arr.size and (int(arr.min()) < lim.min or int(arr.max()) > lim.max):
-        raise MpipeError(-1, f"{name}: a value beyond {lim.bits} bits")
-    return np.ascontiguousarray(arr, dtype=dtype)
-
-
-def _p(arr: Optional[np.ndarray]):
-    return None if arr is None else arr.__array_interface__["data"][0]
+        _bad(f"{name}: a value beyond {lim.bits} bits")
+    return arr.astype(dtype)
 
 
 def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, time_step=None,
@@ -630,88 +621,120 @@ def op_seam_positions(seq_row, seq_len, item_row, grid_thw, pos, seq_pos=None, t
     ir = _host_ints(item_row, "item_row")
     g = _host_ints(np.asarray(grid_thw).reshape(-1), "grid_thw", np.int32)
     ts = None if time_step is None else _host_ints(time_step, "time_step", np.int32)
-    _need(sl.size == sr.size and (sp is None or sp.size == sr.size),
-          "seq_row, seq_len and seq_pos differ in length")
-    _need(g.size == 3 * ir.size and (ts is None or ts.size == ir.size),
-          "item_row, grid_thw and time_step differ in length")
-    _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == 3 and
-          (pos.shape[1] <= 1 or pos.stride(1) == 1), "pos: int32 [3][rows], rows adjacent")
+    if sl.size != sr.size or (sp is not None and sp.size != sr.size):
+        _bad("seq_row, seq_len and seq_pos differ in length")
+    if g.size != 3 * ir.size or (ts is not None and ts.size != ir.size):
+        _bad("item_row, grid_thw and time_step differ in length")
+    if (pos.dtype is not torch.int32 or pos.dim() != 2 or pos.shape[0] != 3 or
+            (pos.shape[1] > 1 and pos.stride(1) != 1)):
+        _bad("pos: int32 [3][rows], rows adjacent")
     nxt = np.zeros(sr.size, np.int64)
-    _launch(load().mpipe_op_seam_positions, (pos,), stream, _p(sr), _p(sl), _p(sp), sr.size,
-            _p(ir), _p(g), _p(ts), ir.size, pos.shape[1], pos.data_ptr(), pos.stride(0), _p(nxt))
+    # (the arrays' bytes: ctypes passes their address at once)
+    _launch(load().mpipe_op_seam_positions, pos.get_device(), stream, sr.tobytes(), sl.tobytes(),
+            None if sp is None else sp.tobytes(), sr.size, ir.tobytes(), g.tobytes(),
+            None if ts is None else ts.tobytes(), ir.size, pos.shape[1], pos.data_ptr(),
+            pos.stride(0), nxt.ctypes.data)
     return nxt
 
 
 _HEADS = struct.Struct("PqqiI")    # mpipe_heads
 
 
-def _heads(t, like=None):
-    """mpipe_heads of [rows][heads][head_dim]; None: no heads."""
-    if t is None:
-        return None
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise MpipeError(-1, "inputs, gradients and outputs differ in shape or dtype")
-    rs, hs, cs = t.stride()
-    if cs != 1:
-        raise MpipeError(-1, "the columns of a head must be adjacent")
-    return _HEADS.pack(t.data_ptr(), rs, hs, t.shape[1], 0)
-
-
-def _qk_common(cfg, q, k, pos, outs):
-    """(dtype, rows) of q and k [rows][heads][head_dim] (either may be None) and the tensors
-    of the call."""
+def _qk(cfg, pos, q, k, q_more, k_more):
+    """(torch dtype, rows, device, views of q and of q_more, of k and of k_more): q and k
+    [rows][heads][head_dim] with any strides of rows and heads, either may be None, and what
+    goes with each of the same shape.  A view is an mpipe_heads; None: no heads."""
     import torch
     one = q if q is not None else k
-    _need(one is not None, "neither q nor k")
-    rows, dtype, ts = one.shape[0], one.dtype, [pos]
-    for x, ys in ((q, outs[0]), (k, outs[1])):
+    if one is None:
+        _bad("neither q nor k")
+    rows, dtype, dev, views = one.shape[0], one.dtype, one.get_device(), []
+    for x, more in ((q, q_more), (k, k_more)):
         if x is None:
-            _need(all(y is None for y in ys), "one of q and k without its input")
+            if any(y is not None for y in more):
+                _bad("an output or gradient of q or k without its input")
+            views.append((None,) * (1 + len(more)))
             continue
-        _need(x.dim() == 3 and x.shape[2] == cfg.head_dim and x.shape[0] == rows and
-              x.dtype == dtype, "q and k: [rows][heads][head_dim] of one dtype")
-        _need(all(y is not None for y in ys), "one of q and k without its output")
-        ts.append(x)
-        ts.extend(ys)
-    _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == cfg.axes and
-          pos.shape[1] == rows and (rows <= 1 or pos.stride(1) == 1),
-          "pos: int32 [axes][rows], rows adjacent")
-    return _dt(one), rows, ts
+        shape = x.shape
+        if len(shape) != 3 or shape[0] != rows or shape[2] != cfg.head_dim:
+            _bad("q and k: [rows][heads][head_dim]")
+        heads, v = shape[1], []
+        for y in (x, *more):
+            if y is None:
+                _bad("q or k without its output or gradient")
+            if y.dtype is not dtype or (y is not x and y.shape != shape):
+                _bad("inputs, gradients and outputs differ in shape or dtype")
+            rs, hs, cs = y.stride()
+            if cs != 1:
+                _bad("the columns of a head must be adjacent")
+            if y.get_device() != dev:
+                _bad("tensors on different devices")
+            v.append(_HEADS.pack(y.data_ptr(), rs, hs, heads, 0))
+        views.append(v)
+    if (pos.dtype is not torch.int32 or pos.dim() != 2 or pos.shape[0] != cfg.axes or
+            pos.shape[1] != rows or (rows > 1 and pos.stride(1) != 1)):
+        _bad("pos: int32 [axes][rows], rows adjacent")
+    if pos.get_device() != dev:
+        _bad("tensors on different devices")
+    return dtype, rows, dev, views[0], views[1]
 
 
-def _gains(cfg, x, gain, name):
-    if x is None:
-        return
-    _need(gain is not None and gain.dtype == x.dtype and gain.dim() == 1 and
-          gain.shape[0] == cfg.head_dim and gain.is_contiguous(),
-          f"{name}: [head_dim] in the heads' dtype")
+def _vector(t, n: int, dtype, dev: int, what: str) -> int:
+    """The address of a vector of n."""
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        _bad(what)
+    if t.get_device() != dev:
+        _bad("tensors on different devices")
+    return t.data_ptr()
+
+
+def _buffer(t, dev: int) -> Tuple[Optional[int], int]:
+    """Address and bytes of scratch."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        _bad("scratch must be contiguous")
+    if t.get_device() != dev:
+        _bad("tensors on different devices")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _code(dtype) -> int:
+    import torch
+    if dtype is torch.bfloat16:
+        return BF16
+    if dtype is torch.float32:
+        return F32
+    raise MpipeError(-1, f"unsupported dtype {dtype}")
 
 
 def op_rope_axes(cfg, q, k, pos, q_out, k_out, inverse: bool = False, stream=None) -> None:
     """q_out, k_out = q, k ([rows][heads][head_dim], any strides of rows and heads; k and
     k_out may be None) turned by pos (int32 [axes][rows]); inverse turns back (the gradient).
     An output may be its own input."""
-    dt, rows, ts = _qk_common(cfg, q, k, pos, ((q_out,), (k_out,)))
-    _launch(load().mpipe_op_rope_axes, ts, stream, dt, C.byref(cfg), rows, _heads(q), _heads(k),
-            pos.data_ptr(), pos.stride(0), int(bool(inverse)), _heads(q_out, q),
-            _heads(k_out, k))
+    dtype, rows, dev, (q, qo), (k, ko) = _qk(cfg, pos, q, k, (q_out,), (k_out,))
+    _launch(load().mpipe_op_rope_axes, dev, stream, _code(dtype), C.byref(cfg), rows, q, k,
+            pos.data_ptr(), pos.stride(0), 1 if inverse else 0, qo, ko)
+
+
+_GAIN = "gains: [head_dim] in the heads' dtype"
+_GAIN_GRAD = "gain gradients: fp32 [head_dim]"
 
 
 def op_qk_norm_rope_fwd(cfg, q, k, q_gain, k_gain, eps: float, pos, q_out, k_out,
                         stream=None) -> None:
     """The same behind a root-mean-square norm of every head with a gain [head_dim]."""
-    dt, rows, ts = _qk_common(cfg, q, k, pos, ((q_out,), (k_out,)))
-    _gains(cfg, q, q_gain, "q_gain")
-    _gains(cfg, k, k_gain, "k_gain")
-    ts += [g for g in (q_gain, k_gain) if g is not None]
-    _launch(load().mpipe_op_qk_norm_rope_fwd, ts, stream, dt, C.byref(cfg), rows, _heads(q),
-            _heads(k), _ptr(q_gain), _ptr(k_gain), eps, pos.data_ptr(), pos.stride(0),
-            _heads(q_out, q), _heads(k_out, k))
+    dtype, rows, dev, (q, qo), (k, ko) = _qk(cfg, pos, q, k, (q_out,), (k_out,))
+    gains = [None if g is None else _vector(g, cfg.head_dim, dtype, dev, _GAIN)
+             for g in (q_gain, k_gain)]
+    _launch(load().mpipe_op_qk_norm_rope_fwd, dev, stream, _code(dtype), C.byref(cfg), rows, q, k,
+            *gains, eps, pos.data_ptr(), pos.stride(0), qo, ko)
 
 
 def op_qk_norm_rope_scratch_bytes(rows: int, heads_q: int, heads_k: int, head_dim: int) -> int:
     n = int(load().mpipe_op_qk_norm_rope_scratch_bytes(rows, heads_q, heads_k, head_dim))
-    _need(n > 0, "op_qk_norm_rope_scratch_bytes: argument out of range")
+    if n == 0:
+        _bad("op_qk_norm_rope_scratch_bytes: argument out of range")
     return n
 
 
@@ -723,20 +746,16 @@ def op_qk_norm_rope_bwd(cfg, dq, dk, q, k, q_gain, k_gain, eps: float, pos, dq_i
     [head_dim], may be None) are added to, or overwritten with accumulate=False.  scratch:
     op_qk_norm_rope_scratch_bytes."""
     import torch
-    dt, rows, ts = _qk_common(cfg, q, k, pos, ((dq, dq_in), (dk, dk_in)))
-    _gains(cfg, q, q_gain, "q_gain")
-    _gains(cfg, k, k_gain, "k_gain")
-    for g, x in ((grad_q_gain, q), (grad_k_gain, k)):
-        _need(g is None or (x is not None and g.dtype == torch.float32 and g.dim() == 1 and
-                            g.shape[0] == cfg.head_dim and g.is_contiguous()),
-              "gain gradients: fp32 [head_dim]")
-    _need(scratch is None or scratch.is_contiguous(), "scratch must be contiguous")
-    ts += [t for t in (q_gain, k_gain, grad_q_gain, grad_k_gain, scratch) if t is not None]
-    _launch(load().mpipe_op_qk_norm_rope_bwd, ts, stream, dt, C.byref(cfg), rows, _heads(dq, q),
-            _heads(dk, k), _heads(q), _heads(k), _ptr(q_gain), _ptr(k_gain), eps, pos.data_ptr(),
-            pos.stride(0), _heads(dq_in, q), _heads(dk_in, k), _ptr(grad_q_gain),
-            _ptr(grad_k_gain), int(bool(accumulate)), _ptr(scratch),
-            0 if scratch is None else scratch.numel() * scratch.element_size())
+    if (q is None and grad_q_gain is not None) or (k is None and grad_k_gain is not None):
+        _bad("a gain's gradient without its heads")
+    dtype, rows, dev, (q, dq, qi), (k, dk, ki) = _qk(cfg, pos, q, k, (dq, dq_in), (dk, dk_in))
+    d, f32 = cfg.head_dim, torch.float32
+    gains = [None if g is None else _vector(g, d, dtype, dev, _GAIN) for g in (q_gain, k_gain)]
+    grads = [None if g is None else _vector(g, d, f32, dev, _GAIN_GRAD)
+             for g in (grad_q_gain, grad_k_gain)]
+    _launch(load().mpipe_op_qk_norm_rope_bwd, dev, stream, _code(dtype), C.byref(cfg), rows, dq,
+            dk, q, k, *gains, eps, pos.data_ptr(), pos.stride(0), qi, ki, *grads,
+            1 if accumulate else 0, *_buffer(scratch, dev))
 
 
 class GradList:
@@ -745,13 +764,15 @@ class GradList:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        n = len(self.tensors)
-        self.array = (_GradTensor * max(n, 1))()
+        self.n = len(self.tensors)
+        self.array = (_GradTensor * max(self.n, 1))()
+        self.dev = self.tensors[0].get_device() if self.n else None
         for a, t in zip(self.array, self.tensors):
-            _need(t.is_contiguous(), "gradients must be contiguous")
-            _need(t.device == self.tensors[0].device, "tensors on different devices")
-            a.data, a.n, a.dtype = t.data_ptr(), t.numel(), _dt(t)
-        self.n = n
+            if not t.is_contiguous():
+                _bad("gradients must be contiguous")
+            if t.get_device() != self.dev:
+                _bad("tensors on different devices")
+            a.data, a.n, a.dtype = t.data_ptr(), t.numel(), _code(t.dtype)
 
 
 def _grad_list(grads) -> GradList:
@@ -767,18 +788,25 @@ def op_grad_scratch_bytes(grads) -> int:
     return n
 
 
+def _result(t, n: int, dtype, dev: int, what: str) -> int:
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _bad(what)
+    if t.get_device() != dev:
+        _bad("tensors on different devices")
+    return t.data_ptr()
+
+
 def op_grad_norm(grads, sumsq, norms, scratch, stream=None) -> None:
     """sumsq (fp64 [1]) = the sum of squares over all of grads (a GradList or tensors);
     norms (fp32 [tensors], may be None) = each one's L2 norm."""
     import torch
-    g = _grad_list(grads)
-    _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1, "sumsq: fp64 [1]")
-    _need(norms is None or (norms.dtype == torch.float32 and norms.numel() == g.n and
-                            norms.is_contiguous()), "norms: fp32 [tensors]")
-    _need(scratch.is_contiguous(), "scratch must be contiguous")
-    ts = [sumsq, scratch] + g.tensors[:1] + ([] if norms is None else [norms])
-    _launch(load().mpipe_op_grad_norm, ts, stream, g.array, g.n, _ptr(sumsq), _ptr(norms),
-            _ptr(scratch), scratch.numel() * scratch.element_size())
+    g, dev = _grad_list(grads), sumsq.get_device()
+    if g.dev not in (None, dev):
+        _bad("tensors on different devices")
+    _launch(load().mpipe_op_grad_norm, dev, stream, g.array, g.n,
+            _result(sumsq, 1, torch.float64, dev, "sumsq: fp64 [1]"),
+            None if norms is None else _result(norms, g.n, torch.float32, dev,
+                                               "norms: fp32 [tensors]"), *_buffer(scratch, dev))
 
 
 def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None) -> None:
@@ -786,12 +814,11 @@ def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None
     or into `out` (tensors of the same lengths, fp32 or bf16, always written).  norm (fp32
     [1], may be None) = sqrt(sumsq)."""
     import torch
-    g = _grad_list(grads)
-    o = None if out is None else _grad_list(out)
-    _need(sumsq.dtype == torch.float64 and sumsq.numel() == 1, "sumsq: fp64 [1]")
-    _need(norm is None or (norm.dtype == torch.float32 and norm.numel() == 1), "norm: fp32 [1]")
-    _need(o is None or o.n == g.n, "grads and out differ in number")
-    ts = [sumsq] + g.tensors[:1] + ([] if norm is None else [norm]) + \
-        ([] if o is None else o.tensors[:1])
-    _launch(load().mpipe_op_grad_clip, ts, stream, g.array, None if o is None else o.array, g.n,
-            _ptr(sumsq), float(max_norm), _ptr(norm))
+    g, o, dev = _grad_list(grads), None if out is None else _grad_list(out), sumsq.get_device()
+    if g.dev not in (None, dev) or (o is not None and o.dev not in (None, dev)):
+        _bad("tensors on different devices")
+    if o is not None and o.n != g.n:
+        _bad("grads and out differ in number")
+    _launch(load().mpipe_op_grad_clip, dev, stream, g.array, None if o is None else o.array, g.n,
+            _result(sumsq, 1, torch.float64, dev, "sumsq: fp64 [1]"), max_norm,
+            None if norm is None else _result(norm, 1, torch.float32, dev, "norm: fp32 [1]"))
