@@ -13,12 +13,29 @@
 namespace mpipe {
 namespace {
 
-constexpr int kNormTensors = 190, kClipTensors = 130;   // arguments below 4 KB
+constexpr int kNormTensors = 248, kClipTensors = 164;   // arguments below 4 KB
 
+// A tensor in 16 bytes (24 with an output): its address, below 2^48, under the upper bits of
+// its size; the size is elements * 4 + 1 where it is bf16, + 2 where its output is.
 struct NormArgs {
-  const void* p[kNormTensors];
-  int64_t n[kNormTensors];   // elements * 2 + (1 where bf16)
+  uint64_t at[kNormTensors];
+  uint32_t size[kNormTensors];
   int32_t first[kNormTensors];   // first chunk, from chunk0
+};
+__host__ __device__ __forceinline__ uint64_t upper(uint64_t at, int64_t size) {
+  return at | ((uint64_t)size >> 32) << 48;
+}
+struct Tensor {
+  const char* p;
+  int64_t n;
+  bool in16, out16;
+  __device__ __forceinline__ Tensor(uint64_t at, uint32_t size) {
+    const uint64_t whole = (at >> 48) << 32 | size;
+    p = reinterpret_cast<const char*>(at & 0xFFFFFFFFFFFFull);
+    n = (int64_t)(whole >> 2);
+    in16 = whole & 1;
+    out16 = whole & 2;
+  }
 };
 
 // The tensor of chunk c: how many first chunks are not behind it, less one.  All of them are
@@ -120,14 +137,28 @@ __global__ __launch_bounds__(256) void sumsq_kernel(NormArgs a, int n, int tenso
                                                     int32_t* starts) {
   __shared__ double lds[4];
   const int c = blockIdx.x, t = tensor_of(a.first, n, c), nth = c - a.first[t];
-  const int64_t len = a.n[t] >> 1, at = nth * chunk;
-  const int m = (int)(len - at < chunk ? len - at : chunk);
-  const double s = block_sum((a.n[t] & 1) ? chunk_sum((const bf16*)a.p[t] + at, m)
-                                          : chunk_sum((const float*)a.p[t] + at, m), lds);
+  const Tensor x(a.at[t], a.size[t]);
+  const int64_t at = nth * chunk;
+  const int m = (int)(x.n - at < chunk ? x.n - at : chunk);
+  const double s = block_sum(x.in16 ? chunk_sum((const bf16*)x.p + at, m)
+                                    : chunk_sum((const float*)x.p + at, m), lds);
   if (threadIdx.x == 0) {
     partial[chunk0 + c] = s;
     if (nth == 0) starts[tensor0 + t] = chunk0 + c;
   }
+}
+
+// the thread's share of p[begin .. end): eight loads at once (those past the end repeat the last)
+__device__ __forceinline__ double strided_sum(const double* p, int begin, int end) {
+  double s = 0.0;
+  for (int c = begin + threadIdx.x; c < end; c += 8 * 256) {
+    double v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = p[min(c + u * 256, end - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += c + u * 256 < end ? v[u] : 0.0;
+  }
+  return s;
 }
 
 // block t: the sum of tensor t's chunks, its norm
@@ -135,10 +166,8 @@ __global__ __launch_bounds__(256) void tensor_sum_kernel(const double* partial,
                                                          const int32_t* starts, int n, int chunks,
                                                          double* sums, float* norms) {
   __shared__ double lds[4];
-  const int t = blockIdx.x, end = t + 1 < n ? starts[t + 1] : chunks;
-  double s = 0.0;
-  for (int c = starts[t] + threadIdx.x; c < end; c += 256) s += partial[c];
-  s = block_sum(s, lds);
+  const int t = blockIdx.x;
+  const double s = block_sum(strided_sum(partial, starts[t], t + 1 < n ? starts[t + 1] : chunks), lds);
   if (threadIdx.x == 0) {
     sums[t] = s;
     if (norms) norms[t] = (float)sqrt(s);
@@ -147,41 +176,46 @@ __global__ __launch_bounds__(256) void tensor_sum_kernel(const double* partial,
 
 __global__ __launch_bounds__(256) void total_kernel(const double* sums, int n, double* sumsq) {
   __shared__ double lds[4];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
-  s = block_sum(s, lds);
+  const double s = block_sum(strided_sum(sums, 0, n), lds);
   if (threadIdx.x == 0) *sumsq = s;
 }
 
-// both steps in one block, where there are few tensors and chunks: a wave a tensor
+// Both steps in one block, where there are few tensors and chunks: the chunks' sums to LDS at
+// once, then a wave a tensor.
 constexpr int kFewTensors = 64, kFewChunks = 4096;
 __global__ __launch_bounds__(1024) void few_sums_kernel(const double* partial,
                                                         const int32_t* starts, int n, int chunks,
                                                         float* norms, double* sumsq) {
-  __shared__ double lds[kFewTensors];
+  __shared__ double part[kFewChunks], sums[kFewTensors];
+  __shared__ int32_t first[kFewTensors + 1];
   const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 0; k < kFewChunks; k += 1024)
+    if (k + (int)threadIdx.x < chunks) part[k + threadIdx.x] = partial[k + threadIdx.x];
+  if ((int)threadIdx.x <= n) first[threadIdx.x] = (int)threadIdx.x < n ? starts[threadIdx.x] : chunks;
+  __syncthreads();
   for (int t = threadIdx.x >> 6; t < n; t += 16) {
-    const int end = t + 1 < n ? starts[t + 1] : chunks;
     double s = 0.0;
-    for (int c = starts[t] + lane; c < end; c += 64) s += partial[c];
+#pragma unroll 8
+    for (int c = first[t] + lane; c < first[t + 1]; c += 64) s += part[c];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
     if (lane == 0) {
-      lds[t] = s;
+      sums[t] = s;
       if (norms) norms[t] = (float)sqrt(s);
     }
   }
   __syncthreads();
   if (threadIdx.x < 64) {
-    double s = lane < n ? lds[lane] : 0.0;
+    double s = lane < n ? sums[lane] : 0.0;
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
     if (lane == 0) *sumsq = s;
   }
 }
 
 struct ClipArgs {
-  const void* p[kClipTensors];
-  void* o[kClipTensors];
-  int64_t n[kClipTensors];   // elements * 4 + (1 where the input is bf16) + (2 where the output is)
+  uint64_t at[kClipTensors];
+  void* out[kClipTensors];
+  uint32_t size[kClipTensors];
   int32_t first[kClipTensors];
 };
 
@@ -225,14 +259,15 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t ch
   if (norm && c == 0 && threadIdx.x == 0) *norm = (float)len2;
   if (n == 0) return;
   const int t = tensor_of(a.first, n, c);
-  const int64_t len = a.n[t] >> 2, at = (c - a.first[t]) * chunk;
-  const int m = (int)(len - at < chunk ? len - at : chunk);
-  if (a.p[t] == a.o[t] && !scales) return;
-  const bool in16 = a.n[t] & 1, out16 = a.n[t] & 2;
-  if (in16 && out16) chunk_scale<PAST>((const bf16*)a.p[t] + at, (bf16*)a.o[t] + at, m, f);
-  else if (in16) chunk_scale<PAST>((const bf16*)a.p[t] + at, (float*)a.o[t] + at, m, f);
-  else if (out16) chunk_scale<PAST>((const float*)a.p[t] + at, (bf16*)a.o[t] + at, m, f);
-  else chunk_scale<PAST>((const float*)a.p[t] + at, (float*)a.o[t] + at, m, f);
+  const Tensor x(a.at[t], a.size[t]);
+  void* out = a.out[t];
+  if (x.p == out && !scales) return;
+  const int64_t at = (c - a.first[t]) * chunk;
+  const int m = (int)(x.n - at < chunk ? x.n - at : chunk);
+  if (x.in16 && x.out16) chunk_scale<PAST>((const bf16*)x.p + at, (bf16*)out + at, m, f);
+  else if (x.in16) chunk_scale<PAST>((const bf16*)x.p + at, (float*)out + at, m, f);
+  else if (x.out16) chunk_scale<PAST>((const float*)x.p + at, (bf16*)out + at, m, f);
+  else chunk_scale<PAST>((const float*)x.p + at, (float*)out + at, m, f);
 }
 
 int chunks_of(int64_t n, int64_t chunk) { return (int)std::max<int64_t>(1, (n + chunk - 1) / chunk); }
@@ -254,8 +289,9 @@ hipError_t grad_norm(const mpipe_grad_tensor* t, int n, const GradPlan& p, doubl
     const int tensor0 = i;
     int k = 0, c = 0;
     for (; i < n && k < kNormTensors; ++i, ++k) {
-      a.p[k] = t[i].data;
-      a.n[k] = t[i].n * 2 + (t[i].dtype == DT_BF16);
+      const int64_t size = t[i].n * 4 + (t[i].dtype == DT_BF16);
+      a.at[k] = upper((uintptr_t)t[i].data, size);
+      a.size[k] = (uint32_t)size;
       a.first[k] = c;
       c += chunks_of(t[i].n, p.chunk);
     }
@@ -296,9 +332,10 @@ hipError_t grad_clip(const mpipe_grad_tensor* in, const mpipe_grad_tensor* out, 
     int c = 0;
     for (int i = begin; i < end; ++i) {
       const int k = i - begin;
-      a.p[k] = in[i].data;
-      a.o[k] = out[i].data;
-      a.n[k] = in[i].n * 4 + (in[i].dtype == DT_BF16) + 2 * (out[i].dtype == DT_BF16);
+      const int64_t size = in[i].n * 4 + (in[i].dtype == DT_BF16) + 2 * (out[i].dtype == DT_BF16);
+      a.at[k] = upper((uintptr_t)in[i].data, size);
+      a.out[k] = out[i].data;
+      a.size[k] = (uint32_t)size;
       a.first[k] = c;
       c += chunks_of(in[i].n, p.chunk);
     }

@@ -229,6 +229,8 @@ mpipe_status tensors_ok(const mpipe_grad_tensor* t, int32_t n, int64_t& total, s
       return fail(why, MPIPE_ERR_INVALID_ARG, "a tensor of fewer than 0 or more than 2^44 elements");
     if (t[i].n > 0 && (!t[i].data || (uintptr_t)t[i].data % esz_of(t[i].dtype)))
       return fail(why, MPIPE_ERR_INVALID_ARG, "a null tensor, or one not aligned to its elements");
+    if ((uintptr_t)t[i].data >> 48)   // the kernels' lists keep 48 bits of it
+      return fail(why, MPIPE_ERR_INVALID_ARG, "an address of more than 48 bits");
     total += t[i].n;
     if (total > (int64_t(1) << 44))
       return fail(why, MPIPE_ERR_INVALID_ARG, "more than 2^44 elements in all");

@@ -470,6 +470,8 @@ __global__ __launch_bounds__(256, KP == 2 ? 3 : 2) void qk_bwd_kernel(QkArgs a) 
                                         (cols[2 * kMaxHeadDim + i] + cols[3 * kMaxHeadDim + i]);
 }
 
+constexpr int kMaxBlocks = 4096, kMaxBwdBlocks = 1536;
+
 // grad[z][c] (+)= sum of part[z][b][c] over the blocks, in order
 struct GainArgs {
   const float* part[2];
@@ -483,8 +485,16 @@ __global__ __launch_bounds__(1024) void gain_reduce_kernel(GainArgs a) {
   const int z = blockIdx.y, cl = threadIdx.x & 7, bl = threadIdx.x >> 3, c = blockIdx.x * 8 + cl;
   if (!a.grad[z]) return;
   float s = 0.f;
-#pragma unroll 8
-  for (int b = bl; b < a.blocks[z]; b += 128) s += a.part[z][(int64_t)b * a.d + c];
+  constexpr int kEach = kMaxBwdBlocks / 128;   // all loads at once, those past the end once more
+  const int blocks = a.blocks[z];
+  if (blocks > 0) {
+    float v[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u)
+      v[u] = a.part[z][(int64_t)min(bl + u * 128, blocks - 1) * a.d + c];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) s += bl + u * 128 < blocks ? v[u] : 0.f;
+  }
   lds[bl][cl] = s;
   __syncthreads();
   for (int o = 64; o > 0; o >>= 1) {
@@ -504,7 +514,6 @@ int log2_up(int n) {
 int vector_of(int dtype, int half, int d) {
   return dtype == DT_BF16 && half % 8 == 0 && (d - 2 * half) % 8 == 0 ? 8 : 4;
 }
-constexpr int kMaxBlocks = 4096, kMaxBwdBlocks = 1536;
 
 // Heads a wave holds at once: the most (a row's angles are worked out once per wave) that
 // leave at most an eighth of the slots over a row's heads idle, or the fewest idle.  Rows of
