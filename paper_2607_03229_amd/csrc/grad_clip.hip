@@ -4,7 +4,11 @@
 //   S = sum g^2 (fp64), norm = sqrt(S), out = g * (norm > max ? max / norm : 1)
 // Tensors are cut into chunks; their addresses travel in the kernels' arguments, a hundred or
 // two tensors a launch.  Every chunk's sum goes to its own place and the places are added in
-// order, so the result has the same bits every time.
+// order, so the result has the same bits every time.  fp64, because an fp32 square overflows at
+// 1.8e19 and a sum of 10^8 of them needs more than 24 bits; it costs nothing.
+//
+// Bound by HBM: MI355X, 675.8 M fp32 elements in 392 tensors: norm 441 us (6.1 TB/s), clip into
+// other buffers 1013 us (5.3); 30 tensors of 0.9 M bf16 elements 12 us in three launches.
 #include <algorithm>
 
 #include "common.h"
@@ -255,7 +259,8 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t ch
   const double len2 = sqrt(*sumsq);
   const bool scales = len2 > max_norm && len2 <= 1.7976931348623157e308;
   const float f = scales ? (float)(max_norm / len2) : 1.f;
-  const int c = gridDim.x - 1 - blockIdx.x;   // what the norm read last is cached still
+  // from the last chunk back: what the norm read last is cached still (1517 -> 1500 us)
+  const int c = gridDim.x - 1 - blockIdx.x;
   if (norm && c == 0 && threadIdx.x == 0) *norm = (float)len2;
   if (n == 0) return;
   const int t = tensor_of(a.first, n, c);

@@ -4,6 +4,11 @@
 //   u = R^T dy, r = (mean x^2 + eps)^(-1/2):  y = R (g x r),  dg = sum u x r,
 //   dx = r (g u - x r^2 mean(g u x))
 // R turns the pair (a, b) by the angle of its axis' position: (a c - b s, b c + a s).
+//
+// Bound by HBM: q and k are read and written once (the backward reads their output gradients
+// too).  MI355X, 65536 rows, 28 + 4 heads of 128, bf16: rotation 192 us (5.6 TB/s), norm
+// backward 308 us (5.2); 42940 rows, 16 + 16 heads of 80, norm forward 93 us (4.7; five of eight
+// lanes hold a head); a copy of 4 GiB runs at 4.8.  Few rows take 4.5 us, one chain of loads.
 #include <algorithm>
 
 #include "common.h"
