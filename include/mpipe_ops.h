@@ -190,8 +190,9 @@ mpipe_status mpipe_op_qk_norm_rope_fwd(int32_t dtype, const mpipe_rope_cfg* cfg,
  * positions; the norms' statistics are recomputed.  dq_in, dk_in: overwritten with the
  * gradients of q and k (may be the same views as dq, dk or as q, k).  grad_q_gain,
  * grad_k_gain: fp32 [head_dim], nullable; accumulate != 0 adds into them (the Accumulate edge),
- * else they are overwritten, also where there are no rows.  Summed in a fixed order: the same
- * call gives the same bits.  scratch: mpipe_op_qk_norm_rope_scratch_bytes, not kept, aligned
+ * else they are overwritten, also where there are no rows.  Every row counts in them: leave
+ * rows of padding out of the call (a call per sequence, accumulating), or give them finite q,
+ * k and zero dq, dk.  Summed in a fixed order: the same call gives the same bits.  scratch: mpipe_op_qk_norm_rope_scratch_bytes, not kept, aligned
  * to 4 bytes, apart from every other buffer. */
 mpipe_status mpipe_op_qk_norm_rope_bwd(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                        const mpipe_heads* dq, const mpipe_heads* dk,

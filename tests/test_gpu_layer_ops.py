@@ -18,6 +18,16 @@ from tests.gpu_util import announce, torch_dev
 
 pytestmark = pytest.mark.gpu
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Tensors made without a type are fp32, whatever a test before left as torch's default."""
+    torch = pytest.importorskip("torch")
+    old = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(old)
+
+
 OUT = {"bf16": 2.0 ** -8, "f32": 0.0}
 
 CFGS = {

@@ -11,6 +11,16 @@ import paper_2607_03229_amd as mp
 from paper_2607_03229_amd import _binding as B
 from tests import layer_ref as R
 
+@pytest.fixture(autouse=True)
+def fp32_by_default():
+    """Tensors made without a type are fp32, whatever a test before left as torch's default."""
+    torch = pytest.importorskip("torch")
+    old = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(old)
+
+
 FAKE = 0x100000     # never dereferenced: the call must fail on the host first
 
 
