@@ -1,6 +1,6 @@
 // Entry points of the operators around the first LLM layer and of the gradient's norm
 // (include/mpipe_ops.h): every check on the host, then the launches.
-#include <climits>
+#include <algorithm>
 #include <cmath>
 #include <exception>
 #include <string>
@@ -105,16 +105,20 @@ mpipe_status mpipe_op_seam_positions(const int64_t* seq_row, const int64_t* seq_
                                      int32_t* pos, int64_t ld_pos, int64_t* next, void* stream) {
   return guarded([&]() -> mpipe_status {
     std::vector<PosSpan> spans;
+    std::vector<int64_t> last(n_seq > 0 ? n_seq : 0);
     std::string why;
     int64_t end = 0;
     if (ld_pos < n_rows || ld_pos > (int64_t(1) << 40))
       return set_error(MPIPE_ERR_INVALID_ARG, "ld_pos must be at least n_rows");
     if (mpipe_status st = position_spans(seq_row, seq_len, seq_pos, n_seq, item_row, grid_thw,
-                                         time_step, n_items, n_rows, next, spans, end, why))
+                                         time_step, n_items, n_rows, last.data(), spans, end, why))
       return set_error(st, why);
     if (!spans.empty() && (!pos || (uintptr_t)pos % 4))
       return set_error(MPIPE_ERR_INVALID_ARG, "null or misaligned positions");
-    return hip_status(seam_positions(spans, end, pos, ld_pos, reinterpret_cast<hipStream_t>(stream)));
+    const mpipe_status st = hip_status(
+        seam_positions(spans, end, pos, ld_pos, reinterpret_cast<hipStream_t>(stream)));
+    if (st == MPIPE_OK && next) std::copy(last.begin(), last.end(), next);
+    return st;
   });
 }
 

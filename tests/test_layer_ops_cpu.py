@@ -79,6 +79,14 @@ def test_positions_refused(L, name):
     assert B.last_error()
 
 
+def test_refused_positions_write_no_next(L):
+    nxt = np.full(1, -5, np.int64)
+    a, n = np.zeros(1, np.int64), np.full(1, 4, np.int64)
+    assert L.mpipe_op_seam_positions(a.ctypes.data, n.ctypes.data, None, 1, None, None, None, 0, 10,
+                                     None, 10, nxt.ctypes.data, None) == -1
+    assert nxt[0] == -5
+
+
 def test_positions_of_nothing(L):
     """No sequences, or only empty ones: fine, and nothing is launched (the pointer is not
     looked at)."""
