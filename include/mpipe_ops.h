@@ -160,7 +160,7 @@ typedef struct {
  * column], strides in elements, aligned to one element; heads == 0: none (p may be null).
  * Inputs take any strides >= 0.  An output's elements must be distinct, and it may share
  * memory with an input only as the very same view of the same side (in place), or as other
- * columns of rows of one stride (q, k and v of one product). */
+ * columns of rows of one stride (q, k and v of one product); never with positions or gains. */
 typedef struct {
   void* p;
   int64_t row_stride, head_stride;
@@ -189,11 +189,12 @@ mpipe_status mpipe_op_qk_norm_rope_fwd(int32_t dtype, const mpipe_rope_cfg* cfg,
 /* Its backward from dq, dk (gradients of q_out, k_out) and the forward's q, k, gains, eps and
  * positions; the norms' statistics are recomputed.  dq_in, dk_in: overwritten with the
  * gradients of q and k (may be the same views as dq, dk or as q, k).  grad_q_gain,
- * grad_k_gain: fp32 [head_dim], nullable; accumulate != 0 adds into them (the Accumulate edge),
- * else they are overwritten, also where there are no rows.  Every row counts in them: leave
- * rows of padding out of the call (a call per sequence, accumulating), or give them finite q,
- * k and zero dq, dk.  Summed in a fixed order: the same call gives the same bits.  scratch: mpipe_op_qk_norm_rope_scratch_bytes, not kept, aligned
- * to 4 bytes, apart from every other buffer. */
+ * grad_k_gain: fp32 [head_dim], nullable, apart from each other and from dq_in and dk_in;
+ * accumulate != 0 adds into them (the Accumulate edge), else they are overwritten, also where
+ * there are no rows.  Every row counts in them: leave rows of padding out of the call (a call
+ * per sequence, accumulating), or give them finite q, k and zero dq, dk.  Summed in a fixed
+ * order: the same call gives the same bits.  scratch: mpipe_op_qk_norm_rope_scratch_bytes, not
+ * kept, aligned to 4 bytes, apart from every other buffer. */
 mpipe_status mpipe_op_qk_norm_rope_bwd(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                        const mpipe_heads* dq, const mpipe_heads* dk,
                                        const mpipe_heads* q, const mpipe_heads* k,

@@ -90,7 +90,37 @@ mpipe_status check_qk(QkProblem& p, int32_t dtype, const mpipe_rope_cfg* cfg, in
       for (const HeadView* v : {&p.side[w].x, &p.side[w].dy})
         if (!(w == z && same_view(y, *v, rows)) && views_meet(y, *v, rows, d, esz))
           return set_error(MPIPE_ERR_INVALID_ARG, "an output shares memory with another view");
+    // what every wave reads stays as it is while outputs are written
+    for (int a = 0; a < cfg->axes; ++a)
+      if (range_meets(pos + a * (cfg->axes > 1 ? ld_pos : 0), rows * sizeof(int32_t), y, rows, d, esz))
+        return set_error(MPIPE_ERR_INVALID_ARG, "an output shares memory with the positions");
+    for (const QkSide& s : p.side)
+      if (s.gain && range_meets(s.gain, (size_t)d * esz, y, rows, d, esz))
+        return set_error(MPIPE_ERR_INVALID_ARG, "an output shares memory with a gain");
   }
+  return MPIPE_OK;
+}
+
+// The gain gradients and the scratch of a backward: gradients apart from each other and from
+// the outputs; scratch, which blocks write while others still read, apart from everything.
+mpipe_status check_gain_grads(const QkProblem& p, int axes, const void* scratch, size_t bytes) {
+  const int esz = p.dtype == MPIPE_BF16 ? 2 : 4, d = p.head_dim;
+  const size_t gb = d * sizeof(float);
+  const QkSide &q = p.side[0], &k = p.side[1];
+  if (q.grad && k.grad && ranges_meet(q.grad, gb, k.grad, gb))
+    return set_error(MPIPE_ERR_INVALID_ARG, "the gain gradients share memory");
+  for (const QkSide& s : p.side) {
+    if (s.grad && (range_meets(s.grad, gb, q.y, p.rows, d, esz) ||
+                   range_meets(s.grad, gb, k.y, p.rows, d, esz)))
+      return set_error(MPIPE_ERR_INVALID_ARG, "a gain gradient shares memory with an output");
+    bool meets = s.grad && ranges_meet(scratch, bytes, s.grad, gb);
+    meets |= s.gain && ranges_meet(scratch, bytes, s.gain, (size_t)d * esz);
+    for (const HeadView* v : {&s.x, &s.dy, &s.y}) meets |= range_meets(scratch, bytes, *v, p.rows, d, esz);
+    if (meets) return set_error(MPIPE_ERR_INVALID_ARG, "scratch shares memory with another buffer");
+  }
+  for (int a = 0; a < axes && q.x.heads + k.x.heads > 0 && p.rows > 0; ++a)
+    if (ranges_meet(scratch, bytes, p.pos + a * (axes > 1 ? p.ld_pos : 0), p.rows * sizeof(int32_t)))
+      return set_error(MPIPE_ERR_INVALID_ARG, "scratch shares memory with another buffer");
   return MPIPE_OK;
 }
 
@@ -181,17 +211,18 @@ mpipe_status mpipe_op_qk_norm_rope_bwd(int32_t dtype, const mpipe_rope_cfg* cfg,
     if (!(eps > 0.f) || !std::isfinite(eps))
       return set_error(MPIPE_ERR_INVALID_ARG, "eps must be positive and finite");
     if (mpipe_status st = check_qk(p, dtype, cfg, rows, in, grad, out, gain, pos, ld_pos)) return st;
-    if ((uintptr_t)grad_q_gain % 4 || (uintptr_t)grad_k_gain % 4 ||
-        (grad_q_gain && grad_q_gain == grad_k_gain))
-      return set_error(MPIPE_ERR_INVALID_ARG, "gain gradients misaligned or the same");
+    if ((uintptr_t)grad_q_gain % 4 || (uintptr_t)grad_k_gain % 4)
+      return set_error(MPIPE_ERR_INVALID_ARG, "gain gradients misaligned");
     p.norm = p.inverse = true;
     p.eps = eps;
     p.side[0].grad = grad_q_gain;
     p.side[1].grad = grad_k_gain;
     const size_t need = qk_norm_rope_bwd_scratch(rows, p.side[0].x.heads, p.side[1].x.heads, p.head_dim);
-    if ((grad_q_gain || grad_k_gain) && rows > 0 && (!scratch || scratch_bytes < need))
+    const bool sums = (grad_q_gain || grad_k_gain) && rows > 0;
+    if (sums && (!scratch || scratch_bytes < need))
       return set_error(MPIPE_ERR_WORKSPACE, "scratch too small");
     if ((uintptr_t)scratch % 4) return set_error(MPIPE_ERR_INVALID_ARG, "scratch misaligned");
+    if (mpipe_status st = check_gain_grads(p, cfg->axes, scratch, sums ? need : 0)) return st;
     return hip_status(qk_norm_rope_bwd(p, accumulate != 0, reinterpret_cast<float*>(scratch),
                                        reinterpret_cast<hipStream_t>(stream)));
   });

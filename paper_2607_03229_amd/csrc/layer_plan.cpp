@@ -205,6 +205,35 @@ bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, i
   return !(off >= wa && off + wb <= r);
 }
 
+bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+  return a_bytes > 0 && b_bytes > 0 && pa < pb + b_bytes && pb < pa + a_bytes;
+}
+
+bool range_meets(const void* p, size_t bytes, const HeadView& v, int64_t rows, int32_t d, int esz) {
+  if (v.heads == 0 || rows == 0) return false;
+  int64_t n;
+  extent(v, rows, d, n);
+  if (!ranges_meet(p, bytes, v.p, (size_t)n * esz)) return false;
+  // the range as [lo, hi) from the view's start; the shorter side of the view is walked, and
+  // on the other the first run of columns that ends behind lo starts before hi or none does
+  const int64_t lo = (int64_t)((uintptr_t)p - (uintptr_t)v.p), hi = lo + (int64_t)bytes;
+  const bool by_head = v.heads <= rows;
+  const int64_t s_row = rows > 1 ? v.row * esz : 0, s_head = v.heads > 1 ? v.head * esz : 0;
+  const int64_t n_out = by_head ? v.heads : rows, n_in = by_head ? rows : v.heads;
+  const int64_t s_out = by_head ? s_head : s_row, s_in = by_head ? s_row : s_head;
+  for (int64_t o = 0; o < n_out; ++o) {
+    const int64_t behind = lo - o * s_out - (int64_t)d * esz;   // the run's offset is above it
+    int64_t i = 0;
+    if (behind >= 0) {
+      if (s_in == 0) continue;
+      i = behind / s_in + 1;
+    }
+    if (i < n_in && o * s_out + i * s_in < hi) return true;
+  }
+  return false;
+}
+
 // ---- gradient lists -------------------------------------------------------------------------
 
 int64_t grad_chunk(int64_t total) {

@@ -54,6 +54,10 @@ bool same_view(const HeadView& a, const HeadView& b, int64_t rows);
 // Whether two (valid) views may share an element: not if their ranges are apart, or if they
 // are apart inside rows of one stride.
 bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, int esz);
+// Whether two ranges of bytes share one, and whether a range shares one with an element of a
+// (valid) view.
+bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes);
+bool range_meets(const void* p, size_t bytes, const HeadView& v, int64_t rows, int32_t d, int esz);
 
 // ---- gradient lists -----------------------------------------------------------------------
 // Elements of a work chunk: enough chunks for every compute unit from 8 M elements on.

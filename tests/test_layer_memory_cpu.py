@@ -1,0 +1,61 @@
+"""Buffers that the operators around the first LLM layer write, over others of the same call:
+refused on the host with nothing launched.  The addresses are never dereferenced."""
+import ctypes as C
+
+import pytest
+
+import paper_2607_03229_amd as mp
+from paper_2607_03229_amd import _binding as B
+
+KB, MB = 1 << 10, 1 << 20
+ROWS, HEADS, D = 4, 8, 128          # bf16: a view is 8 KB, a gain 256 bytes, its gradient 512
+
+# each buffer in a megabyte of its own
+AT = {n: (i + 1) * MB for i, n in enumerate(
+    ("q", "k", "dq", "dk", "q_out", "k_out", "q_gain", "k_gain", "q_grad", "k_grad", "pos", "scratch"))}
+
+
+@pytest.fixture(scope="module")
+def L():
+    return B.load()
+
+
+def _call(L, op, at):
+    cfg = mp.RopeCfg(D, [16, 24, 24])
+    h = lambda n: B._HEADS.pack(at[n], HEADS * D, D, HEADS, 0)
+    pos, out = (at["pos"], ROWS), (h("q_out"), h("k_out"))
+    if op == "rope":
+        return L.mpipe_op_rope_axes(1, C.byref(cfg), ROWS, h("q"), h("k"), *pos, 0, *out, None)
+    gains = (at["q_gain"], at["k_gain"], 1e-6)
+    if op == "fwd":
+        return L.mpipe_op_qk_norm_rope_fwd(1, C.byref(cfg), ROWS, h("q"), h("k"), *gains, *pos, *out, None)
+    need = mp.op_qk_norm_rope_scratch_bytes(ROWS, HEADS, HEADS, D)
+    return L.mpipe_op_qk_norm_rope_bwd(1, C.byref(cfg), ROWS, h("dq"), h("dk"), h("q"), h("k"), *gains,
+                                       *pos, *out, at["q_grad"], at["k_grad"], 1, at["scratch"], need,
+                                       None)
+
+
+SHARED = [
+    # gain gradients that share some or all of their elements
+    ("bwd", "k_grad", "q_grad", 0), ("bwd", "k_grad", "q_grad", 4), ("bwd", "k_grad", "q_grad", 508),
+    ("bwd", "q_grad", "k_grad", 256),
+    # gain gradients in an output
+    ("bwd", "q_grad", "q_out", 0), ("bwd", "q_grad", "k_out", 4 * KB), ("bwd", "k_grad", "q_out", 8 * KB - 4),
+    ("bwd", "k_grad", "k_out", -508),
+    # scratch over any other
+    *[("bwd", "scratch", n, 0) for n in AT if n != "scratch"],
+    ("bwd", "scratch", "q", 8 * KB - 4), ("bwd", "pos", "scratch", 64), ("bwd", "k_grad", "scratch", 1024),
+    ("bwd", "q_gain", "scratch", 16),
+    # what is read by every wave, in an output: positions (48 bytes) and gains
+    *[(op, n, out, 4 * KB) for op in ("fwd", "bwd") for n in ("pos", "q_gain", "k_gain")
+      for out in ("q_out", "k_out")],
+    ("rope", "pos", "q_out", -44), ("rope", "pos", "k_out", 8 * KB - 4),
+]
+
+
+@pytest.mark.parametrize("op,name,over,shift", SHARED, ids=str)
+def test_qk_buffers_that_share_memory(L, op, name, over, shift):
+    at = dict(AT)
+    at[name] = at[over] + shift
+    assert _call(L, op, at) == -1
+    assert "share" in B.last_error()
