@@ -220,7 +220,8 @@ typedef struct {
  * nullable) = the L2 norm of each tensor.  Squares and sums in fp64 and in a fixed order: no
  * overflow for any fp32 gradient, and the same call gives the same bits.  sumsq is apart from
  * the norm so that a program can add the ranks' values first.  Two tensors of a list must not
- * share memory.  scratch: mpipe_op_grad_scratch_bytes, 8-byte aligned, not kept. */
+ * share memory, nor sumsq, norms and scratch with each other or with a tensor.  scratch:
+ * mpipe_op_grad_scratch_bytes, 8-byte aligned, not kept. */
 mpipe_status mpipe_op_grad_norm(const mpipe_grad_tensor* grads, int32_t n, double* sumsq,
                                 float* norms, void* scratch, size_t scratch_bytes,
                                 void* hip_stream);
@@ -231,7 +232,8 @@ size_t mpipe_op_grad_scratch_bytes(const mpipe_grad_tensor* grads, int32_t n);
  * max_norm and f = 1 elsewhere (a norm that is infinite or not a number included: the caller
  * sees it in norm), out[i] = grads[i] * f in out[i]'s dtype.  out == NULL or out[i].data ==
  * grads[i].data: in place, where f == 1 writes nothing.  Other outputs are apart from every
- * input and always written.  sumsq: device fp64 [1], as of this call's turn on the stream.
+ * input and always written.  sumsq: device fp64 [1], as of this call's turn on the stream, apart
+ * from every output; norm apart from sumsq and from every tensor.
  * max_norm >= 0 (infinity: never scales). */
 mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad_tensor* out,
                                 int32_t n, const double* sumsq, double max_norm, float* norm,

@@ -248,9 +248,16 @@ mpipe_status mpipe_op_grad_norm(const mpipe_grad_tensor* grads, int32_t n, doubl
     if (mpipe_status st = grad_plan(grads, n, p, why)) return set_error(st, why);
     if (!sumsq || (uintptr_t)sumsq % 8 || (uintptr_t)norms % 4)
       return set_error(MPIPE_ERR_INVALID_ARG, "null or misaligned result");
-    if (!scratch || scratch_bytes < grad_norm_scratch(n, p))
-      return set_error(MPIPE_ERR_WORKSPACE, "scratch too small");
+    const size_t need = grad_norm_scratch(n, p), norms_bytes = norms ? n * sizeof(float) : 0;
+    if (!scratch || scratch_bytes < need) return set_error(MPIPE_ERR_WORKSPACE, "scratch too small");
     if ((uintptr_t)scratch % 8) return set_error(MPIPE_ERR_INVALID_ARG, "scratch misaligned");
+    if (ranges_meet(sumsq, sizeof(double), norms, norms_bytes) ||
+        ranges_meet(scratch, need, sumsq, sizeof(double)) ||
+        ranges_meet(scratch, need, norms, norms_bytes))
+      return set_error(MPIPE_ERR_INVALID_ARG, "results or scratch share memory");
+    if (list_meets(grads, n, sumsq, sizeof(double)) || list_meets(grads, n, norms, norms_bytes) ||
+        list_meets(grads, n, scratch, need))
+      return set_error(MPIPE_ERR_INVALID_ARG, "a result or scratch shares memory with a gradient");
     return hip_status(grad_norm(grads, n, p, sumsq, norms, reinterpret_cast<char*>(scratch),
                                 reinterpret_cast<hipStream_t>(stream)));
   });
@@ -268,8 +275,13 @@ mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad
       if (mpipe_status st = grad_outputs_ok(grads, out, n, why)) return set_error(st, why);
     if (!sumsq || (uintptr_t)sumsq % 8 || (uintptr_t)norm % 4)
       return set_error(MPIPE_ERR_INVALID_ARG, "null sumsq, or a misaligned result");
-    if (norm && (uintptr_t)norm < (uintptr_t)(sumsq + 1) && (uintptr_t)(norm + 1) > (uintptr_t)sumsq)
-      return set_error(MPIPE_ERR_INVALID_ARG, "norm inside sumsq");
+    // read by every block, or written by one, while others read gradients and write outputs
+    const size_t norm_bytes = norm ? sizeof(float) : 0;
+    if (ranges_meet(sumsq, sizeof(double), norm, norm_bytes))
+      return set_error(MPIPE_ERR_INVALID_ARG, "norm shares memory with sumsq");
+    if (list_meets(out, n, sumsq, sizeof(double)) || list_meets(out, n, norm, norm_bytes) ||
+        (out != grads && list_meets(grads, n, norm, norm_bytes)))
+      return set_error(MPIPE_ERR_INVALID_ARG, "norm or sumsq shares memory with a tensor");
     if (!(max_norm >= 0.0)) return set_error(MPIPE_ERR_INVALID_ARG, "max_norm must be 0 or more");
     return hip_status(grad_clip(grads, out, n, p, sumsq, max_norm, norm,
                                 reinterpret_cast<hipStream_t>(stream)));

@@ -336,4 +336,10 @@ mpipe_status grad_outputs_ok(const mpipe_grad_tensor* in, const mpipe_grad_tenso
   return MPIPE_OK;
 }
 
+bool list_meets(const mpipe_grad_tensor* t, int32_t n, const void* p, size_t bytes) {
+  for (int32_t i = 0; i < n; ++i)
+    if (ranges_meet(p, bytes, t[i].data, (size_t)t[i].n * esz_of(t[i].dtype))) return true;
+  return false;
+}
+
 }  // namespace mpipe

@@ -70,5 +70,7 @@ mpipe_status grad_plan(const mpipe_grad_tensor* t, int32_t n, GradPlan& p, std::
 // either its own input (same type) or apart from every input.
 mpipe_status grad_outputs_ok(const mpipe_grad_tensor* in, const mpipe_grad_tensor* out, int32_t n,
                              std::string& why);
+// Whether a range of bytes shares one with a tensor of a (valid) list.
+bool list_meets(const mpipe_grad_tensor* t, int32_t n, const void* p, size_t bytes);
 
 }  // namespace mpipe

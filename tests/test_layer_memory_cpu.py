@@ -59,3 +59,42 @@ def test_qk_buffers_that_share_memory(L, op, name, over, shift):
     at[name] = at[over] + shift
     assert _call(L, op, at) == -1
     assert "share" in B.last_error()
+
+
+# ---- the norm of a gradient and its clip --------------------------------------------------------
+
+def _list(*ts):
+    a = (B._GradTensor * len(ts))()
+    for x, (p, n, dt) in zip(a, ts):
+        x.data, x.n, x.dtype = p, n, dt
+    return a
+
+
+GRADS = [(1 * MB, 1000, 0), (2 * MB, 0, 0), (3 * MB, 1000, 1)]     # 4000, 0 and 2000 bytes
+
+
+@pytest.mark.parametrize("kw", [
+    dict(norms=5 * MB), dict(norms=5 * MB - 8), dict(norms=5 * MB + 4),           # sumsq inside
+    dict(scratch=5 * MB), dict(scratch=5 * MB - 64), dict(scratch=6 * MB), dict(scratch=6 * MB + 8),
+    dict(scratch=1 * MB + 3992), dict(scratch=3 * MB - 8), dict(scratch=3 * MB + 1992),
+    dict(sumsq=1 * MB + 3992), dict(sumsq=3 * MB), dict(norms=1 * MB), dict(norms=3 * MB - 8),
+], ids=str)
+def test_norm_buffers_that_share_memory(L, kw):
+    at = dict(dict(sumsq=5 * MB, norms=6 * MB, scratch=7 * MB), **kw)
+    a = _list(*GRADS)
+    need = L.mpipe_op_grad_scratch_bytes(a, 3)
+    assert L.mpipe_op_grad_norm(a, 3, at["sumsq"], at["norms"], at["scratch"], need, None) == -1
+    assert "share" in B.last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(sumsq=1 * MB + 3992), dict(sumsq=3 * MB), dict(norm=1 * MB), dict(norm=3 * MB + 1996),
+    dict(norm=5 * MB), dict(norm=5 * MB + 4),
+    dict(out=True, sumsq=9 * MB), dict(out=True, norm=9 * MB + 3996), dict(out=True, norm=1 * MB),
+    dict(out=True, norm=11 * MB + 4),
+], ids=str)
+def test_clip_buffers_that_share_memory(L, kw):
+    at = dict(dict(sumsq=5 * MB, norm=6 * MB, out=False), **kw)
+    a, o = _list(*GRADS), _list(*[(p + 8 * MB, n, 0) for p, n, _ in GRADS])
+    assert L.mpipe_op_grad_clip(a, o if at["out"] else None, 3, at["sumsq"], 1.0, at["norm"], None) == -1
+    assert "share" in B.last_error()
