@@ -582,16 +582,19 @@ def _launch(fn, dev: int, stream, *args) -> None:
     if dev < 0:
         _bad("tensors must be on the GPU")
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
+        # the current stream's handle alone (0.1 us; a Stream object around it takes 1.1)
+        handle = torch._C._cuda_getCurrentRawStream(dev)
     elif stream.device_index != dev:
         _bad("a stream of another device than the tensors'")
+    else:
+        handle = stream.cuda_stream
     here = torch.cuda.current_device()
     if here == dev:
-        _check(fn(*args, stream.cuda_stream))
+        _check(fn(*args, handle))
         return
     torch.cuda.set_device(dev)
     try:
-        _check(fn(*args, stream.cuda_stream))
+        _check(fn(*args, handle))
     finally:
         torch.cuda.set_device(here)
 
@@ -760,23 +763,42 @@ def op_qk_norm_rope_bwd(cfg, dq, dk, q, k, q_gain, k_gain, eps: float, pos, dq_i
 
 class GradList:
     """The tensors of a gradient (fp32 or bf16, contiguous, one GPU) as the calls take them;
-    it keeps them alive.  Made once for buffers that stay, or for every call."""
+    it keeps them alive.  Made once for buffers that stay, or for every call.  A tensor whose
+    memory was replaced since (`.data`, `set_`, a growing `resize_`) is taken with its new one."""
 
     def __init__(self, tensors):
+        import torch
+        self.address = torch.Tensor.data_ptr
         self.tensors = list(tensors)
         self.n = len(self.tensors)
         self.array = (_GradTensor * max(self.n, 1))()
+        self._read()
+
+    def _read(self):
+        self.at = None      # read again by the next call if this one refuses a tensor
         self.dev = self.tensors[0].get_device() if self.n else None
+        at, keep = [], []
         for a, t in zip(self.array, self.tensors):
             if not t.is_contiguous():
                 _bad("gradients must be contiguous")
             if t.get_device() != self.dev:
                 _bad("tensors on different devices")
-            a.data, a.n, a.dtype = t.data_ptr(), t.numel(), _code(t.dtype)
+            p = t.data_ptr()
+            a.data, a.n, a.dtype = p, t.numel(), _code(t.dtype)
+            at.append(p)
+            keep.append(t.untyped_storage())
+        # with the memory itself kept, no other tensor can come to lie at a known address
+        self.at, self.keep = at, keep
+
+    def now(self) -> "GradList":
+        """The list with the tensors' present memory (1.2 us to see that 32 have not moved)."""
+        if list(map(self.address, self.tensors)) != self.at:
+            self._read()
+        return self
 
 
 def _grad_list(grads) -> GradList:
-    return grads if isinstance(grads, GradList) else GradList(grads)
+    return grads.now() if isinstance(grads, GradList) else GradList(grads)
 
 
 def op_grad_scratch_bytes(grads) -> int:

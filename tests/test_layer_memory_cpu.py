@@ -98,3 +98,27 @@ def test_clip_buffers_that_share_memory(L, kw):
     a, o = _list(*GRADS), _list(*[(p + 8 * MB, n, 0) for p, n, _ in GRADS])
     assert L.mpipe_op_grad_clip(a, o if at["out"] else None, 3, at["sumsq"], 1.0, at["norm"], None) == -1
     assert "share" in B.last_error()
+
+
+def test_grad_list_follows_its_tensors():
+    """A list made once takes the memory that its tensors have at the call, not the freed one."""
+    torch = pytest.importorskip("torch")
+    f = dict(dtype=torch.float32)
+    a, b = torch.zeros(1000, **f), torch.zeros(7, **f)
+    gl = mp.GradList([a, b])
+    small = mp.op_grad_scratch_bytes(gl)
+    for change in (lambda: setattr(a, "data", torch.zeros(400_000, **f)),
+                   lambda: a.set_(torch.zeros(300_000, **f)), lambda: a.resize_(500_000)):
+        change()
+        assert mp.op_grad_scratch_bytes(gl) == mp.op_grad_scratch_bytes([a, b]) > small
+        assert (gl.array[0].data, gl.array[0].n) == (a.data_ptr(), a.numel())
+        assert (gl.array[1].data, gl.array[1].n) == (b.data_ptr(), 7)
+    a.data = torch.zeros(9, dtype=torch.bfloat16)
+    assert mp.op_grad_scratch_bytes(gl) == small and gl.array[0].dtype == 1
+    a.data = torch.zeros(8, 8, **f).t()
+    for _ in range(2):                       # refused for as long as it is so
+        with pytest.raises(mp.MpipeError, match="contiguous"):
+            mp.op_grad_scratch_bytes(gl)
+    a.data = torch.zeros(5, **f)
+    mp.op_grad_scratch_bytes(gl)
+    assert (gl.array[0].data, gl.array[0].n, gl.array[0].dtype) == (a.data_ptr(), 5, 0)
