@@ -177,8 +177,8 @@ mpipe_status mpipe_op_rope_axes(int32_t dtype, const mpipe_rope_cfg* cfg, int64_
 
 /* The same behind a root-mean-square norm of every head, in one pass: n = g * x * r,
  * r = 1 / sqrt(mean of x^2 over head_dim + eps), then the rotation.  q_gain, k_gain:
- * [head_dim] in dtype.  Statistics and arithmetic in fp32 (|x| below 1e18, as squares are
- * summed), one rounding.  The backward needs q and k as they went in: in place only without it. */
+ * [head_dim] in dtype; eps finite, at least 2^-126.  Statistics and arithmetic in fp32 (|x| below
+ * 1e18, as squares are summed), one rounding.  The backward needs q and k as they went in: in place only without it. */
 mpipe_status mpipe_op_qk_norm_rope_fwd(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                        const mpipe_heads* q, const mpipe_heads* k,
                                        const void* q_gain, const void* k_gain, float eps,

@@ -30,6 +30,11 @@ mpipe_status guarded(F f) {
   }
 }
 
+// The reciprocal root takes no subnormal, and from 2^-126 on squares that underflow (below
+// 2^-150 each) stay under an fp32 step of the mean.
+bool eps_ok(float eps) { return eps >= 0x1p-126f && std::isfinite(eps); }
+constexpr const char* kBadEps = "eps must be finite and at least 2^-126";
+
 HeadView view_of(const mpipe_heads* h) {
   HeadView v;
   if (h) {
@@ -177,8 +182,7 @@ mpipe_status mpipe_op_qk_norm_rope_fwd(int32_t dtype, const mpipe_rope_cfg* cfg,
     const mpipe_heads* in[2] = {q, k};
     const mpipe_heads* out[2] = {q_out, k_out};
     const void* gain[2] = {q_gain, k_gain};
-    if (!(eps > 0.f) || !std::isfinite(eps))
-      return set_error(MPIPE_ERR_INVALID_ARG, "eps must be positive and finite");
+    if (!eps_ok(eps)) return set_error(MPIPE_ERR_INVALID_ARG, kBadEps);
     if (mpipe_status st = check_qk(p, dtype, cfg, rows, in, nullptr, out, gain, pos, ld_pos)) return st;
     p.norm = true;
     p.eps = eps;
@@ -208,8 +212,7 @@ mpipe_status mpipe_op_qk_norm_rope_bwd(int32_t dtype, const mpipe_rope_cfg* cfg,
     const mpipe_heads* grad[2] = {dq, dk};
     const mpipe_heads* out[2] = {dq_in, dk_in};
     const void* gain[2] = {q_gain, k_gain};
-    if (!(eps > 0.f) || !std::isfinite(eps))
-      return set_error(MPIPE_ERR_INVALID_ARG, "eps must be positive and finite");
+    if (!eps_ok(eps)) return set_error(MPIPE_ERR_INVALID_ARG, kBadEps);
     if (mpipe_status st = check_qk(p, dtype, cfg, rows, in, grad, out, gain, pos, ld_pos)) return st;
     if ((uintptr_t)grad_q_gain % 4 || (uintptr_t)grad_k_gain % 4)
       return set_error(MPIPE_ERR_INVALID_ARG, "gain gradients misaligned");

@@ -28,3 +28,31 @@ def test_grad_list_of_replaced_memory():
     mp.op_grad_clip(gl, sumsq, 0.5 * 2660 ** 0.5)
     # the factor 0.5 off by three fp64 roundings comes out as 0.5 in fp32
     assert bool((a == 0.5).all()) and bool((b == 1).all()) and bool((old == 3).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_at_the_smallest_eps(dtype):
+    """eps = 2^-126 on heads of zeros, of values whose squares are subnormal or nothing, and of
+    ordinary ones."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce(f"norm at the smallest eps {dtype}")
+    c, rows, d, eps = R.rope_cfg(64, [8, 4], rot=24), 6, 64, 2.0 ** -126
+    gen = torch.Generator().manual_seed(71)
+    p, pos = _pos(np.random.default_rng(7), 2, rows)
+    x, dy = _rand(gen, (rows, 2, d), dtype), _rand(gen, (rows, 2, d), dtype)
+    for r, scale in enumerate((0.0, 1e-24, 1e-20, 1e-19, 1e-10, 1.0)):
+        x[r] *= scale
+    g = 1 + 0.2 * _rand(gen, (d,), dtype)
+    y, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty(d, device=dev)
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, 2, 0, d), dtype=torch.uint8, device=dev)
+    mp.op_qk_norm_rope_fwd(_cfg(c), x, None, g, None, eps, pos, y, None)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dy, None, x, None, g, None, eps, pos, dx, None, dg, None, scratch,
+                           accumulate=False)
+    xn, gn = _np(x), _np(g)
+    r = 1.0 / np.sqrt((xn * xn).mean(-1, keepdims=True) + eps)
+    _close(y, R.norm_rope(c, xn, gn, eps, p), R.partners(c, xn * r * gn), 2.0 ** -19, dtype, "forward")
+    wx, wg, sx, sg = R.norm_rope_bwd(c, _np(dy), xn, gn, eps, p)
+    _close(dx, wx, sx, 2.0 ** -18, dtype, "dx")
+    _close(dg, wg, sg, 2.0 ** -19 + 12 * 2.0 ** -24, "f32", "dg")
+    assert bool((y[0] == 0).all())
