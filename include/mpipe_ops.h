@@ -228,13 +228,14 @@ mpipe_status mpipe_op_grad_norm(const mpipe_grad_tensor* grads, int32_t n, doubl
 /* 0 for a list that is refused. */
 size_t mpipe_op_grad_scratch_bytes(const mpipe_grad_tensor* grads, int32_t n);
 
-/* norm (device fp32 [1], nullable) = sqrt(sumsq); with f = max_norm / norm where norm >
- * max_norm and f = 1 elsewhere (a norm that is infinite or not a number included: the caller
- * sees it in norm), out[i] = grads[i] * f in out[i]'s dtype.  out == NULL or out[i].data ==
- * grads[i].data: in place, where f == 1 writes nothing.  Other outputs are apart from every
- * input and always written.  sumsq: device fp64 [1], as of this call's turn on the stream, apart
- * from every output; norm apart from sumsq and from every tensor.
- * max_norm >= 0 (infinity: never scales). */
+/* norm (device fp32 [1], nullable) = sqrt(sumsq); with f = max_norm / sqrt(sumsq) where the root
+ * is above max_norm and f = 1 elsewhere (a root that is infinite or not a number included: the
+ * caller sees it in norm), out[i] = grads[i] * f in out[i]'s dtype.  The root and f are fp64:
+ * where the root is finite but beyond fp32, so that norm is infinite, f still scales.
+ * out == NULL or out[i].data == grads[i].data: in place, where f == 1 writes nothing.  Other
+ * outputs are apart from every input and always written.  sumsq: device fp64 [1], as of this
+ * call's turn on the stream, apart from every output; norm apart from sumsq and from every
+ * tensor.  max_norm >= 0 (infinity: never scales). */
 mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad_tensor* out,
                                 int32_t n, const double* sumsq, double max_norm, float* norm,
                                 void* hip_stream);

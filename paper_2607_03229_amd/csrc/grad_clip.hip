@@ -252,13 +252,21 @@ __device__ __forceinline__ void chunk_scale(const A* p, B* o, int n, float f) {
   if (i < n) o[i] = (B)((float)p[i] * f);
 }
 
+// The same by a factor that fp32 holds as a subnormal, or as zero: one fp64 product, rounded
+// to fp32 once.  Such norms are beyond 1e35 times max_norm, so its time does not matter.
+template <class A, class B>
+__device__ __forceinline__ void chunk_scale_far(const A* p, B* o, int n, double f) {
+  for (int i = threadIdx.x; i < n; i += 256) o[i] = (B)(float)((double)(float)p[i] * f);
+}
+
 template <bool PAST>
 __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t chunk,
                                                    const double* sumsq, double max_norm,
                                                    float* norm) {
   const double len2 = sqrt(*sumsq);
   const bool scales = len2 > max_norm && len2 <= 1.7976931348623157e308;
-  const float f = scales ? (float)(max_norm / len2) : 1.f;
+  const double f64 = scales ? max_norm / len2 : 1.0;
+  const float f = (float)f64;
   // from the last chunk back: what the norm read last is cached still (1517 -> 1500 us)
   const int c = gridDim.x - 1 - blockIdx.x;
   if (norm && c == 0 && threadIdx.x == 0) *norm = (float)len2;
@@ -269,6 +277,13 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t ch
   if (x.p == out && !scales) return;
   const int64_t at = (c - a.first[t]) * chunk;
   const int m = (int)(x.n - at < chunk ? x.n - at : chunk);
+  if (f64 < 0x1p-126) {
+    if (x.in16 && x.out16) chunk_scale_far((const bf16*)x.p + at, (bf16*)out + at, m, f64);
+    else if (x.in16) chunk_scale_far((const bf16*)x.p + at, (float*)out + at, m, f64);
+    else if (x.out16) chunk_scale_far((const float*)x.p + at, (bf16*)out + at, m, f64);
+    else chunk_scale_far((const float*)x.p + at, (float*)out + at, m, f64);
+    return;
+  }
   if (x.in16 && x.out16) chunk_scale<PAST>((const bf16*)x.p + at, (bf16*)out + at, m, f);
   else if (x.in16) chunk_scale<PAST>((const bf16*)x.p + at, (float*)out + at, m, f);
   else if (x.out16) chunk_scale<PAST>((const float*)x.p + at, (bf16*)out + at, m, f);

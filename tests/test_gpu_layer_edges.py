@@ -56,3 +56,33 @@ def test_norm_at_the_smallest_eps(dtype):
     _close(dx, wx, sx, 2.0 ** -18, dtype, "dx")
     _close(dg, wg, sg, 2.0 ** -19 + 12 * 2.0 ** -24, "f32", "dg")
     assert bool((y[0] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+def test_clip_of_a_norm_far_above(dtype, out):
+    """Factors below fp32's normal range and below all of it: the scaled gradient keeps fp32's
+    precision (half a step of its product, half a step of a subnormal result)."""
+    torch, dev = torch_dev()
+    mp, gen = _mp(), torch.Generator().manual_seed(81)
+    announce(f"clip of a norm far above {dtype}->{out}")
+    for size, max_norm in ((1e38, 1.0), (1e38, 1e-3), (3e38, 1e-9), (3e38, 1e-30), (1e38, 1e-44)):
+        ts = [torch.full((n,), size, device=dev).to(_tdt(dtype)) * torch.sign(
+            torch.randn(n, generator=gen)).to(dev).to(_tdt(dtype)) for n in (1000, 77, 40001)]
+        ts[0][::3] = 1e-3                    # and small ones among them, which vanish
+        sumsq, _ = _norm_call(ts)
+        ref = [_np(t) for t in ts]
+        total = float(np.sqrt(sum((r * r).sum() for r in ref)))
+        os = [torch.full((t.numel(),), float("nan"), device=dev, dtype=_tdt(out)) for t in ts]
+        norm = torch.zeros(1, device=dev)
+        mp.op_grad_clip(ts, sumsq, max_norm, norm, out=os)
+        with np.errstate(over="ignore"):
+            assert float(norm) == float(np.float32(total))
+        f = max_norm / total
+        half = 2.0 ** -24 if out == "f32" else 2.0 ** -24 + 2.0 ** -8
+        step = 2.0 ** -150 if out == "f32" else 2.0 ** -134 + 2.0 ** -150    # of subnormals
+        for r, o in zip(ref, os):
+            # f is off by a few fp64 steps, the product by a rounding of its own
+            assert bool((np.abs(_np(o) - r * f) <= (half + 1e-12) * np.abs(r * f) + step).all()), max_norm
+        if dtype == out:
+            mp.op_grad_clip(ts, sumsq, max_norm)
+            assert all(torch.equal(a, b) for a, b in zip(ts, os))
