@@ -160,7 +160,8 @@ typedef struct {
  * column], strides in elements, aligned to one element; heads == 0: none (p may be null).
  * Inputs take any strides >= 0.  An output's elements must be distinct, and it may share
  * memory with an input only as the very same view of the same side (in place), or as other
- * columns of rows of one stride (q, k and v of one product); never with positions or gains. */
+ * columns of rows of one stride (q, k and v of one product, side by side or head by head); never
+ * with positions or gains. */
 typedef struct {
   void* p;
   int64_t row_stride, head_stride;

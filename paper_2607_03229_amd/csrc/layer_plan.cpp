@@ -189,20 +189,58 @@ bool same_view(const HeadView& a, const HeadView& b, int64_t rows) {
          (a.head == b.head || a.heads == 1);
 }
 
+namespace {
+// Whether x + c * step comes within (-d, d) for a whole c of [lo, hi].
+bool comes_near(int64_t x, int64_t step, int64_t lo, int64_t hi, int32_t d) {
+  // the last c that leaves it at or below zero, and the next
+  const int64_t last = step == 0 ? lo : x > 0 ? -((x - 1) / step) - 1 : -x / step;
+  for (int64_t c : {last, last + 1}) {
+    const int64_t y = x + std::max(lo, std::min(hi, c)) * step;
+    if (y > -d && y < d) return true;
+  }
+  return false;
+}
+}  // namespace
+
 bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, int esz) {
   if (a.heads == 0 || b.heads == 0 || rows == 0) return false;
+  if (b.heads > a.heads) return views_meet(b, a, rows, d, esz);
   int64_t na, nb;
   extent(a, rows, d, na);
   extent(b, rows, d, nb);
-  const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
-  if (pa + (uintptr_t)na * esz <= pb || pb + (uintptr_t)nb * esz <= pa) return false;
-  if (a.row != b.row || rows == 1) return true;
-  const int64_t r = a.row * esz;
-  const int64_t wa = ((a.heads - 1) * a.head + d) * esz, wb = ((b.heads - 1) * b.head + d) * esz;
-  if (r == 0 || wa > r || wb > r) return true;
-  int64_t off = (int64_t)(pb - pa) % r;
-  if (off < 0) off += r;
-  return !(off >= wa && off + wb <= r);
+  if (!ranges_meet(a.p, (size_t)na * esz, b.p, (size_t)nb * esz)) return false;
+  if (rows > 1 && a.row != b.row) return true;
+  const int64_t row = rows > 1 ? a.row : 0, head_a = a.heads > 1 ? a.head : 0,
+                head_b = b.heads > 1 ? b.head : head_a;
+  const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p) / esz;
+  const int64_t wa = (a.heads - 1) * head_a + d, wb = (b.heads - 1) * head_b + d;
+  const bool whole = row > 0 && wa <= row && wb <= row;   // a row holds each of them
+  const int64_t in_row = whole ? (off % row + row) % row : 0;
+  if (whole && in_row >= wa && in_row + wb <= row) return false;   // side by side
+  // Heads of one stride, too: the distances of two heads are off + i * row + j * head for all
+  // i and j between the rows' and the heads' differences.
+  if (head_a == head_b) {
+    if (a.heads + (int64_t)b.heads < 2 * rows) {
+      for (int64_t j = 1 - a.heads; j < b.heads; ++j)
+        if (comes_near(off + j * head_a, row, 1 - rows, rows - 1, d)) return true;
+    } else {
+      for (int64_t i = 1 - rows; i < rows; ++i)
+        if (comes_near(off + i * row, head_a, 1 - a.heads, b.heads - 1, d)) return true;
+    }
+    return false;
+  }
+  // Otherwise b's heads one by one against a's of the same row and, where a head runs on into
+  // the next, of that one; which rows come first and last is not looked at.
+  if (row > 0 && !whole) return true;
+  for (int64_t j = 0; j < b.heads; ++j) {
+    int64_t x = off + j * head_b;
+    if (row > 0) {
+      x = (x % row + row) % row;
+      if (comes_near(row - x, head_a, 0, a.heads - 1, d)) return true;
+    }
+    if (comes_near(-x, head_a, 0, a.heads - 1, d)) return true;
+  }
+  return false;
 }
 
 bool ranges_meet(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {

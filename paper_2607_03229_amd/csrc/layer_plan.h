@@ -51,8 +51,8 @@ struct HeadView {
 bool view_ok(const HeadView& v, int64_t rows, int32_t d, int esz, bool written, std::string& why);
 // the same elements (a stride over one row or head does not count)
 bool same_view(const HeadView& a, const HeadView& b, int64_t rows);
-// Whether two (valid) views may share an element: not if their ranges are apart, or if they
-// are apart inside rows of one stride.
+// Whether two (valid) views may share an element: exactly where their rows and their heads have
+// one stride each, or their rows and a row holds either; else not if their ranges are apart.
 bool views_meet(const HeadView& a, const HeadView& b, int64_t rows, int32_t d, int esz);
 // Whether two ranges of bytes share one, and whether a range shares one with an element of a
 // (valid) view.

@@ -65,10 +65,57 @@ void check_ranges() {
   expect(!range_meets((const void*)4112, 4, v, 1, 8, 2), "behind one head of one row", 0);
 }
 
+// Views of one product in any order of rows, heads and q | k | v: exactly; any others: never
+// apart where they meet.
+void check_views() {
+  int said_apart = 0, meet = 0, close = 0;
+  for (int k = 0; k < 40000; ++k) {
+    const int d = 8, esz = 2, rows = uniform(1, 6);
+    const bool one_row = uniform(0, 3) > 0, one_head = uniform(0, 3) > 0;
+    HeadView v[2];
+    for (int z = 0; z < 2; ++z) {
+      v[z].heads = uniform(1, 4);
+      v[z].row = z && one_row ? v[0].row : uniform(0, 1) ? 8 * uniform(1, 20) : uniform(0, 120);
+      v[z].head = z && one_head ? v[0].head : uniform(0, 1) ? 8 * uniform(1, 20) : uniform(0, 120);
+      v[z].p = (const void*)(uintptr_t)(4096 + (uniform(0, 1) ? 16 * uniform(0, 20) : 2 * uniform(0, 160)));
+    }
+    const std::set<uintptr_t> a = elements(v[0], rows, d, esz), b = elements(v[1], rows, d, esz);
+    bool share = false;
+    for (uintptr_t e : a) share |= b.count(e) > 0;
+    const bool said = views_meet(v[0], v[1], rows, d, esz);
+    expect(said == views_meet(v[1], v[0], rows, d, esz), "either way round", k);
+    expect(said || !share, "views that meet", k);
+    const bool row = rows == 1 || v[0].row == v[1].row,
+               head = v[0].heads == 1 || v[1].heads == 1 || v[0].head == v[1].head;
+    if (row && head) expect(said == share, "views of one product", k);
+    said_apart += !said;
+    meet += share;
+    close += !said && *a.begin() < *b.rbegin() && *b.begin() < *a.rbegin();
+  }
+  std::printf("%d of 40000 pairs meet, %d said apart, %d of them within each other\n", meet, said_apart, close);
+  expect(meet > 4000 && said_apart > 4000 && close > 1000, "every kind of views", 0);
+  // [rows][heads][q | k | v][d], and [heads][rows][q | k | v][d]
+  for (int order = 0; order < 2; ++order)
+    for (int z = 0; z < 9; ++z) {
+      const HeadView a = {(const void*)(uintptr_t)(4096 + 256 * (z / 3)), order ? 384 : 32 * 384,
+                          order ? 1000 * 384 : 384, 32},
+                     b = {(const void*)(uintptr_t)(4096 + 256 * (z % 3)), a.row, a.head, 32};
+      expect(views_meet(a, b, 1000, 128, 2) == (z / 3 == z % 3), "q, k and v head by head", z);
+    }
+  // q, k, q, v of groups of two heads: strides of 2 d and 4 d; k reaches into a row's last q
+  const HeadView q = {(const void*)4096, 2048, 256, 8}, k = {(const void*)(4096 + 256), 2048, 512, 4},
+                 over = {(const void*)(4096 + 260), 2048, 512, 4};
+  expect(!views_meet(q, k, 100, 128, 2) && views_meet(q, over, 100, 128, 2), "groups", 0);
+  // strides over one row or one head may be anything
+  HeadView w = {(const void*)4096, INT64_MAX, INT64_MAX, 1};
+  expect(views_meet(w, w, 1, 8, 2), "one head of one row", 0);
+}
+
 }  // namespace
 
 int main() {
   check_ranges();
+  check_views();
   if (failures) return 1;
   std::puts("memory checks passed");
   return 0;

@@ -86,3 +86,43 @@ def test_clip_of_a_norm_far_above(dtype, out):
         if dtype == out:
             mp.op_grad_clip(ts, sumsq, max_norm)
             assert all(torch.equal(a, b) for a, b in zip(ts, os))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("order", ["rows", "heads"])
+def test_q_k_v_head_by_head(order, dtype):
+    """[rows][heads][q | k | v][d] and [heads][rows][q | k | v][d], in place: the bits of dense
+    tensors, and v as it was."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce(f"q, k, v head by head, {order} first, {dtype}")
+    c, rows, heads, d = R.rope_cfg(64, [4, 6, 6], rot=32, pairing=1), 75, 5, 64
+    cfg, gen = _cfg(c), torch.Generator().manual_seed(91)
+    _, pos = _pos(np.random.default_rng(9), 3, rows)
+    g = [1 + 0.2 * _rand(gen, (d,), dtype) for _ in range(2)]
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, heads, heads, d), dtype=torch.uint8, device=dev)
+
+    def product():
+        x = _rand(gen, (rows, heads, 3, d) if order == "rows" else (heads, rows, 3, d), dtype)
+        v = x if order == "rows" else x.transpose(0, 1)
+        return x, v[:, :, 0], v[:, :, 1], v[:, :, 2]
+
+    def like(t):
+        return torch.full(t.shape, float("nan"), dtype=t.dtype, device=dev)
+
+    for f in (lambda q, k, qo, ko: mp.op_rope_axes(cfg, q, k, pos, qo, ko),
+              lambda q, k, qo, ko: mp.op_qk_norm_rope_fwd(cfg, q, k, *g, 1e-6, pos, qo, ko)):
+        x, q, k, v = product()
+        want, keep = [like(q), like(k)], v.clone()
+        f(q.contiguous(), k.contiguous(), *want)
+        f(q, k, q, k)
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(v, keep)
+    _, q, k, _ = product()
+    _, dq, dk, dv = product()
+    want, keep = [like(q), like(k)], dv.clone()
+    gw, gg = ([torch.zeros(d, device=dev) for _ in range(2)] for _ in range(2))
+    mp.op_qk_norm_rope_bwd(cfg, dq.contiguous(), dk.contiguous(), q.contiguous(), k.contiguous(), *g, 1e-6,
+                           pos, *want, *gw, scratch)
+    mp.op_qk_norm_rope_bwd(cfg, dq, dk, q, k, *g, 1e-6, pos, dq, dk, *gg, scratch)
+    assert torch.equal(dq, want[0]) and torch.equal(dk, want[1]) and torch.equal(dv, keep)
+    assert torch.equal(gg[0], gw[0]) and torch.equal(gg[1], gw[1])
