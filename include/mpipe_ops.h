@@ -169,7 +169,8 @@ typedef struct {
 } mpipe_heads;
 
 /* q_out, k_out = q, k turned by the positions pos[axis * ld_pos + row] (device int32, any
- * values); inverse != 0 turns back, which is the gradient.  Angles keep their phase at any
+ * values; ld_pos at least rows, or 0: one row of positions for all axes, as text has them);
+ * inverse != 0 turns back, which is the gradient.  Angles keep their phase at any
  * position (whole-number products modulo one turn); arithmetic in fp32, one rounding. */
 mpipe_status mpipe_op_rope_axes(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                 const mpipe_heads* q, const mpipe_heads* k, const int32_t* pos,

@@ -713,8 +713,8 @@ def _code(dtype) -> int:
 
 def op_rope_axes(cfg, q, k, pos, q_out, k_out, inverse: bool = False, stream=None) -> None:
     """q_out, k_out = q, k ([rows][heads][head_dim], any strides of rows and heads; k and
-    k_out may be None) turned by pos (int32 [axes][rows]); inverse turns back (the gradient).
-    An output may be its own input."""
+    k_out may be None) turned by pos (int32 [axes][rows], or one row of positions expanded to
+    all axes); inverse turns back (the gradient).  An output may be its own input."""
     dtype, rows, dev, (q, qo), (k, ko) = _qk(cfg, pos, q, k, (q_out,), (k_out,))
     _launch(load().mpipe_op_rope_axes, dev, stream, _code(dtype), C.byref(cfg), rows, q, k,
             pos.data_ptr(), pos.stride(0), 1 if inverse else 0, qo, ko)

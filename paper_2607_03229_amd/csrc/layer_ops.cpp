@@ -84,8 +84,8 @@ mpipe_status check_qk(QkProblem& p, int32_t dtype, const mpipe_rope_cfg* cfg, in
   }
   if (!any) return MPIPE_OK;
   if (!pos || (uintptr_t)pos % 4) return set_error(MPIPE_ERR_INVALID_ARG, "null or misaligned positions");
-  if (cfg->axes > 1 && (ld_pos < rows || ld_pos > (int64_t(1) << 40)))
-    return set_error(MPIPE_ERR_INVALID_ARG, "ld_pos must be at least rows");
+  if (cfg->axes > 1 && ld_pos != 0 && (ld_pos < rows || ld_pos > (int64_t(1) << 40)))
+    return set_error(MPIPE_ERR_INVALID_ARG, "ld_pos must be at least rows, or 0");
   // an output meets an input only in place, on its own side, and never another output
   for (int z = 0; z < 2; ++z) {
     const HeadView& y = p.side[z].y;

@@ -126,3 +126,30 @@ def test_q_k_v_head_by_head(order, dtype):
     mp.op_qk_norm_rope_bwd(cfg, dq, dk, q, k, *g, 1e-6, pos, dq, dk, *gg, scratch)
     assert torch.equal(dq, want[0]) and torch.equal(dk, want[1]) and torch.equal(dv, keep)
     assert torch.equal(gg[0], gw[0]) and torch.equal(gg[1], gw[1])
+
+
+@pytest.mark.parametrize("rows", [1, 2, 130])
+def test_one_row_of_positions_for_all_axes(rows):
+    """Positions of text: one row of them expanded to every axis, the bits of its copies."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce(f"one row of positions, {rows} rows")
+    c, d = R.rope_cfg(128, [16, 24, 24], theta=1e6), 128
+    cfg, gen = _cfg(c), torch.Generator().manual_seed(95)
+    p, one = _pos(np.random.default_rng(9), 1, rows)
+    copies, one = one.repeat(3, 1), one.expand(3, rows)
+    assert one.stride(0) == 0
+    q, k = _rand(gen, (rows, 6, d), "bf16"), _rand(gen, (rows, 2, d), "bf16")
+    g = [_rand(gen, (d,), "bf16") for _ in range(2)]
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, 6, 2, d), dtype=torch.uint8, device=dev)
+    got, want = [], []
+    for out, pos in ((want, copies), (got, one)):
+        o = [torch.empty_like(t) for t in (q, k) * 3] + [torch.empty(d, device=dev) for _ in range(2)]
+        mp.op_rope_axes(cfg, q, k, pos, o[0], o[1])
+        mp.op_qk_norm_rope_fwd(cfg, q, k, *g, 1e-6, pos, o[2], o[3])
+        mp.op_qk_norm_rope_bwd(cfg, q, k, q, k, *g, 1e-6, pos, o[4], o[5], o[6], o[7], scratch, accumulate=False)
+        out += o
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    _close(got[0], R.rotate(c, _np(q), np.repeat(p, 3, 0)), R.partners(c, _np(q)), 2.0 ** -22, "bf16", rows)
+    with pytest.raises(mp.MpipeError):          # written positions have a row for every axis
+        mp.op_seam_positions([0], [rows], [], [], one)
