@@ -153,3 +153,140 @@ def test_one_row_of_positions_for_all_axes(rows):
     _close(got[0], R.rotate(c, _np(q), np.repeat(p, 3, 0)), R.partners(c, _np(q)), 2.0 ** -22, "bf16", rows)
     with pytest.raises(mp.MpipeError):          # written positions have a row for every axis
         mp.op_seam_positions([0], [rows], [], [], one)
+
+
+# ---- the last lane of a head half filled ---------------------------------------------------------
+
+# bf16 vectors of eight columns with an odd number of them behind the turned ones
+HALF_FILLED = {
+    "d40": R.rope_cfg(40, [4, 2, 2], rot=16),
+    "d72_adjacent": R.rope_cfg(72, [8, 8], rot=32, pairing=1),
+    "d104_interleaved": R.rope_cfg(104, [8, 8, 8], rot=48, order=1),
+    "d248_adjacent": R.rope_cfg(248, [20, 50, 50], rot=240, pairing=1),
+}
+
+
+@pytest.mark.parametrize("layout", ["fused", "shifted"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", HALF_FILLED)
+def test_half_filled_last_lane(name, dtype, layout):
+    """Rotation both ways, norm and backward, out of place and in place: no column twice in the
+    sums, none written twice with another value, none left out."""
+    torch, dev = torch_dev()
+    mp, c = _mp(), HALF_FILLED[name]
+    cfg, d, axes, eps = _cfg(c), c["head_dim"], len(c["sections"]), float(np.float32(1e-6))
+    rng, gen = np.random.default_rng(15), torch.Generator().manual_seed(16)
+    for rows, hq, hk in ((1, 1, 1), (37, 7, 3), (130, 28, 4)):
+        announce(f"half filled last lane {name} {dtype} {layout} rows={rows} heads={hq}+{hk}")
+        p, pos = _pos(rng, axes, rows)
+        x, dy = ([_filled(gen, (rows, h, d), dtype, layout)[0] for h in (hq, hk)] for _ in range(2))
+        g = [1 + 0.2 * _rand(gen, (d,), dtype) for _ in range(2)]
+        gg = [torch.full((d,), float("nan"), device=dev) for _ in range(2)]
+        sc = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, hq, hk, d), dtype=torch.uint8, device=dev)
+        new = lambda: [_view(t.shape, dtype, layout) for t in x]
+        turned, back, normed, dx = new(), new(), new(), new()
+        v = lambda o: (o[0][0], o[1][0])
+        mp.op_rope_axes(cfg, *x, pos, *v(turned))
+        mp.op_rope_axes(cfg, *x, pos, *v(back), inverse=True)
+        mp.op_qk_norm_rope_fwd(cfg, *x, *g, 1e-6, pos, *v(normed))
+        mp.op_qk_norm_rope_bwd(cfg, *dy, *x, *g, 1e-6, pos, *v(dx), *gg, sc, accumulate=False)
+        for z in range(2):
+            xn, gn = _np(x[z]), _np(g[z])
+            r = 1.0 / np.sqrt((xn * xn).mean(-1, keepdims=True) + eps)
+            for o, inverse in ((turned, False), (back, True)):
+                _close(o[z][0], R.rotate(c, xn, p, inverse), R.partners(c, xn), 2.0 ** -22, dtype, inverse)
+            _close(normed[z][0], R.norm_rope(c, xn, gn, eps, p), R.partners(c, xn * r * gn), 2.0 ** -19,
+                   dtype, "norm")
+            wx, wg, sx, sg = R.norm_rope_bwd(c, _np(dy[z]), xn, gn, eps, p)
+            _close(dx[z][0], wx, sx, 2.0 ** -18, dtype, "dx")
+            n = min(rows * x[z].shape[1], 1200)
+            _close(gg[z], wg, sg, 2.0 ** -19 + n * 2.0 ** -24, "f32", "dg")
+            assert all(_untouched(*o[z]) for o in (turned, back, normed, dx))
+        mp.op_qk_norm_rope_bwd(cfg, *dy, *x, *g, 1e-6, pos, *dy, None, None, sc)
+        mp.op_qk_norm_rope_fwd(cfg, *x, *g, 1e-6, pos, *x)
+        assert all(torch.equal(a, b[0]) for a, b in zip(x + dy, normed + dx))
+
+
+# ---- the gains' gradient over large grids ----------------------------------------------------------
+
+GAIN_CASES = [
+    ("bf16", 33000, 28, 4, R.rope_cfg(128, [16, 24, 24], theta=1e6)),
+    ("bf16", 60000, 28, 0, R.rope_cfg(128, [64])),
+    ("f32", 17000, 28, 4, R.rope_cfg(128, [24, 20, 20], theta=1e6, order=1)),
+    ("bf16", 90000, 1, 1, R.rope_cfg(128, [64])),              # eight angles a lane
+    ("bf16", 120001, 2, 1, R.rope_cfg(64, [4, 6, 6], rot=32, pairing=1)),
+    ("f32", 300007, 1, 2, R.rope_cfg(8, [4])),
+    ("bf16", 20003, 9, 9, R.rope_cfg(256, [30, 45, 45], rot=240, pairing=1)),
+    ("bf16", 9001, 65, 3, R.rope_cfg(16, [2, 2], rot=8)),
+]
+
+
+@pytest.mark.parametrize("case", GAIN_CASES, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}-{c[3]}-{c[4]['head_dim']}")
+def test_gain_gradient_counts_every_head_once(case):
+    """Values of +-1 have a root-mean-square of 1, and at position 0 nothing turns: every term is
+    a small whole number and every partial sum is exact (below 2^24), whatever the order.  One
+    term lost or taken twice shows.  1 + eps is 1 in fp32."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    dtype, rows, hq, hk, c = case
+    d, axes = c["head_dim"], len(c["sections"])
+    announce(f"gains of {rows} rows, {hq}+{hk} heads of {d} {dtype}")
+    gen = torch.Generator(device=dev).manual_seed(rows)
+
+    def heads(h):
+        if h == 0:
+            return None, None
+        x = torch.randint(0, 2, (rows, h, d), device=dev, generator=gen) * 2 - 1
+        dy = torch.randint(1, 4, (rows, h, d), device=dev, generator=gen)
+        dy *= torch.randint(0, 2, (rows, h, d), device=dev, generator=gen) * 2 - 1
+        return x.to(_tdt(dtype)), dy.to(_tdt(dtype))
+
+    (q, dq), (k, dk) = heads(hq), heads(hk)
+    pos = torch.zeros((axes, rows), dtype=torch.int32, device=dev)
+    g = [None if t is None else torch.ones(d, dtype=_tdt(dtype), device=dev) for t in (q, k)]
+    base = [None if t is None else torch.randint(-99, 99, (d,), device=dev, generator=gen).float()
+            for t in (q, k)]
+    grad = [None if b is None else b.clone() for b in base]
+    out = [None if t is None else torch.empty_like(t) for t in (q, k)]
+    need = mp.op_qk_norm_rope_scratch_bytes(rows, hq, hk, d)
+    scratch = torch.full((need // 4,), float("nan"), device=dev)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dq, dk, q, k, *g, 1e-12, pos, *out, *grad, scratch)
+    for x, dy, b, got in zip((q, k), (dq, dk), base, grad):
+        if x is not None:
+            assert torch.equal(got.double(), b.double() + (x.double() * dy.double()).sum((0, 1)))
+    if hk == 0:       # the largest grid: one side with more blocks than are resident at once
+        assert int((~scratch.isnan()).sum()) // d > 768
+
+
+@pytest.mark.parametrize("case", [GAIN_CASES[0], GAIN_CASES[2]],
+                         ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}-{c[3]}-{c[4]['head_dim']}")
+def test_gain_gradient_of_many_rows(case):
+    """Ordinary values against float64 sums.  A wave takes at most 28 steps of heads here (1,280
+    and 1,228 blocks of four waves for q), then 3 additions join its lanes, 2 its block's waves,
+    12 a lane's blocks and 7 the lanes: no chain of more than 64.  A term is off by 2^-19 of its
+    size.  Each side's bound is of its own sum of sizes."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    dtype, rows, hq, hk, c = case
+    d, axes, half = c["head_dim"], len(c["sections"]), c["rot_dim"] // 2
+    announce(f"gains of {rows} rows against float64, {hq}+{hk} heads of {d} {dtype}")
+    gen = torch.Generator(device=dev).manual_seed(rows)
+    p, pos = _pos(np.random.default_rng(rows), axes, rows)
+    rand = lambda *s: torch.randn(s, device=dev, generator=gen).to(_tdt(dtype))
+    x, dy = [rand(rows, h, d) for h in (hq, hk)], [rand(rows, h, d) for h in (hq, hk)]
+    g, grad = [rand(d) for _ in range(2)], [torch.empty(d, device=dev) for _ in range(2)]
+    out = [torch.empty_like(t) for t in x]
+    scratch = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, hq, hk, d), dtype=torch.uint8, device=dev)
+    mp.op_qk_norm_rope_bwd(_cfg(c), *dy, *x, *g, 1e-6, pos, *out, *grad, scratch, accumulate=False)
+    ang = torch.from_numpy(R.angles(c, p)).to(dev)[:, None]
+    cos, sin = ang.cos(), ang.sin()
+    for z in range(2):
+        v, u = x[z].double(), dy[z].double()
+        a, b = u[..., :half].clone(), u[..., half:].clone()      # whole heads in halves
+        u[..., :half], u[..., half:] = a * cos + b * sin, b * cos - a * sin
+        size = a.abs() + b.abs()
+        v *= torch.rsqrt(v.square().mean(-1, keepdim=True) + 1e-6)
+        want = (u * v).sum((0, 1))
+        sizes = (torch.cat([size, size], -1) * v.abs()).sum((0, 1))
+        err = (grad[z].double() - want).abs()
+        assert bool((err <= (2.0 ** -19 + 64 * 2.0 ** -24) * sizes).all()), float((err / sizes).max())
