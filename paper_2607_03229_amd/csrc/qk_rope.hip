@@ -445,12 +445,12 @@ __global__ __launch_bounds__(256, KP == 2 ? 3 : 2) void qk_bwd_kernel(QkArgs a) 
         const float k = inv_rms(head_sum(ss, w.log_c), a.inv_d, a.eps);
         const float m = k * k * head_sum(gs, w.log_c) * a.inv_d;
         const int drs = w.past_rows(now.rg), dhs = w.past_heads(now.h);
-        const float kd = drs + dhs > 0 || w.at.extra ? 0.f : k;   // repeats add nothing
+        if (drs + dhs == 0) {   // repeats add nothing (nor 0 times an infinity)
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-          dg[e] = fmaf(u[e], v[e] * kd, dg[e]);
-          u[e] = k * fmaf(u[e], g[e], -v[e] * m);
+          for (int e = 0; e < 2 * V; ++e) dg[e] = fmaf(u[e], v[e] * k, dg[e]);
         }
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) u[e] = k * fmaf(u[e], g[e], -v[e] * m);
         const T* at[2];
         y.at(w.row0(now.rg), now.h, drs, dhs, w.edge(now), at);
         store_head<T, V, PAST>(at, u);

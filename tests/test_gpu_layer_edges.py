@@ -290,3 +290,28 @@ def test_gain_gradient_of_many_rows(case):
         sizes = (torch.cat([size, size], -1) * v.abs()).sum((0, 1))
         err = (grad[z].double() - want).abs()
         assert bool((err <= (2.0 ** -19 + 64 * 2.0 ** -24) * sizes).all()), float((err / sizes).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,heads", [(1, 1), (3, 1), (5, 3), (67, 5)])
+def test_an_infinite_output_gradient(rows, heads, dtype):
+    """An infinity in the last row's last head of dy makes its pair's two columns of the gains'
+    gradient infinite, of the formula's signs, and no other column anything but finite."""
+    torch, dev = torch_dev()
+    mp = _mp()
+    announce(f"infinite output gradient {rows} rows {heads} heads {dtype}")
+    c, d, eps = R.rope_cfg(128, [16, 24, 24], theta=1e6), 128, float(np.float32(1e-6))
+    p, pos = _pos(np.random.default_rng(3), 3, rows)
+    gen = torch.Generator().manual_seed(33)
+    x, dy = _rand(gen, (rows, heads, d), dtype), _rand(gen, (rows, heads, d), dtype)
+    dy[-1, -1, 5] = float("inf")
+    g, dx, dg = torch.ones(d, device=dev, dtype=_tdt(dtype)), torch.empty_like(x), torch.empty(d, device=dev)
+    sc = torch.empty(mp.op_qk_norm_rope_scratch_bytes(rows, heads, 0, d), dtype=torch.uint8, device=dev)
+    mp.op_qk_norm_rope_bwd(_cfg(c), dy, None, x, None, g, None, 1e-6, pos, dx, None, dg, None, sc,
+                           accumulate=False)
+    with np.errstate(invalid="ignore"):
+        _, want, _, _ = R.norm_rope_bwd(c, _np(dy), _np(x), _np(g), eps, p)
+    assert sorted(np.flatnonzero(~np.isfinite(want)).tolist()) == [5, 69] and np.isinf(want[[5, 69]]).all()
+    got = _np(dg)
+    assert got[5] == want[5] and got[69] == want[69]
+    assert np.isfinite(np.delete(got, [5, 69])).all()
