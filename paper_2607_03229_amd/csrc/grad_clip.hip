@@ -7,8 +7,8 @@
 // order, so the result has the same bits every time.  fp64, because an fp32 square overflows at
 // 1.8e19 and a sum of 10^8 of them needs more than 24 bits; it costs nothing.
 //
-// Bound by HBM: MI355X, 675.8 M fp32 elements in 392 tensors: norm 441 us (6.1 TB/s), clip into
-// other buffers 1013 us (5.3); 30 tensors of 0.9 M bf16 elements 12 us in three launches.
+// Bound by HBM: MI355X, 675.8 M fp32 elements in 392 tensors: norm 440 us (6.1 TB/s), clip into
+// other buffers 1009 us (5.4); 32 tensors of 0.9 M bf16 elements 12 us in three launches.
 #include <algorithm>
 
 #include "common.h"

@@ -3,8 +3,8 @@
 // The host cuts the rows into spans of text and items (layer_plan.cpp) and passes them in the
 // kernel's arguments, kSpans at a time: no upload, no wait, and the launch can be captured.  A
 // thread finds its row's span by halving a copy of the spans' first rows in LDS and writes
-// three words; 12 bytes a row, so the launch itself is what a call costs (2.3 us for 32 rows,
-// 7.5 us in two launches for 262144 rows and their items).
+// three words; 12 bytes a row, so the launch itself is what a call costs (2.4 us for 32 rows,
+// 7.9 us in two launches for 262144 rows and their items).
 #include <algorithm>
 
 #include "layer_kernels.h"

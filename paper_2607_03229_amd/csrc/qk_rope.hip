@@ -553,9 +553,10 @@ int min_slots_log2(const QkArgs& a) {
   while ((2 << (a.log_c + h)) < a.half) ++h;
   return h;
 }
-// The sides of a launch.  Blocks: as many as are resident at once (`resident`: four waves a
-// SIMD forward, three backward), or `many` where each of their waves would take `long_walk`
-// steps and more.  Each side's share of them is its share of the steps, a row's angles
+// The sides of a launch.  Blocks: `resident`, what the bf16 kernels of eight columns a vector and
+// two angles a lane hold at once (four waves a SIMD forward, three backward; of the others fp32
+// holds 6 and 4, eight angles a lane 2 to 4), or `many` where each of their waves would take
+// `long_walk` steps and more.  Each side's share of them is its share of the steps, a row's angles
 // counted as another.  Returns the position loads of a step (2 or 8).
 int divide(QkArgs& a, int resident, int many, int long_walk) {
   const int min_log_h = min_slots_log2(a);
