@@ -170,8 +170,8 @@ typedef struct {
 
 /* q_out, k_out = q, k turned by the positions pos[axis * ld_pos + row] (device int32, any
  * values; ld_pos at least rows, or 0: one row of positions for all axes, as text has them);
- * inverse != 0 turns back, which is the gradient.  Angles keep their phase at any
- * position (whole-number products modulo one turn); arithmetic in fp32, one rounding. */
+ * inverse != 0 turns back, which is the gradient.  Angles keep their phase at any position
+ * (whole-number products modulo one turn); arithmetic in fp32, one rounding. */
 mpipe_status mpipe_op_rope_axes(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                 const mpipe_heads* q, const mpipe_heads* k, const int32_t* pos,
                                 int64_t ld_pos, int32_t inverse, const mpipe_heads* q_out,
@@ -180,7 +180,8 @@ mpipe_status mpipe_op_rope_axes(int32_t dtype, const mpipe_rope_cfg* cfg, int64_
 /* The same behind a root-mean-square norm of every head, in one pass: n = g * x * r,
  * r = 1 / sqrt(mean of x^2 over head_dim + eps), then the rotation.  q_gain, k_gain:
  * [head_dim] in dtype; eps finite, at least 2^-126.  Statistics and arithmetic in fp32 (|x| below
- * 1e18, as squares are summed), one rounding.  The backward needs q and k as they went in: in place only without it. */
+ * 1e18, as squares are summed), one rounding.  The backward needs q and k as they went in: in
+ * place only without it. */
 mpipe_status mpipe_op_qk_norm_rope_fwd(int32_t dtype, const mpipe_rope_cfg* cfg, int64_t rows,
                                        const mpipe_heads* q, const mpipe_heads* k,
                                        const void* q_gain, const void* k_gain, float eps,

@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256) void clip_kernel(ClipArgs a, int n, int64_t ch
   if (x.p == out && !scales) return;
   const int64_t at = (c - a.first[t]) * chunk;
   const int m = (int)(x.n - at < chunk ? x.n - at : chunk);
-  if (f64 < 0x1p-126) {
+  if (f64 > 0.0 && f64 < 0x1p-126) {
     if (x.in16 && x.out16) chunk_scale_far((const bf16*)x.p + at, (bf16*)out + at, m, f64);
     else if (x.in16) chunk_scale_far((const bf16*)x.p + at, (float*)out + at, m, f64);
     else if (x.out16) chunk_scale_far((const float*)x.p + at, (bf16*)out + at, m, f64);

@@ -65,7 +65,8 @@ def test_clip_of_a_norm_far_above(dtype, out):
     torch, dev = torch_dev()
     mp, gen = _mp(), torch.Generator().manual_seed(81)
     announce(f"clip of a norm far above {dtype}->{out}")
-    for size, max_norm in ((1e38, 1.0), (1e38, 1e-3), (3e38, 1e-9), (3e38, 1e-30), (1e38, 1e-44)):
+    for size, max_norm in ((1e38, 1.0), (1e38, 1e-3), (3e38, 1e-9), (3e38, 1e-30), (1e38, 1e-37), (1e38, 1e-44),
+                           (1e38, 0.0)):
         ts = [torch.full((n,), size, device=dev).to(_tdt(dtype)) * torch.sign(
             torch.randn(n, generator=gen)).to(dev).to(_tdt(dtype)) for n in (1000, 77, 40001)]
         ts[0][::3] = 1e-3                    # and small ones among them, which vanish
