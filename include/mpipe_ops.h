@@ -243,6 +243,116 @@ mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad
                                 int32_t n, const double* sumsq, double max_norm, float* norm,
                                 void* hip_stream);
 
+/* ---- The first LLM layer's attention ----------------------------------------------------
+ * As above: no call synchronizes, allocates or keeps anything, and each can be captured into a
+ * graph (host arguments stay as captured; device tables, positions and lengths are read anew).
+ * The current device has to be that of the stream and the buffers; calls that overlap need
+ * results and scratch of their own.
+ *
+ * Causal attention over sequences, grouped heads.  q, o, d_o, dq: [rows_q][heads of q][head_dim];
+ * k, v, dk, dv: [rows_k][heads of k][head_dim]; the heads of q are a multiple of those of k, and
+ * query head h reads key head h / (their quotient).  head_dim: a multiple of 8 of at most 256.
+ *   seq_row, seq_len  host [n_seq]: sequence s's queries are the rows seq_row[s] .. + seq_len[s]
+ *                     of rows_q (padded batches leave gaps; an empty one is allowed; any order;
+ *                     none may overlap).
+ *   key_row, key_len  host [n_seq], both or neither: its keys are the rows key_row[s] .. +
+ *                     key_len[s] of rows_k; null: the queries' rows.  They end together: query i
+ *                     of a sequence sees its keys 0 .. i + key_len - seq_len, so that more keys
+ *                     than queries are a prefix, and with fewer the first queries see none.
+ *                     Sequences may share keys in the forward only.
+ * o = softmax(scale q k^T) v over the keys a query sees, lse[head * ld_lse + row] = the natural
+ * logarithm of the sum of exp(scale q k) (fp32, nullable in the forward; ld_lse at least rows_q).
+ * A query that sees no key gets o = 0 and lse = -infinity, and gradients of 0.  A key that a
+ * query does not see does not count for it, whatever its values.  Rows of no sequence keep what
+ * they held in every output.  Scores, statistics and sums are fp32; in bf16 the weights and the
+ * score gradients are rounded to bf16 (half a step of 2^-8 each) before their products.  The
+ * same call gives the same bits.  Outputs are apart from every other buffer but each other's
+ * columns of one product, side by side. */
+mpipe_status mpipe_op_causal_attention_fwd(int32_t dtype, int32_t head_dim, int64_t rows_q,
+                                           int64_t rows_k, const mpipe_heads* q,
+                                           const mpipe_heads* k, const mpipe_heads* v,
+                                           const int64_t* seq_row, const int64_t* seq_len,
+                                           const int64_t* key_row, const int64_t* key_len,
+                                           int32_t n_seq, float scale, const mpipe_heads* o,
+                                           float* lse, int64_t ld_lse, void* hip_stream);
+
+/* Its backward: dq, dk, dv overwritten (a key that no query sees gets 0) from d_o, the gradient
+ * of o, and the forward's inputs, o and lse.  lse itself has no gradient here.  The gradients of a
+ * key head are summed over the query heads of its group, in a fixed order.  scratch:
+ * mpipe_op_causal_attention_scratch_bytes, aligned to 16 bytes, not kept. */
+mpipe_status mpipe_op_causal_attention_bwd(int32_t dtype, int32_t head_dim, int64_t rows_q,
+                                           int64_t rows_k, const mpipe_heads* d_o,
+                                           const mpipe_heads* q, const mpipe_heads* k,
+                                           const mpipe_heads* v, const mpipe_heads* o,
+                                           const float* lse, int64_t ld_lse,
+                                           const int64_t* seq_row, const int64_t* seq_len,
+                                           const int64_t* key_row, const int64_t* key_len,
+                                           int32_t n_seq, float scale, const mpipe_heads* dq,
+                                           const mpipe_heads* dk, const mpipe_heads* dv,
+                                           void* scratch, size_t scratch_bytes, void* hip_stream);
+/* 0 for arguments out of range. */
+size_t mpipe_op_causal_attention_scratch_bytes(int64_t rows_q, int32_t heads_q, int64_t rows_k,
+                                               int32_t heads_k, int32_t head_dim);
+
+/* A paged key-value cache: k, v [n_pages][heads][page][head_dim] in dtype (aligned to 16 bytes),
+ * page a power of two (tokens).  MPIPE_E4M3 (one sign bit, four of exponent, three of mantissa, no
+ * infinity) keeps a token's head as e4m3 values times a power of two of its own: k_scale, v_scale
+ * uint8 [n_pages][heads][page], the power's exponent + 127; null for the other types.
+ *   table  device int32, table[s * ld_table + i]: the page that holds the tokens i * page .. of
+ *          sequence s (n_seq sequences, `width` pages each at most).  Sequences may share pages
+ *          that are only read. */
+#define MPIPE_E4M3 2
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t n_pages;
+  int32_t heads, page, head_dim, dtype;
+} mpipe_kv_cache;
+
+/* Row i of k and v ([rows][heads][head_dim] in dtype, MPIPE_F32 or MPIPE_BF16) to token pos[i] of
+ * sequence seq[i] (device int32; seq null: sequence i).  Rounded to nearest even where the cache
+ * is narrower.  In e4m3 the power of two is the least that brings the largest finite magnitude
+ * of the head to 448 or less, its exponent between -120 and 120; values that are infinite or not
+ * a number are kept as not a number.  A row with pos[i] < 0 or seq[i] < 0 is left out (padding).
+ * A row whose sequence is not below n_seq, whose page is not in the table's width or whose page
+ * number is not in the pool is left out too, and *status (device int32, nullable, not cleared by the
+ * call) becomes 1.  Rows of one call are of different places (or what such a place holds is
+ * any mix of them). */
+mpipe_status mpipe_op_cache_write(const mpipe_kv_cache* cache, int32_t dtype, int64_t rows,
+                                  const mpipe_heads* k, const mpipe_heads* v,
+                                  const int32_t* table, int64_t ld_table, int32_t n_seq,
+                                  int32_t width, const int32_t* seq, const int32_t* pos,
+                                  int32_t* status, void* hip_stream);
+
+/* The other way: row i of k and v becomes the token's keys and values, in dtype, rounded to
+ * nearest even where that is narrower.  Rows left out as above keep what they held, but one of a bad
+ * place (status 1) becomes not a number. */
+mpipe_status mpipe_op_cache_read(const mpipe_kv_cache* cache, int32_t dtype, int64_t rows,
+                                 const int32_t* table, int64_t ld_table, int32_t n_seq,
+                                 int32_t width, const int32_t* seq, const int32_t* pos,
+                                 const mpipe_heads* k, const mpipe_heads* v, int32_t* status,
+                                 void* hip_stream);
+
+/* Attention of one new token of every sequence over the cache: row s of q and o ([n_seq][heads of
+ * q][head_dim] in dtype) is sequence s, which sees its tokens 0 .. lens[s] - 1 (device int32; the
+ * new token's own keys and values are written before).  dtype MPIPE_BF16 reads bf16 or e4m3
+ * pages, MPIPE_F32 fp32 or e4m3 ones.  lse[head * ld_lse + s] (fp32, nullable).  lens[s] <= 0: o
+ * = 0, lse = -infinity.  A sequence longer than its table, or one of whose pages is not in the
+ * pool, gets not a number.  Statistics as in the causal attention.  The same call gives the same
+ * bits; where a sequence is cut, and with it its last bits, depends on the batch's lengths.
+ * scratch: mpipe_op_cache_attention_scratch_bytes, aligned to 16 bytes, not kept. */
+mpipe_status mpipe_op_cache_attention(const mpipe_kv_cache* cache, int32_t dtype, int32_t n_seq,
+                                      const mpipe_heads* q, const int32_t* table,
+                                      int64_t ld_table, int32_t width, const int32_t* lens,
+                                      float scale, const mpipe_heads* o, float* lse,
+                                      int64_t ld_lse, void* scratch, size_t scratch_bytes,
+                                      void* hip_stream);
+/* 0 for arguments out of range. */
+size_t mpipe_op_cache_attention_scratch_bytes(int32_t n_seq, int32_t heads_q, int32_t heads_k,
+                                              int32_t head_dim);
+
 #ifdef __cplusplus
 }
 #endif

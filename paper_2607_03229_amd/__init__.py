@@ -13,9 +13,11 @@ from ._binding import (  # noqa: F401
     op_attention_bwd, op_scratch_bytes, op_splitk_reduce, gemm_split, gemm_kernel,
     op_seam_positions, op_rope_axes, op_qk_norm_rope_fwd, op_qk_norm_rope_bwd,
     op_qk_norm_rope_scratch_bytes, op_grad_norm, op_grad_clip, op_grad_scratch_bytes,
+    op_causal_attention_fwd, op_causal_attention_bwd, op_causal_attention_scratch_bytes,
+    op_cache_write, op_cache_read, op_cache_attention, op_cache_attention_scratch_bytes, KvCache,
     RopeCfg, GradList, ROPE_BLOCKS, ROPE_INTERLEAVED, ROPE_ONE_SPECTRUM, ROPE_AXIS_SPECTRA,
     ROPE_HALVES, ROPE_ADJACENT,
-    F32, BF16, OK, NOOP_FROZEN,
+    F32, BF16, E4M3, OK, NOOP_FROZEN,
     owner_map, OWNER_GREEDY, OWNER_EXACT, OWNER_REFINED,
     schedule_valid, Derived, EVENT_FIELDS,
     SK_1F1B, SK_GPIPE, SK_TRANSPOSE, LAYOUT_SHARDED, LAYOUT_REPLICATED,

@@ -124,6 +124,16 @@ def load():
         "mpipe_op_grad_norm": (st, [P, i32, P, P, P, sz, P]),
         "mpipe_op_grad_scratch_bytes": (sz, [P, i32]),
         "mpipe_op_grad_clip": (st, [P, P, i32, P, C.c_double, P, P]),
+        "mpipe_op_causal_attention_fwd": (st, [i32, i32, i64, i64, P, P, P, P, P, P, P, i32,
+                                               C.c_float, P, P, i64, P]),
+        "mpipe_op_causal_attention_bwd": (st, [i32, i32, i64, i64, P, P, P, P, P, P, i64, P, P, P,
+                                               P, i32, C.c_float, P, P, P, P, sz, P]),
+        "mpipe_op_causal_attention_scratch_bytes": (sz, [i64, i32, i64, i32, i32]),
+        "mpipe_op_cache_write": (st, [P, i32, i64, P, P, P, i64, i32, i32, P, P, P, P]),
+        "mpipe_op_cache_read": (st, [P, i32, i64, P, i64, i32, i32, P, P, P, P, P, P]),
+        "mpipe_op_cache_attention": (st, [P, i32, i32, P, P, i64, i32, P, C.c_float, P, P, i64, P,
+                                          sz, P]),
+        "mpipe_op_cache_attention_scratch_bytes": (sz, [i32, i32, i32, i32]),
         "mpipe_encoder_cost": (st, [P, P, i32, P, i32, i32, C.c_double, C.c_double, P]),
         "mpipe_owner_map": (st, [P, i32, P, i32, i32, P, P, P]),
         "mpipe_schedule_valid": (st, [P, i32, i32, P]),
@@ -844,3 +854,212 @@ def op_grad_clip(grads, sumsq, max_norm: float, norm=None, out=None, stream=None
     _launch(load().mpipe_op_grad_clip, dev, stream, g.array, None if o is None else o.array, g.n,
             _result(sumsq, 1, torch.float64, dev, "sumsq: fp64 [1]"), max_norm,
             None if norm is None else _result(norm, 1, torch.float32, dev, "norm: fp32 [1]"))
+
+
+# --------------------------------------------------------------------------
+# The first LLM layer's attention
+# --------------------------------------------------------------------------
+
+def _view(t, rows: int, d: int, dtype, dev: int, what: str) -> bytes:
+    """An mpipe_heads of [rows][heads][d], any strides of rows and heads."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != rows or shape[2] != d or t.dtype is not dtype:
+        _bad(what)
+    rs, hs, cs = t.stride()
+    if cs != 1:
+        _bad("the columns of a head must be adjacent")
+    if t.get_device() != dev:
+        _bad("tensors on different devices")
+    return _HEADS.pack(t.data_ptr(), rs, hs, shape[1], 0)
+
+
+def _lse(t, heads: int, rows: int, dev: int) -> Tuple[Optional[int], int]:
+    import torch
+    if t is None:
+        return None, 0
+    if (t.dtype is not torch.float32 or t.dim() != 2 or t.shape[0] != heads or
+            t.shape[1] != rows or (rows > 1 and t.stride(1) != 1)):
+        _bad("lse: fp32 [heads of q][rows], rows adjacent")
+    if t.get_device() != dev:
+        _bad("tensors on different devices")
+    return t.data_ptr(), t.stride(0) if heads > 1 else rows
+
+
+def _sequence_lists(seq_row, seq_len, key_row, key_len):
+    sr, sl = _host_ints(seq_row, "seq_row"), _host_ints(seq_len, "seq_len")
+    if (key_row is None) != (key_len is None):
+        _bad("key_row and key_len go together")
+    kr = None if key_row is None else _host_ints(key_row, "key_row")
+    kl = None if key_len is None else _host_ints(key_len, "key_len")
+    n = sr.size
+    if sl.size != n or (kr is not None and (kr.size != n or kl.size != n)):
+        _bad("seq_row, seq_len, key_row and key_len differ in length")
+    return (sr.tobytes(), sl.tobytes(), None if kr is None else kr.tobytes(),
+            None if kl is None else kl.tobytes(), n)
+
+
+_ATTN_Q = "q, o and their gradients: [rows][heads][head_dim] of one dtype"
+_ATTN_K = "k, v and their gradients: [key rows][key heads][head_dim] in the dtype of q"
+
+
+def _attn_shapes(q, k):
+    if len(q.shape) != 3 or len(k.shape) != 3:
+        _bad(_ATTN_Q)
+    return q.shape[0], k.shape[0], q.shape[2], q.dtype, q.get_device()
+
+
+def op_causal_attention_fwd(q, k, v, o, lse, seq_row, seq_len, key_row=None, key_len=None,
+                            scale: Optional[float] = None, stream=None) -> None:
+    """o ([rows][heads][head_dim]) = causal attention of q over k, v ([key rows][key heads]
+    [head_dim], any strides of rows and heads), sequence s being the rows seq_row[s] .. +
+    seq_len[s] and its keys key_row[s] .. + key_len[s] (the same rows unless given); they end
+    together, so more keys are a prefix.  lse (fp32 [heads][rows], may be None) for the
+    backward.  scale: head_dim ** -0.5 unless given.  Rows of no sequence are left as they
+    were."""
+    rq, rk, d, dtype, dev = _attn_shapes(q, k)
+    p, ld = _lse(lse, q.shape[1], rq, dev)
+    _launch(load().mpipe_op_causal_attention_fwd, dev, stream, _code(dtype), d, rq, rk,
+            _view(q, rq, d, dtype, dev, _ATTN_Q), _view(k, rk, d, dtype, dev, _ATTN_K),
+            _view(v, rk, d, dtype, dev, _ATTN_K),
+            *_sequence_lists(seq_row, seq_len, key_row, key_len),
+            d ** -0.5 if scale is None else scale, _view(o, rq, d, dtype, dev, _ATTN_Q), p, ld)
+
+
+def op_causal_attention_scratch_bytes(rows: int, heads: int, key_rows: int, key_heads: int,
+                                      head_dim: int) -> int:
+    n = int(load().mpipe_op_causal_attention_scratch_bytes(rows, heads, key_rows, key_heads,
+                                                           head_dim))
+    if n == 0:
+        _bad("op_causal_attention_scratch_bytes: argument out of range")
+    return n
+
+
+def op_causal_attention_bwd(d_o, q, k, v, o, lse, seq_row, seq_len, dq, dk, dv, scratch,
+                            key_row=None, key_len=None, scale: Optional[float] = None,
+                            stream=None) -> None:
+    """Gradients of op_causal_attention_fwd from d_o, the gradient of o, and what the forward took
+    and gave: dq, dk, dv overwritten in the sequences' rows (they may be columns of one product).
+    scratch: op_causal_attention_scratch_bytes."""
+    rq, rk, d, dtype, dev = _attn_shapes(q, k)
+    if lse is None:
+        _bad("the backward needs lse")
+    p, ld = _lse(lse, q.shape[1], rq, dev)
+    _launch(load().mpipe_op_causal_attention_bwd, dev, stream, _code(dtype), d, rq, rk,
+            _view(d_o, rq, d, dtype, dev, _ATTN_Q), _view(q, rq, d, dtype, dev, _ATTN_Q),
+            _view(k, rk, d, dtype, dev, _ATTN_K), _view(v, rk, d, dtype, dev, _ATTN_K),
+            _view(o, rq, d, dtype, dev, _ATTN_Q), p, ld,
+            *_sequence_lists(seq_row, seq_len, key_row, key_len),
+            d ** -0.5 if scale is None else scale, _view(dq, rq, d, dtype, dev, _ATTN_Q),
+            _view(dk, rk, d, dtype, dev, _ATTN_K), _view(dv, rk, d, dtype, dev, _ATTN_K),
+            *_buffer(scratch, dev))
+
+
+_KV_CACHE = struct.Struct("PPPPqiiii")    # mpipe_kv_cache
+E4M3 = 2
+
+
+class KvCache:
+    """The pages of a key-value cache: k, v [pages][heads][page][head_dim] (contiguous; fp32,
+    bf16 or torch.float8_e4m3fn, a page's tokens a power of two) and for 8 bits k_scale, v_scale,
+    uint8 [pages][heads][page], which hold the exponent + 127 of each token's power of two.
+    It keeps the tensors; their memory must stay where it is."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype:
+            _bad("k and v: [pages][heads][page][head_dim] of one dtype")
+        eight = k.dtype is torch.float8_e4m3fn
+        self.dtype = E4M3 if eight else _code(k.dtype)
+        if eight != (k_scale is not None) or eight != (v_scale is not None):
+            _bad("scales go with 8-bit pages, and only with them")
+        self.tensors = [t for t in (k, v, k_scale, v_scale) if t is not None]
+        for t in self.tensors[2:]:
+            if t.dtype is not torch.uint8 or t.shape != k.shape[:3]:
+                _bad("scales: uint8 [pages][heads][page]")
+        self.dev = k.get_device()
+        for t in self.tensors:
+            if not t.is_contiguous():
+                _bad("the cache must be contiguous")
+            if t.get_device() != self.dev:
+                _bad("tensors on different devices")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads, self.page, self.head_dim = k.shape
+
+    def _now(self) -> bytes:
+        return _KV_CACHE.pack(self.k.data_ptr(), self.v.data_ptr(),
+                              0 if self.k_scale is None else self.k_scale.data_ptr(),
+                              0 if self.v_scale is None else self.v_scale.data_ptr(), self.pages,
+                              self.heads, self.page, self.head_dim, self.dtype)
+
+
+def _table(table, dev: int) -> Tuple[int, int, int, int]:
+    """Address, stride, sequences and width of page tables."""
+    import torch
+    if (table.dtype is not torch.int32 or table.dim() != 2 or
+            (table.shape[1] > 1 and table.stride(1) != 1)):
+        _bad("table: int32 [sequences][pages], a sequence's pages adjacent")
+    if table.get_device() != dev:
+        _bad("tensors on different devices")
+    n, width = table.shape
+    return table.data_ptr(), table.stride(0) if n > 1 else width, n, width
+
+
+def _row_ints(t, rows: int, dev: int, what: str) -> Optional[int]:
+    import torch
+    return None if t is None else _vector(t, rows, torch.int32, dev, what)
+
+
+def _cache_rows(cache, k, v, table, pos, seq, status):
+    import torch
+    rows, d, dtype, dev = k.shape[0], cache.head_dim, k.dtype, cache.dev
+    what = "k and v: [rows][heads][head_dim] of one dtype"
+    if pos is None:
+        _bad("pos: int32 [rows]")
+    return (rows, _code(dtype), _view(k, rows, d, dtype, dev, what),
+            _view(v, rows, d, dtype, dev, what), _table(table, dev),
+            _row_ints(seq, rows, dev, "seq: int32 [rows]"),
+            _row_ints(pos, rows, dev, "pos: int32 [rows]"),
+            None if status is None else _result(status, 1, torch.int32, dev, "status: int32 [1]"))
+
+
+def op_cache_write(cache, k, v, table, pos, seq=None, status=None, stream=None) -> None:
+    """Row i of k and v ([rows][heads][head_dim], fp32 or bf16, any strides of rows and heads)
+    to token pos[i] of sequence seq[i] (int32; sequence i unless given), whose pages are
+    table[seq[i]] (int32).  Rows with a negative pos or seq are left out; rows of a place
+    outside the tables or the pool too, and status (int32 [1], may be None) becomes 1."""
+    rows, code, kv, vv, tab, seq, pos, status = _cache_rows(cache, k, v, table, pos, seq, status)
+    _launch(load().mpipe_op_cache_write, cache.dev, stream, cache._now(), code, rows, kv, vv,
+            *tab, seq, pos, status)
+
+
+def op_cache_read(cache, table, pos, k, v, seq=None, status=None, stream=None) -> None:
+    """The other way: the keys and values of token pos[i] of sequence seq[i] into row i of k and
+    v.  Rows left out keep what they held; rows of a bad place become NaN."""
+    rows, code, kv, vv, tab, seq, pos, status = _cache_rows(cache, k, v, table, pos, seq, status)
+    _launch(load().mpipe_op_cache_read, cache.dev, stream, cache._now(), code, rows, *tab, seq,
+            pos, kv, vv, status)
+
+
+def op_cache_attention(cache, q, table, lens, o, scratch, lse=None, scale: Optional[float] = None,
+                       stream=None) -> None:
+    """o[s] = attention of q[s] ([sequences][heads][head_dim]), the new token of sequence s, over
+    its lens[s] (int32) tokens in the cache, the new one's own among them.  lse: fp32
+    [heads][sequences], may be None.  scratch: op_cache_attention_scratch_bytes."""
+    import torch
+    n, d, dtype, dev = q.shape[0], cache.head_dim, q.dtype, cache.dev
+    at, ld, seqs, width = _table(table, dev)
+    if seqs != n:
+        _bad("table and q differ in sequences")
+    p, ld_lse = _lse(lse, q.shape[1], n, dev)
+    _launch(load().mpipe_op_cache_attention, dev, stream, cache._now(), _code(dtype), n,
+            _view(q, n, d, dtype, dev, _ATTN_Q), at, ld, width,
+            _vector(lens, n, torch.int32, dev, "lens: int32 [sequences]"),
+            d ** -0.5 if scale is None else scale, _view(o, n, d, dtype, dev, _ATTN_Q), p, ld_lse,
+            *_buffer(scratch, dev))
+
+
+def op_cache_attention_scratch_bytes(seqs: int, heads: int, key_heads: int, head_dim: int) -> int:
+    n = int(load().mpipe_op_cache_attention_scratch_bytes(seqs, heads, key_heads, head_dim))
+    if n == 0:
+        _bad("op_cache_attention_scratch_bytes: argument out of range")
+    return n

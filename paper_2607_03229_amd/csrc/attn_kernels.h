@@ -1,0 +1,77 @@
+// Launch interface of the first LLM layer's attention (causal_attention.hip,
+// causal_general.hip, cache_attention.hip, kv_cache.hip); arguments are checked by attn_ops.cpp.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "attn_plan.h"
+#include "internal.h"
+
+namespace mpipe {
+
+struct CausalProblem {
+  int dtype = 0, head_dim = 0;
+  int64_t rows_q = 0, rows_k = 0;
+  HeadView q, k, v, o, d_o, dq, dk, dv;
+  float* lse = nullptr;
+  int64_t ld_lse = 0;
+  float* scratch = nullptr;
+  float scale = 0.f;
+  std::vector<AttnSeq> seqs;
+};
+hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s);
+hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s);
+size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k,
+                                int head_dim);
+
+// What a kernel of causal attention takes; all of it stays below 4 KB.
+struct AttnView {
+  const void* p;
+  int64_t row, head;
+};
+struct CausalArgs {
+  AttnPool pool;
+  AttnView q, k, v, o, d_o, dq, dk, dv;
+  float* lse;
+  float* delta;   // backward: dO . O of every [head][row], rows_q apart
+  int64_t ld_lse, rows_q;
+  float scale;
+  int d, heads_k, group;
+};
+static_assert(sizeof(CausalArgs) <= 4000, "a launch's arguments");
+// Any dtype, alignment and head_dim of at most 256 (causal_general.hip).
+hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
+
+struct CacheRows {   // rows on their way into or out of a cache
+  mpipe_kv_cache cache;
+  int dtype = 0;
+  int64_t rows = 0;
+  HeadView k, v;
+  const int32_t* table = nullptr;
+  int64_t ld_table = 0;
+  int32_t n_seq = 0, width = 0;
+  const int32_t* seq = nullptr;
+  const int32_t* pos = nullptr;
+  int32_t* status = nullptr;
+};
+hipError_t cache_write(const CacheRows& p, hipStream_t s);
+hipError_t cache_read(const CacheRows& p, hipStream_t s);
+
+struct CacheAttention {
+  mpipe_kv_cache cache;
+  int dtype = 0;
+  int32_t n_seq = 0, width = 0;
+  HeadView q, o;
+  const int32_t* table = nullptr;
+  int64_t ld_table = 0;
+  const int32_t* lens = nullptr;
+  float scale = 0.f;
+  float* lse = nullptr;
+  int64_t ld_lse = 0;
+  float* scratch = nullptr;
+};
+hipError_t cache_attention(const CacheAttention& p, hipStream_t s);
+size_t cache_attention_scratch(int n_seq, int heads_q, int heads_k, int head_dim);
+
+}  // namespace mpipe

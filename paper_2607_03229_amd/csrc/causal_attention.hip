@@ -1,0 +1,72 @@
+// Causal attention with grouped heads over sequences (mpipe_op_causal_attention_fwd / _bwd):
+// the launches.
+#include "attn_kernels.h"
+#include "common.h"
+
+namespace mpipe {
+namespace {
+
+AttnView view(const HeadView& v) { return {v.p, v.row, v.head}; }
+
+CausalArgs args_of(const CausalProblem& p) {
+  CausalArgs a;
+  a.q = view(p.q);
+  a.k = view(p.k);
+  a.v = view(p.v);
+  a.o = view(p.o);
+  a.d_o = view(p.d_o);
+  a.dq = view(p.dq);
+  a.dk = view(p.dk);
+  a.dv = view(p.dv);
+  a.lse = p.lse;
+  a.ld_lse = p.ld_lse;
+  a.delta = p.scratch;
+  a.rows_q = p.rows_q;
+  a.scale = p.scale;
+  a.d = p.head_dim;
+  a.heads_k = p.k.heads;
+  a.group = p.q.heads / p.k.heads;
+  return a;
+}
+
+// All items, as many to a launch as its arguments and 2^23 blocks hold.
+template <class Launch>
+hipError_t in_pieces(const CausalProblem& p, CausalArgs& a, bool by_keys, int64_t blocks_per_item,
+                     Launch one) {
+  std::vector<AttnItem> items;
+  attn_items(p.seqs, by_keys, items);
+  const int64_t most = (int64_t(1) << 23) / blocks_per_item;
+  for (size_t at = 0; at < items.size();) {
+    const int n = attn_pack(p.seqs, items, at, most, a.pool);
+    if (hipError_t e = one(a, n)) return e;
+    at += n;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
+  CausalArgs a = args_of(p);
+  return in_pieces(p, a, false, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
+    return causal_general_fwd(p.dtype, b, n, s);
+  });
+}
+
+size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k,
+                                int head_dim) {
+  return ((size_t)rows_q * heads_q * sizeof(float) + 15) / 16 * 16 + 16;
+}
+
+hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
+  CausalArgs a = args_of(p);
+  if (hipError_t e = in_pieces(p, a, false, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
+        return causal_general_dq(p.dtype, b, n, s);
+      }))
+    return e;
+  return in_pieces(p, a, true, 8 * p.k.heads, [&](const CausalArgs& b, int n) {
+    return causal_general_dkdv(p.dtype, b, n, s);
+  });
+}
+
+}  // namespace mpipe
