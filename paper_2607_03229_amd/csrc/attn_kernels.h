@@ -38,10 +38,15 @@ struct CausalArgs {
   int d, heads_k, group;
 };
 static_assert(sizeof(CausalArgs) <= 4000, "a launch's arguments");
-// Any dtype, alignment and head_dim of at most 256 (causal_general.hip).
+// Any dtype, alignment and head_dim of at most 256 (causal_general.hip): items of kGeneralRows.
+constexpr int kGeneralRows = 128;
 hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
+
+// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip): items of kForwardRows.
+constexpr int kForwardRows = 256;
+hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
 
 struct CacheRows {   // rows on their way into or out of a cache
   mpipe_kv_cache cache;

@@ -55,18 +55,19 @@ mpipe_status attn_sequences(const int64_t* seq_row, const int64_t* seq_len, cons
   return MPIPE_OK;
 }
 
-void attn_items(const std::vector<AttnSeq>& seqs, bool by_keys, std::vector<AttnItem>& items) {
+void attn_items(const std::vector<AttnSeq>& seqs, bool by_keys, int rows,
+                std::vector<AttnItem>& items) {
   struct Order {
     int64_t walk;
     AttnItem item;
   };
   std::vector<Order> order;
   for (size_t s = 0; s < seqs.size(); ++s) {
-    const int64_t nq = seqs[s].q_len, nk = seqs[s].k_len, rows = by_keys ? nk : nq;
-    for (int64_t t = 0; t * kAttnRows < rows; ++t) {
+    const int64_t nq = seqs[s].q_len, nk = seqs[s].k_len, n = by_keys ? nk : nq;
+    for (int64_t t = 0; t * rows < n; ++t) {
       // keys the item's last query sees, or queries that see the item's first key
-      const int64_t walk = by_keys ? std::min(nq, nk - t * kAttnRows)
-                                   : std::min(nk, (t + 1) * kAttnRows + nk - nq);
+      const int64_t walk = by_keys ? std::min(nq, nk - t * rows)
+                                   : std::min(nk, (t + 1) * rows + nk - nq);
       order.push_back({walk, {(int32_t)s, (int32_t)t}});
     }
   }

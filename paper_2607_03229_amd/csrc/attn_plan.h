@@ -21,14 +21,14 @@ mpipe_status attn_sequences(const int64_t* seq_row, const int64_t* seq_len, cons
                             const int64_t* key_len, int32_t n_seq, int64_t rows_q, int64_t rows_k,
                             bool keys_apart, std::vector<AttnSeq>& seqs, std::string& why);
 
-// A work item: kAttnRows rows (queries, or keys) of one sequence.
-constexpr int kAttnRows = 128;
+// A work item: a tile of rows (queries, or keys) of one sequence.
 struct AttnItem {
   int32_t seq, tile;
 };
-// Items of every query (by_keys: key) row, the longest walks over the other side first, so that
-// what starts last ends soon.
-void attn_items(const std::vector<AttnSeq>& seqs, bool by_keys, std::vector<AttnItem>& items);
+// Items of `rows` query (by_keys: key) rows each, the longest walks over the other side first, so
+// that what starts last ends soon.
+void attn_items(const std::vector<AttnSeq>& seqs, bool by_keys, int rows,
+                std::vector<AttnItem>& items);
 
 // What one launch carries in its arguments: sequences from the front (four words each), items
 // from the back (a word: sequence in 8 bits, tile in 24).

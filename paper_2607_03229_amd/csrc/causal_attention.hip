@@ -1,5 +1,7 @@
 // Causal attention with grouped heads over sequences (mpipe_op_causal_attention_fwd / _bwd):
 // the launches.
+#include <initializer_list>
+
 #include "attn_kernels.h"
 #include "common.h"
 
@@ -31,10 +33,10 @@ CausalArgs args_of(const CausalProblem& p) {
 
 // All items, as many to a launch as its arguments and 2^23 blocks hold.
 template <class Launch>
-hipError_t in_pieces(const CausalProblem& p, CausalArgs& a, bool by_keys, int64_t blocks_per_item,
-                     Launch one) {
+hipError_t in_pieces(const CausalProblem& p, CausalArgs& a, bool by_keys, int rows,
+                     int64_t blocks_per_item, Launch one) {
   std::vector<AttnItem> items;
-  attn_items(p.seqs, by_keys, items);
+  attn_items(p.seqs, by_keys, rows, items);
   const int64_t most = (int64_t(1) << 23) / blocks_per_item;
   for (size_t at = 0; at < items.size();) {
     const int n = attn_pack(p.seqs, items, at, most, a.pool);
@@ -44,11 +46,24 @@ hipError_t in_pieces(const CausalProblem& p, CausalArgs& a, bool by_keys, int64_
   return hipSuccess;
 }
 
+// Whether the bf16 kernels can read and write these views: 16-byte pieces at 16-byte places, and a
+// tile's 64 rows less than 2^31 bytes apart.
+bool tiled(const CausalProblem& p, std::initializer_list<const HeadView*> views) {
+  if (p.dtype != DT_BF16 || p.head_dim > 128) return false;
+  for (const HeadView* v : views)
+    if ((uintptr_t)v->p % 16 || v->row % 8 || v->head % 8 || v->row > (1 << 23)) return false;
+  return true;
+}
+
 }  // namespace
 
 hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
-  return in_pieces(p, a, false, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
+  if (tiled(p, {&p.q, &p.k, &p.v, &p.o}))
+    return in_pieces(p, a, false, kForwardRows, p.q.heads, [&](const CausalArgs& b, int n) {
+      return causal_bf16_fwd(b, n, s);
+    });
+  return in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
     return causal_general_fwd(p.dtype, b, n, s);
   });
 }
@@ -60,11 +75,11 @@ size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int
 
 hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
-  if (hipError_t e = in_pieces(p, a, false, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
+  if (hipError_t e = in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
         return causal_general_dq(p.dtype, b, n, s);
       }))
     return e;
-  return in_pieces(p, a, true, 8 * p.k.heads, [&](const CausalArgs& b, int n) {
+  return in_pieces(p, a, true, kGeneralRows, 8 * p.k.heads, [&](const CausalArgs& b, int n) {
     return causal_general_dkdv(p.dtype, b, n, s);
   });
 }

@@ -1,0 +1,233 @@
+// Shared pieces of the bf16 kernels of causal attention (causal_fwd.hip, causal_bwd.hip).
+//
+// A tile is 64 rows of one head, DP columns wide (32, 64, 96 or 128; columns past head_dim and
+// rows past the sequence are zeros), row-major in LDS in chunks of 16 bytes, chunk c of row R at
+// c ^ swz(R).  It is filled by 16-byte global-to-LDS copies, whose lane l writes slot base + l,
+// so each lane picks the source of its slot.  Two kinds of reads take MFMA operands from it:
+//   rows        16 bytes of row l % 32: sixteen rows at a time fall on sixteen different chunks
+//   transposed  (ds_read_b64_tr_b16) four rows x 64 bytes at a time: swz moves rows of one such
+//               group to four different groups of four chunks
+// so neither meets a bank twice.
+//
+// MFMA operands (v_mfma_f32_32x32x16_bf16), lane l = 32 h + c: A holds row c, B column c, both the
+// eight reduction indices 8h .. 8h + 7; the accumulator's element i is row 8 (i / 4) + 4h + i % 4
+// of column c.
+#pragma once
+#include "attn_kernels.h"
+#include "common.h"
+
+namespace mpipe {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <int DP> struct Tile {
+  static constexpr int NC = DP / 8;         // chunks of a row
+  static constexpr int SLOTS = 64 * NC;
+  static constexpr int KF = DP / 16;        // 16-wide steps over the columns
+  static constexpr int DT = DP / 32;        // 32-wide output tiles
+};
+
+template <int DP> __device__ __forceinline__ int swz(int row) {
+  const int lo = (row >> 2) & 3;
+  if constexpr (DP == 128) return lo | (row & 3) << 2;
+  if constexpr (DP == 64) return lo | ((row >> 1) & 1) << 2;
+  return lo;
+}
+// A lane's places in a tile, bytes from its start, once a kernel; a read adds the tile's LDS
+// address, and what is a multiple of 16 rows is part of the instruction.
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+template <int DP> struct RowReads {   // rows r0 + c (r0 a multiple of 32), columns 16f + 8h ..
+  uint32_t at[Tile<DP>::KF];
+  __device__ __forceinline__ void init(int c, int h) {
+#pragma unroll
+    for (int f = 0; f < Tile<DP>::KF; ++f) at[f] = (c * Tile<DP>::NC + ((2 * f + h) ^ swz<DP>(c))) * 16;
+  }
+  __device__ __forceinline__ bf16x8 get(uint32_t tile, int r0, int f) const {
+    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+    return *reinterpret_cast<lds_bf16x8*>(tile + at[f] + r0 * Tile<DP>::NC * 16);
+  }
+};
+// Transposed: column 32 dt + c, rows k0 + 4h .. + 3 and k0 + 8 + 4h .. + 3 (k0 a multiple of
+// 16): the rows whose scores an accumulator's elements 8j .. 8j + 7 hold.
+template <int DP> struct ColReads {
+  uint32_t at[Tile<DP>::DT][2];
+  __device__ __forceinline__ void init(int l) {
+    const int h = l >> 5, r = l & 15;
+#pragma unroll
+    for (int dt = 0; dt < Tile<DP>::DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = 4 * h + (r >> 2) + 8 * i;    // of k0's sixteen
+        const int chunk = 4 * dt + 2 * ((l >> 4) & 1) + ((r & 3) >> 1);
+        at[dt][i] = (row * Tile<DP>::NC + (chunk ^ swz<DP>(row))) * 16 + (r & 1) * 8;
+      }
+  }
+  __device__ __forceinline__ bf16x8 get(uint32_t tile, int k0, int dt) const {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<lds_s16x4*>(tile + at[dt][i] + k0 * Tile<DP>::NC * 16));
+      const bf16* p = reinterpret_cast<const bf16*>(&a);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * i + e] = p[e];
+    }
+    return v;
+  }
+};
+__device__ __forceinline__ f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+// row of an accumulator's element i
+__device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// Registers' operand of one row from memory, as B (or A) over the columns.
+template <int DP> struct RowOp {
+  bf16x8 f[Tile<DP>::KF];
+};
+template <int DP>
+__device__ __forceinline__ void load_row(RowOp<DP>& R, const bf16* row, int d, int h) {
+#pragma unroll
+  for (int f = 0; f < Tile<DP>::KF; ++f) {
+    const int col = 16 * f + 8 * h;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (col < d) v = *reinterpret_cast<const uint4*>(row + col);
+    R.f[f] = *reinterpret_cast<bf16x8*>(&v);
+  }
+}
+
+// Sources of pad columns and of rows past the end.
+static __device__ const uint4 kZeroChunk = {0, 0, 0, 0};
+
+// Wave w of NWV waves copies its share of a pair of tiles (x, then y): wave instruction j = w,
+// NWV + w, ... of 2 NC, each 64 slots.  A lane's source is a 32-bit distance from the tile's first
+// row: 64 rows of a view are less than 2^31 bytes.
+template <int DP, int NWV> struct PairCopy {
+  static constexpr int NC = Tile<DP>::NC, N = 2 * NC / NWV;
+  static_assert(2 * NC % NWV == 0, "whole instructions for every wave");
+  uint32_t off[N];
+  __device__ __forceinline__ static bool of_x(int i, int w) {
+    if constexpr (NC % NWV == 0) return i < NC / NWV;
+    else return i * NWV + w < NC;
+  }
+  __device__ __forceinline__ static int slot(int i, int w, int l) {
+    const int j = i * NWV + w;
+    return (of_x(i, w) ? j : j - NC) * 64 + l;
+  }
+  __device__ __forceinline__ static int row(int s) { return s / NC; }
+  __device__ __forceinline__ static int col(int s) { return 8 * (s % NC ^ swz<DP>(s / NC)); }
+  __device__ __forceinline__ void init(int w, int l, int64_t ld_x, int64_t ld_y) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int s = slot(i, w, l);
+      off[i] = 2 * (uint32_t)(row(s) * (of_x(i, w) ? ld_x : ld_y) + col(s));
+    }
+  }
+  // Share i into `tile`, from rows X.. of which `rows` (any number) exist and d columns.
+  __device__ __forceinline__ void copy(int i, int w, int l, uint32_t tile, const bf16* X, int rows, int d) const {
+    const int s0 = slot(i, w, 0);
+    const char* from = reinterpret_cast<const char*>(X) + off[i];
+    if (rows < 64 || d < DP) {
+      const int s = s0 + l;
+      if (row(s) >= rows || col(s) >= d) from = reinterpret_cast<const char*>(&kZeroChunk);
+    }
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(from),
+                                     reinterpret_cast<lds_void*>(tile + 16 * s0), 16, 0, 0);
+  }
+};
+
+// Wait until at most n of the wave's memory operations are under way (s_waitcnt: vmcnt in bits
+// 3:0 and 15:14; expcnt and lgkmcnt at their largest).
+template <int n> __device__ __forceinline__ void wait_copies() {
+  static_assert(n >= 0 && n < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | (((n >> 4) & 3) << 14));
+}
+// A barrier that waits for the wave's LDS reads, not for copies under way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// 2^x (v_exp_f32): results below the normal range become 0, which no bf16 weight notices.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ bf16x8 pack8(const f32x16& s, int j) {
+  bf16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (bf16)s[8 * j + e];
+  return r;
+}
+template <int N> __device__ __forceinline__ bool finite16(const f32x16 (&acc)[N]) {
+  float z = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z = fmaf(acc[i][e], 0.f, z);
+  return __all(z == 0.f);
+}
+
+// The block's sequence, first row and head; the key head is the fastest index: blocks go round
+// the eight XCDs, so those that read the same keys share an L2.
+struct AttnPlace {
+  int q_row, q_len, k_row, k_len, r0, head_k, gq;
+};
+__device__ __forceinline__ AttnPlace attn_place(const CausalArgs& p, int per_head, int rows) {
+  AttnPlace a;
+  int b = blockIdx.x;
+  a.head_k = b % p.heads_k;
+  b /= p.heads_k;
+  a.gq = b % per_head;
+  b /= per_head;
+  const uint32_t it = (uint32_t)p.pool.word[kAttnWords - 1 - b];
+  const int32_t* s = p.pool.word + 4 * (it & 255);
+  a.q_row = s[0];
+  a.q_len = s[1];
+  a.k_row = s[2];
+  a.k_len = s[3];
+  a.r0 = (int)(it >> 8) * rows;
+  return a;
+}
+__device__ __forceinline__ const bf16* head_of(const AttnView& v, int head, int row) {
+  return reinterpret_cast<const bf16*>(v.p) + v.head * head + v.row * row;
+}
+__device__ __forceinline__ bf16* out_of(const AttnView& v, int head, int row) {
+  return const_cast<bf16*>(head_of(v, head, row));
+}
+
+// acc += the products of a cut tile pair by pair: weights w (elements as an accumulator's of the
+// tile's 64 rows), `tile` the other operand's rows in LDS, seen(row) whether the pair counts.
+template <int DP, class Seen>
+__device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf16x8 (&w)[4],
+                                          const uint4* tile, int l, Seen seen) {
+  const int c = l & 31, h = l >> 5;
+  for (int row = 0; row < 64; ++row) {
+    const int half = row >> 5, i = ((row & 31) >> 3) * 4 + (row & 3), src = (row >> 2) & 1;
+    float x = 0.f;
+#pragma unroll
+    for (int n = 0; n < 32; ++n) x = n == 16 * half + i ? (float)w[n >> 3][n & 7] : x;
+    x = __shfl(x, c + 32 * src);
+    const bool in = seen(row);
+#pragma unroll
+    for (int dt = 0; dt < Tile<DP>::DT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {     // columns 32 dt + 8q + 4h ..
+        const uint4* chunk = tile + row * Tile<DP>::NC + ((4 * dt + q) ^ swz<DP>(row));
+        const bf16* y = reinterpret_cast<const bf16*>(chunk) + 4 * h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[dt][4 * q + e] = in ? fmaf(x, (float)y[e], acc[dt][4 * q + e]) : acc[dt][4 * q + e];
+      }
+  }
+}
+
+}  // namespace mpipe

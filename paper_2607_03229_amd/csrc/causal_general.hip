@@ -23,7 +23,7 @@
 namespace mpipe {
 namespace {
 
-constexpr int SUB = kAttnRows / 16;   // 16-row blocks of a work item
+constexpr int SUB = kGeneralRows / 16;   // 16-row blocks of a work item
 
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 typedef __attribute__((ext_vector_type(4), aligned(2))) bf16 bf16x4_any;
@@ -170,7 +170,7 @@ __device__ __forceinline__ Place place_of(const CausalArgs& p, int per_head) {
   a.q_len = s[1];
   a.k_row = s[2];
   a.k_len = s[3];
-  a.r0 = (int)(it >> 8) * kAttnRows + 16 * (b % SUB);
+  a.r0 = (int)(it >> 8) * kGeneralRows + 16 * (b % SUB);
   return a;
 }
 
