@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libmpipe.so")
 SOURCES = ["gemm.hip", "gemm_big.hip", "gemm_f32.hip", "gemm_small.hip", "attention.hip", "elementwise.hip", "plan.cpp", "encoder.cpp", "ops.cpp", "owner.cpp", "derive.cpp", "noalloc.hip",
            "layer_plan.cpp", "layer_ops.cpp", "positions.hip", "qk_rope.hip", "grad_clip.hip",
            "attn_plan.cpp", "attn_ops.cpp", "causal_attention.hip", "causal_general.hip",
-           "causal_fwd.hip",
+           "causal_fwd.hip", "causal_bwd.hip",
            "cache_attention.hip", "kv_cache.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -32,7 +32,7 @@ struct CausalArgs {
   AttnPool pool;
   AttnView q, k, v, o, d_o, dq, dk, dv;
   float* lse;
-  float* delta;   // backward: dO . O of every [head][row], rows_q apart
+  float* delta;   // backward: [2][heads][rows_q] of what one kernel leaves to the next
   int64_t ld_lse, rows_q;
   float scale;
   int d, heads_k, group;
@@ -44,9 +44,12 @@ hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStre
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
 
-// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip): items of kForwardRows.
-constexpr int kForwardRows = 256;
+// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip): items of
+// so many rows.  dq writes to `delta` what dkdv reads: -lse * log2(e), then -dO . O.
+constexpr int kForwardRows = 256, kBackwardQRows = 256, kBackwardKRows = 128;
 hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s);
 
 struct CacheRows {   // rows on their way into or out of a cache
   mpipe_kv_cache cache;

@@ -70,11 +70,20 @@ hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
 
 size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k,
                                 int head_dim) {
-  return ((size_t)rows_q * heads_q * sizeof(float) + 15) / 16 * 16 + 16;
+  return (size_t)rows_q * heads_q * 2 * sizeof(float) + 16;
 }
 
 hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
+  if (tiled(p, {&p.q, &p.k, &p.v, &p.o, &p.d_o, &p.dq, &p.dk, &p.dv})) {
+    if (hipError_t e = in_pieces(p, a, false, kBackwardQRows, p.q.heads, [&](const CausalArgs& b, int n) {
+          return causal_bf16_dq(b, n, s);
+        }))
+      return e;
+    return in_pieces(p, a, true, kBackwardKRows, p.k.heads, [&](const CausalArgs& b, int n) {
+      return causal_bf16_dkdv(b, n, s);
+    });
+  }
   if (hipError_t e = in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
         return causal_general_dq(p.dtype, b, n, s);
       }))

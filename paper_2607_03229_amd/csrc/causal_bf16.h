@@ -19,7 +19,6 @@
 namespace mpipe {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 template <int DP> struct Tile {
@@ -109,6 +108,23 @@ __device__ __forceinline__ void load_row(RowOp<DP>& R, const bf16* row, int d, i
 // Sources of pad columns and of rows past the end.
 static __device__ const uint4 kZeroChunk = {0, 0, 0, 0};
 
+// Copies from memory into LDS (lane l's 16 or 4 bytes to `to` + its place), under way until
+// wait_copies.  Instructions of their own rather than the builtin: for the builtin's copies the
+// compiler puts a wait before every transposing read, whose LDS it cannot tell from theirs.  They
+// write no register, and read theirs as they are issued.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "s"(to), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void copy16(uint32_t to, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(to), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :: "s"(to), "v"(from) : "memory", "m0");
+}
+
 // Wave w of NWV waves copies its share of a pair of tiles (x, then y): wave instruction j = w,
 // NWV + w, ... of 2 NC, each 64 slots.  A lane's source is a 32-bit distance from the tile's first
 // row: 64 rows of a view are less than 2^31 bytes.
@@ -136,13 +152,14 @@ template <int DP, int NWV> struct PairCopy {
   // Share i into `tile`, from rows X.. of which `rows` (any number) exist and d columns.
   __device__ __forceinline__ void copy(int i, int w, int l, uint32_t tile, const bf16* X, int rows, int d) const {
     const int s0 = slot(i, w, 0);
-    const char* from = reinterpret_cast<const char*>(X) + off[i];
     if (rows < 64 || d < DP) {
       const int s = s0 + l;
+      const char* from = reinterpret_cast<const char*>(X) + off[i];
       if (row(s) >= rows || col(s) >= d) from = reinterpret_cast<const char*>(&kZeroChunk);
+      copy16(tile + 16 * s0, from);
+    } else {
+      copy16(tile + 16 * s0, X, off[i]);
     }
-    __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(from),
-                                     reinterpret_cast<lds_void*>(tile + 16 * s0), 16, 0, 0);
   }
 };
 
@@ -204,17 +221,21 @@ __device__ __forceinline__ bf16* out_of(const AttnView& v, int head, int row) {
   return const_cast<bf16*>(head_of(v, head, row));
 }
 
-// acc += the products of a cut tile pair by pair: weights w (elements as an accumulator's of the
-// tile's 64 rows), `tile` the other operand's rows in LDS, seen(row) whether the pair counts.
-template <int DP, class Seen>
-__device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf16x8 (&w)[4],
+// acc += the products of a cut tile of N rows pair by pair: weights w (elements as the
+// accumulators' of its rows), `tile` the other operand's rows in LDS, seen(row) whether the pair
+// counts.  A pair that does not has weight 0, but 0 times an infinity or a NaN would still reach
+// a sum of products.  Only cut tiles hold such pairs, and only a result that is not finite can
+// be touched: the kernels look at their results, and where one is not finite the block goes
+// over its tiles again this way.
+template <int DP, int N, class Seen>
+__device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf16x8 (&w)[N / 16],
                                           const uint4* tile, int l, Seen seen) {
   const int c = l & 31, h = l >> 5;
-  for (int row = 0; row < 64; ++row) {
+  for (int row = 0; row < N; ++row) {
     const int half = row >> 5, i = ((row & 31) >> 3) * 4 + (row & 3), src = (row >> 2) & 1;
     float x = 0.f;
 #pragma unroll
-    for (int n = 0; n < 32; ++n) x = n == 16 * half + i ? (float)w[n >> 3][n & 7] : x;
+    for (int n = 0; n < N / 2; ++n) x = n == 16 * half + i ? (float)w[n >> 3][n & 7] : x;
     x = __shfl(x, c + 32 * src);
     const bool in = seen(row);
 #pragma unroll
@@ -228,6 +249,21 @@ __device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf1
           acc[dt][4 * q + e] = in ? fmaf(x, (float)y[e], acc[dt][4 * q + e]) : acc[dt][4 * q + e];
       }
   }
+}
+
+// Row c of an output from accumulators that hold its columns as rows, times f.
+template <int DP>
+__device__ __forceinline__ void store_row(bf16* row, const f32x16 (&acc)[Tile<DP>::DT], float f, int d, int h) {
+#pragma unroll
+  for (int dt = 0; dt < Tile<DP>::DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (32 * dt + 8 * i >= d) continue;
+      bf16 x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (bf16)(acc[dt][4 * i + e] * f);
+      *reinterpret_cast<uint2*>(row + 32 * dt + 8 * i + 4 * h) = *reinterpret_cast<uint2*>(x);
+    }
 }
 
 }  // namespace mpipe

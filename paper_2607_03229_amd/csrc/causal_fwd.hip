@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
       if (64 * t >= wave_keys) return;
       const int stage = (t + 1) % STAGES;
       if (by_pairs.value && 64 * t >= first_cut) {
-        add_pairs<DP>(o, pb, vs[stage], l, [&](int r) { return 64 * t + r <= last_key; });
+        add_pairs<DP, 64>(o, pb, vs[stage], l, [&](int r) { return 64 * t + r <= last_key; });
         return;
       }
       const uint32_t vt = vs0 + (uint32_t)stage * SL * 16;
@@ -157,17 +157,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   sum += __shfl_xor(sum, 32);
   if (q0 + c >= a.q_len) return;
   const float inv = last_key < 0 ? 0.f : 1.0f / sum;
-  bf16* O = out_of(p.o, head, a.q_row + row) + 4 * h;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (32 * dt + 8 * i >= p.d) continue;
-      bf16 x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (bf16)(o[dt][4 * i + e] * inv);
-      *reinterpret_cast<uint2*>(O + 32 * dt + 8 * i) = *reinterpret_cast<uint2*>(x);
-    }
+  store_row<DP>(out_of(p.o, head, a.q_row + row), o, inv, p.d, h);
   if (h == 0 && p.lse) p.lse[head * p.ld_lse + a.q_row + row] = (m + log2f(sum)) * kLn2;
 }
 
