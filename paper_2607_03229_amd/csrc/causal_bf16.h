@@ -45,9 +45,17 @@ template <int DP> struct RowReads {   // rows r0 + c (r0 a multiple of 32), colu
 #pragma unroll
     for (int f = 0; f < Tile<DP>::KF; ++f) at[f] = (c * Tile<DP>::NC + ((2 * f + h) ^ swz<DP>(c))) * 16;
   }
-  __device__ __forceinline__ bf16x8 get(uint32_t tile, int r0, int f) const {
-    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
-    return *reinterpret_cast<lds_bf16x8*>(tile + at[f] + r0 * Tile<DP>::NC * 16);
+  // The place of step f in a tile, kept whole: left to itself the compiler keeps the sums of `at`
+  // and every constant over the loop, in registers that the kernels do not have.
+  __device__ __forceinline__ uint32_t base(uint32_t tile, int f) const {
+    uint32_t b = tile + at[f];
+    asm("" : "+v"(b));
+    return b;
+  }
+  __device__ __forceinline__ static bf16x8 get(uint32_t base, int r0) {
+    typedef __attribute__((address_space(3))) const char lds_char;
+    typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+    return *reinterpret_cast<lds_bf16x8*>(reinterpret_cast<lds_char*>(base) + r0 * Tile<DP>::NC * 16);
   }
 };
 // Transposed: column 32 dt + c, rows k0 + 4h .. + 3 and k0 + 8 + 4h .. + 3 (k0 a multiple of
@@ -65,12 +73,27 @@ template <int DP> struct ColReads {
         at[dt][i] = (row * Tile<DP>::NC + (chunk ^ swz<DP>(row))) * 16 + (r & 1) * 8;
       }
   }
-  __device__ __forceinline__ bf16x8 get(uint32_t tile, int k0, int dt) const {
+  struct Base {
+    uint32_t b[Tile<DP>::DT][2];
+  };
+  __device__ __forceinline__ Base base(uint32_t tile) const {
+    Base x;
+#pragma unroll
+    for (int dt = 0; dt < Tile<DP>::DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x.b[dt][i] = tile + at[dt][i];
+        asm("" : "+v"(x.b[dt][i]));
+      }
+    return x;
+  }
+  __device__ __forceinline__ static bf16x8 get(const Base& x, int k0, int dt) {
+    typedef __attribute__((address_space(3))) char lds_char;
     bf16x8 v;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          reinterpret_cast<lds_s16x4*>(tile + at[dt][i] + k0 * Tile<DP>::NC * 16));
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(
+          reinterpret_cast<lds_char*>(x.b[dt][i]) + k0 * Tile<DP>::NC * 16));
       const bf16* p = reinterpret_cast<const bf16*>(&a);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * i + e] = p[e];
@@ -107,6 +130,16 @@ __device__ __forceinline__ void load_row(RowOp<DP>& R, const bf16* row, int d, i
 
 // Sources of pad columns and of rows past the end.
 static __device__ const uint4 kZeroChunk = {0, 0, 0, 0};
+
+// A uniform number that the compiler takes as it comes.  (Stage t mod 3 of a ring, worked out in
+// sight of the reads, is spread into their addresses: more registers than there are.)
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  asm("" : "+s"(x));
+  return x;
+}
+template <int STAGES> __device__ __forceinline__ uint32_t stage_of(int t) {
+  return opaque((uint32_t)t % STAGES);
+}
 
 // Copies from memory into LDS (lane l's 16 or 4 bytes to `to` + its place), under way until
 // wait_copies.  Instructions of their own rather than the builtin: for the builtin's copies the
@@ -153,7 +186,9 @@ template <int DP, int NWV> struct PairCopy {
   __device__ __forceinline__ void copy(int i, int w, int l, uint32_t tile, const bf16* X, int rows, int d) const {
     const int s0 = slot(i, w, 0);
     if (rows < 64 || d < DP) {
-      const int s = s0 + l;
+      // (worked out here, where few tiles come: kept over the loop it would cost registers)
+      int s = s0 + l;
+      asm volatile("" : "+v"(s));
       const char* from = reinterpret_cast<const char*>(X) + off[i];
       if (row(s) >= rows || col(s) >= d) from = reinterpret_cast<const char*>(&kZeroChunk);
       copy16(tile + 16 * s0, from);

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
   auto issue = [&](int t) __attribute__((always_inline)) {
     if (t >= nt) return;
-    const uint32_t stage = (uint32_t)(t % STAGES) * SL * 16;
+    const uint32_t stage = stage_of<STAGES>(t) * (SL * 16);
 #pragma unroll
     for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
       const bool of_k = copy.of_x(i, w);
@@ -80,20 +80,18 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     // step u: keys 32u .. 32u + 31
     auto scores = [&](int u) __attribute__((always_inline)) {
       if (32 * u >= wave_keys) return;
-      const uint32_t stage = (uint32_t)((u >> 1) % STAGES) * SL * 16 + 32 * (u & 1) * T::NC * 16;
-      s = zero16();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) dp[i] = nd;
+      const uint32_t stage = stage_of<STAGES>(u >> 1) * (SL * 16) + 32 * (u & 1) * T::NC * 16;
+      s = dp = zero16();
 #pragma unroll
       for (int f = 0; f < T::KF; ++f) {
-        s = mfma(rread.get(ks0 + stage, 0, f), q.f[f], s);
-        dp = mfma(rread.get(vs0 + stage, 0, f), d_o.f[f], dp);
+        s = mfma(rread.get(rread.base(ks0 + stage, f), 0), q.f[f], s);
+        dp = mfma(rread.get(rread.base(vs0 + stage, f), 0), d_o.f[f], dp);
       }
     };
     auto slopes = [&](int u) __attribute__((always_inline)) {
       if (32 * u >= wave_keys) return;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = exp2_fast(fmaf(s[i], sl2, nl2)) * dp[i];
+      for (int i = 0; i < 16; ++i) s[i] = exp2_fast(fmaf(s[i], sl2, nl2)) * (dp[i] + nd);
       if (32 * u >= first_cut) {
         const int lim = last_key - 32 * u - 4 * h;
 #pragma unroll
@@ -104,17 +102,17 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     };
     auto sums = [&](int u) __attribute__((always_inline)) {
       if (32 * u >= wave_keys) return;
-      const int stage = (u >> 1) % STAGES;
+      const uint32_t stage = stage_of<STAGES>(u >> 1);
       if (by_pairs.value && 32 * u >= first_cut) {
         add_pairs<DP, 32>(dq, ds, ks[stage] + 32 * (u & 1) * T::NC, l,
                           [&](int r) { return 32 * u + r <= last_key; });
         return;
       }
-      const uint32_t kt = ks0 + (uint32_t)stage * SL * 16 + 32 * (u & 1) * T::NC * 16;
+      const auto at = cread.base(ks0 + stage * (SL * 16) + 32 * (u & 1) * T::NC * 16);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) dq[dt] = mfma(cread.get(kt, 16 * j, dt), ds[j], dq[dt]);
+        for (int dt = 0; dt < DT; ++dt) dq[dt] = mfma(cread.get(at, 16 * j, dt), ds[j], dq[dt]);
     };
     // Slots as in the forward, two steps to a tile.  Tile x is read first by the early group in slot
     // 4x - 1 and last by the late one in slot 4x + 4; it is sent for in slots 4x - 4 and 4x - 3, and
@@ -186,10 +184,11 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   const uint32_t rows0 = second ? lds_at(ds_) : lds_at(qs), cols0 = second ? lds_at(qs) : lds_at(ds_);
   auto issue = [&](int t) __attribute__((always_inline)) {
     if (t >= nt) return;
-    const int head = a.head_k * p.group + t / n_tiles, r0 = 64 * (t0 + t % n_tiles), stage = t % STAGES;
+    const int head = a.head_k * p.group + t / n_tiles, r0 = 64 * (t0 + t % n_tiles);
+    const uint32_t stage = stage_of<STAGES>(t);
     const bf16* Q = head_of(p.q, head, a.q_row) + r0 * p.q.row;
     const bf16* dO = head_of(p.d_o, head, a.q_row) + r0 * p.d_o.row;
-    const uint32_t at = (uint32_t)stage * SL * 16;
+    const uint32_t at = stage * (SL * 16);
 #pragma unroll
     for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
       const bool of_q = copy.of_x(i, w);
@@ -213,8 +212,8 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
     auto cut = [&](int r0) { return r0 < whole_q || r0 + 64 > a.q_len; };
     auto products = [&](int t) __attribute__((always_inline)) {
       if (idle(q_of(t))) return;
-      const int stage = t % STAGES;
-      const uint32_t tile = rows0 + (uint32_t)stage * SL * 16;
+      const uint32_t stage = stage_of<STAGES>(t);
+      const uint32_t tile = rows0 + stage * (SL * 16);
 #pragma unroll
       for (int q2 = 0; q2 < 2; ++q2) {
         if (second) {
@@ -229,15 +228,19 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
         } else {
           s[q2] = zero16();
         }
+      }
 #pragma unroll
-        for (int f = 0; f < T::KF; ++f) s[q2] = mfma(rread.get(tile, 32 * q2, f), kv.f[f], s[q2]);
+      for (int f = 0; f < T::KF; ++f) {
+        const uint32_t at = rread.base(tile, f);
+#pragma unroll
+        for (int q2 = 0; q2 < 2; ++q2) s[q2] = mfma(rread.get(at, 32 * q2), kv.f[f], s[q2]);
       }
     };
     auto form = [&](int t) __attribute__((always_inline)) {
       const int r0 = q_of(t);
       if (idle(r0)) return;
       if (!second) {
-        const float* nl2 = nl2s[t % STAGES];
+        const float* nl2 = nl2s[stage_of<STAGES>(t)];
 #pragma unroll
         for (int q2 = 0; q2 < 2; ++q2)
 #pragma unroll
@@ -276,18 +279,19 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
       }
     };
     auto sums = [&](int t) __attribute__((always_inline)) {
-      const int r0 = q_of(t), stage = t % STAGES;
+      const int r0 = q_of(t);
       if (idle(r0)) return;
+      const uint32_t stage = stage_of<STAGES>(t);
       if (by_pairs.value && cut(r0)) {
         add_pairs<DP, 64>(acc, x, second ? qs[stage] : ds_[stage], l,
                           [&](int r) { return r0 + r >= first_q && r0 + r < a.q_len; });
         return;
       }
-      const uint32_t tile = cols0 + (uint32_t)stage * SL * 16;
+      const auto at = cread.base(cols0 + stage * (SL * 16));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma(cread.get(tile, 16 * j, dt), x[j], acc[dt]);
+        for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma(cread.get(at, 16 * j, dt), x[j], acc[dt]);
     };
     // The first waves form P of tile t in slot 2t and multiply in slot 2t + 1, the second ones a slot
     // later.  Tile x is read from slot 2x - 1 to slot 2x + 2, sent for in slot 2x - 3 and waited

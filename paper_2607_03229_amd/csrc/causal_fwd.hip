@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
   // pair t: tile t of K and tile t - 1 of V, in stage t mod 3
   auto issue = [&](int t) __attribute__((always_inline)) {
-    const uint32_t stage = (uint32_t)(t % STAGES) * SL * 16;
+    const uint32_t stage = stage_of<STAGES>(t) * (SL * 16);
 #pragma unroll
     for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
       const bool of_k = copy.of_x(i, w);
@@ -65,12 +65,13 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
     bf16x8 pb[4];
     auto scores = [&](int t) __attribute__((always_inline)) {
       if (64 * t >= wave_keys) return;
-      const uint32_t kt = ks0 + (uint32_t)(t % STAGES) * SL * 16;
+      const uint32_t kt = ks0 + stage_of<STAGES>(t) * (SL * 16);
+      s[0] = s[1] = zero16();
 #pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) {
-        s[k2] = zero16();
+      for (int f = 0; f < T::KF; ++f) {
+        const uint32_t at = kread.base(kt, f);
 #pragma unroll
-        for (int f = 0; f < T::KF; ++f) s[k2] = mfma(kread.get(kt, 32 * k2, f), q.f[f], s[k2]);
+        for (int k2 = 0; k2 < 2; ++k2) s[k2] = mfma(kread.get(at, 32 * k2), q.f[f], s[k2]);
       }
     };
     auto softmax = [&](int t) __attribute__((always_inline)) {
@@ -112,16 +113,16 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
     };
     auto values = [&](int t) __attribute__((always_inline)) {
       if (64 * t >= wave_keys) return;
-      const int stage = (t + 1) % STAGES;
+      const uint32_t stage = stage_of<STAGES>(t + 1);
       if (by_pairs.value && 64 * t >= first_cut) {
         add_pairs<DP, 64>(o, pb, vs[stage], l, [&](int r) { return 64 * t + r <= last_key; });
         return;
       }
-      const uint32_t vt = vs0 + (uint32_t)stage * SL * 16;
+      const auto at = vread.base(vs0 + stage * (SL * 16));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma(vread.get(vt, 16 * j, dt), pb[j], o[dt]);
+        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma(vread.get(at, 16 * j, dt), pb[j], o[dt]);
     };
     // The early group's softmax of tile t meets the late group's products of tile t - 1 in a
     // slot, and the other way round in the next: the matrix and the vector units work at once.
