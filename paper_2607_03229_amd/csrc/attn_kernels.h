@@ -44,12 +44,12 @@ hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStre
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
 
-// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip): items of
-// so many rows.  dq writes to `delta` what dkdv reads: -lse * log2(e), then -dO . O.
-constexpr int kForwardRows = 256, kBackwardQRows = 256, kBackwardKRows = 128;
-hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
-hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s);
-hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s);
+// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip), in blocks of
+// 8 or 4 waves: items of 32 queries a wave, and for dkdv of 16 keys a wave.  dq writes to
+// `delta` what dkdv reads: -lse * log2(e), then -dO . O.
+hipError_t causal_bf16_fwd(const CausalArgs& a, int items, int waves, hipStream_t s);
+hipError_t causal_bf16_dq(const CausalArgs& a, int items, int waves, hipStream_t s);
+hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s);
 
 struct CacheRows {   // rows on their way into or out of a cache
   mpipe_kv_cache cache;

@@ -128,73 +128,96 @@ __device__ __forceinline__ void load_row(RowOp<DP>& R, const bf16* row, int d, i
   }
 }
 
-// Sources of pad columns and of rows past the end.
-static __device__ const uint4 kZeroChunk = {0, 0, 0, 0};
+// Places of the three stages of a ring, bytes: of tile t + 1, t + 2 and t + 3 (which is t's).
+// (t mod 3 in sight of the reads would be spread into their addresses: more registers than there
+// are.)
+struct Ring {
+  uint32_t a, b, c;
+  __device__ __forceinline__ void start(uint32_t bytes) {
+    a = bytes;
+    b = 2 * bytes;
+    c = 0;
+    asm("" : "+s"(a), "+s"(b), "+s"(c));
+  }
+  __device__ __forceinline__ void next() {
+    const uint32_t x = a;
+    a = b;
+    b = c;
+    c = x;
+  }
+};
+// The larger of the values that lanes l and l ^ 32 hold, and their sum: one exchange of the
+// halves of a wave in the vector unit.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
-// A uniform number that the compiler takes as it comes.  (Stage t mod 3 of a ring, worked out in
-// sight of the reads, is spread into their addresses: more registers than there are.)
-__device__ __forceinline__ uint32_t opaque(uint32_t x) {
-  asm("" : "+s"(x));
-  return x;
-}
-template <int STAGES> __device__ __forceinline__ uint32_t stage_of(int t) {
-  return opaque((uint32_t)t % STAGES);
-}
+// The tiles of one tensor's rows in order, as buffers: what lies past a tensor's last row, and a
+// place that no buffer has (kNowhere), are read as zeros, and a tile past the last as nothing else.
+typedef __attribute__((ext_vector_type(4))) uint32_t buffer_t;
+constexpr uint32_t kNowhere = 0x80000000u;
+struct Feed {
+  uint64_t base, step;   // the next tile's first row, and from tile to tile
+  uint32_t tail;         // bytes of the last tile
+  int left;              // tiles, from the next one to the last
+  __device__ __forceinline__ void start(const bf16* X, int64_t ld, int first, int rows, int d) {
+    base = (uint64_t)(X + 64 * first * ld);
+    step = 128 * (uint64_t)ld;
+    left = (rows + 63) / 64 - first;
+    tail = (uint32_t)(2 * ((rows - 1) % 64 * ld + d));
+  }
+  __device__ __forceinline__ buffer_t next() {
+    const buffer_t b = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffff,
+                        left > 1 ? 0x7fffffffu : left == 1 ? tail : 0u, 0x00027000u};
+    base += step;
+    --left;
+    return b;
+  }
+};
 
-// Copies from memory into LDS (lane l's 16 or 4 bytes to `to` + its place), under way until
-// wait_copies.  Instructions of their own rather than the builtin: for the builtin's copies the
-// compiler puts a wait before every transposing read, whose LDS it cannot tell from theirs.  They
-// write no register, and read theirs as they are issued.
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :: "s"(to), "v"(from) : "memory", "m0");
+// Copies from a buffer into LDS (lane l's 16 bytes to `to` + 16 l), under way until wait_copies.
+// An instruction of its own rather than the builtin: for the builtin's copies the compiler puts
+// a wait before every transposing read, whose LDS it cannot tell from theirs.  It writes no
+// register, and reads its own as it is issued.
+__device__ __forceinline__ void copy16(uint32_t to, uint32_t off, const buffer_t& from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(to), "v"(off), "s"(from) : "m0");
 }
-__device__ __forceinline__ void copy16(uint32_t to, const void* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(to), "v"(off), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void copy4(uint32_t to, const void* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-               :: "s"(to), "v"(from) : "memory", "m0");
+__device__ __forceinline__ void copy4(uint32_t to, uint32_t off, const buffer_t& from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :: "s"(to), "v"(off), "s"(from) : "m0");
 }
 
 // Wave w of NWV waves copies its share of a pair of tiles (x, then y): wave instruction j = w,
-// NWV + w, ... of 2 NC, each 64 slots.  A lane's source is a 32-bit distance from the tile's first
-// row: 64 rows of a view are less than 2^31 bytes.
+// NWV + w, ... of 2 NC, each 64 slots.  64 rows of a view are less than 2^31 bytes.
 template <int DP, int NWV> struct PairCopy {
   static constexpr int NC = Tile<DP>::NC, N = 2 * NC / NWV;
   static_assert(2 * NC % NWV == 0, "whole instructions for every wave");
-  uint32_t off[N];
+  uint32_t off[N];   // of the lane's slot in each, bytes from the tile's first row
   __device__ __forceinline__ static bool of_x(int i, int w) {
     if constexpr (NC % NWV == 0) return i < NC / NWV;
     else return i * NWV + w < NC;
   }
-  __device__ __forceinline__ static int slot(int i, int w, int l) {
+  __device__ __forceinline__ static int slot(int i, int w) {
     const int j = i * NWV + w;
-    return (of_x(i, w) ? j : j - NC) * 64 + l;
+    return (of_x(i, w) ? j : j - NC) * 64;
   }
-  __device__ __forceinline__ static int row(int s) { return s / NC; }
-  __device__ __forceinline__ static int col(int s) { return 8 * (s % NC ^ swz<DP>(s / NC)); }
-  __device__ __forceinline__ void init(int w, int l, int64_t ld_x, int64_t ld_y) {
+  __device__ __forceinline__ void init(int w, int l, int64_t ld_x, int64_t ld_y, int d) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int s = slot(i, w, l);
-      off[i] = 2 * (uint32_t)(row(s) * (of_x(i, w) ? ld_x : ld_y) + col(s));
+      const int s = slot(i, w) + l, row = s / NC, col = 8 * (s % NC ^ swz<DP>(row));
+      off[i] = col < d ? 2 * (uint32_t)(row * (of_x(i, w) ? ld_x : ld_y) + col) : kNowhere;
     }
   }
-  // Share i into `tile`, from rows X.. of which `rows` (any number) exist and d columns.
-  __device__ __forceinline__ void copy(int i, int w, int l, uint32_t tile, const bf16* X, int rows, int d) const {
-    const int s0 = slot(i, w, 0);
-    if (rows < 64 || d < DP) {
-      // (worked out here, where few tiles come: kept over the loop it would cost registers)
-      int s = s0 + l;
-      asm volatile("" : "+v"(s));
-      const char* from = reinterpret_cast<const char*>(X) + off[i];
-      if (row(s) >= rows || col(s) >= d) from = reinterpret_cast<const char*>(&kZeroChunk);
-      copy16(tile + 16 * s0, from);
-    } else {
-      copy16(tile + 16 * s0, X, off[i]);
-    }
+  __device__ __forceinline__ void copy(int w, uint32_t x, uint32_t y, const buffer_t& from_x, const buffer_t& from_y) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      copy16((of_x(i, w) ? x : y) + 16 * slot(i, w), off[i], of_x(i, w) ? from_x : from_y);
   }
 };
 
@@ -204,7 +227,14 @@ template <int n> __device__ __forceinline__ void wait_copies() {
   static_assert(n >= 0 && n < 64, "vmcnt");
   __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | (((n >> 4) & 3) << 14));
 }
-// A barrier that waits for the wave's LDS reads, not for copies under way.
+// The same, and until at most m of its LDS operations are.
+template <int n, int m> __device__ __forceinline__ void wait_copies_and_writes() {
+  static_assert(n >= 0 && n < 64 && m >= 0 && m < 16, "vmcnt, lgkmcnt");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (m << 8) | (((n >> 4) & 3) << 14));
+}
+// A barrier that waits for nothing of the wave's own.
+__device__ __forceinline__ void bare_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// A barrier that waits for the wave's LDS reads and writes, not for copies under way.
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
   asm volatile("s_barrier" ::: "memory");
@@ -219,6 +249,21 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& s, int j) {
   for (int e = 0; e < 8; ++e) r[e] = (bf16)s[8 * j + e];
   return r;
 }
+// Order of a stretch of products whose operands come from LDS: `ahead` reads first, then with each
+// product the reads of one that is `ahead` reads later.  One wave of a SIMD reads at a time and a
+// read takes a few hundred cycles, so the compiler's own order, a few reads ahead, left the
+// matrix unit idle half of the time.
+template <int N, int READS> __device__ __forceinline__ void order_step() {
+  if constexpr (N > 0) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // MFMA
+    if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);   // LDS reads
+    order_step<N - 1, READS>();
+  }
+}
+template <int READS> __device__ __forceinline__ void order_reads() {
+  __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+}
+
 template <int N> __device__ __forceinline__ bool finite16(const f32x16 (&acc)[N]) {
   float z = 0.f;
 #pragma unroll

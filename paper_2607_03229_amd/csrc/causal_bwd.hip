@@ -7,28 +7,27 @@
 namespace mpipe {
 namespace {
 
-constexpr int NWV = 8;
-constexpr int STAGES = 3;
+constexpr int STAGES = 3, KSTAGES = 4;   // of tiles of dQ, and of dK and dV
 
 // ---- dQ -----------------------------------------------------------------------------------
 // A wave has 32 queries, one per column: S^T = K Q^T and dP^T = V dO^T over 32 keys, dS^T from
 // both, dQ^T += K^T dS^T.  Half of the waves run their products while the others form dS.
 // Also writes what the other kernel needs of every query: -lse * log2(e), and -dO . O.
-template <int DP>
+template <int DP, int NWV>
 __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
   using T = Tile<DP>;
   constexpr int SL = T::SLOTS, DT = T::DT;
   __shared__ uint4 ks[STAGES][SL], vs[STAGES][SL];
-  const AttnPlace a = attn_place(p, p.group, kBackwardQRows);
+  const AttnPlace a = attn_place(p, p.group, 32 * NWV);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int c = l & 31, h = l >> 5;
-  const bool late = w >= NWV / 2;
+  const bool late = NWV == 8 && w >= NWV / 2;
   const int head = a.head_k * p.group + a.gq, shift = a.k_len - a.q_len;
   const int q0 = a.r0 + 32 * w, row = min(q0 + c, a.q_len - 1);
   const int last_key = row + shift;
   const int wave_keys = q0 < a.q_len ? min(q0 + 31, a.q_len - 1) + shift + 1 : 0;
   const int first_cut = (q0 + shift + 1) & ~31;
-  const int keys = min(a.r0 + kBackwardQRows - 1, a.q_len - 1) + shift + 1;
+  const int keys = min(a.r0 + 32 * NWV - 1, a.q_len - 1) + shift + 1;
   const int nt = keys > 0 ? (keys + 63) / 64 : 0;
   const bf16* K = head_of(p.k, a.head_k, a.k_row);
   const bf16* V = head_of(p.v, a.head_k, a.k_row);
@@ -45,7 +44,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     for (int f = 0; f < T::KF; ++f)
 #pragma unroll
       for (int e = 0; e < 8; ++e) nd = fmaf((float)o.f[f][e], -(float)d_o.f[f][e], nd);
-    nd += __shfl_xor(nd, 32);
+    nd = add_halves(nd);
   }
   const float nl2 = -p.lse[head * p.ld_lse + a.q_row + row] * kLog2e;
   if (h == 0 && q0 + c < a.q_len) {
@@ -54,38 +53,39 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     out[(int64_t)p.heads_k * p.group * p.rows_q] = nd;
   }
   PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.k.row, p.v.row);
+  copy.init(w, l, p.k.row, p.v.row, p.d);
   RowReads<DP> rread;
   rread.init(c, h);
   ColReads<DP> cread;
   cread.init(l);
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    if (t >= nt) return;
-    const uint32_t stage = stage_of<STAGES>(t) * (SL * 16);
-#pragma unroll
-    for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
-      const bool of_k = copy.of_x(i, w);
-      copy.copy(i, w, l, (of_k ? ks0 : vs0) + stage, (of_k ? K : V) + 64 * t * (of_k ? p.k.row : p.v.row),
-                a.k_len - 64 * t, p.d);
-    }
-  };
-
+  constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // row reads before their products begin
   f32x16 dq[DT];
   auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt] = zero16();
+    Feed kf, vf;
+    kf.start(K, p.k.row, 0, min(a.k_len, 64 * nt), p.d);
+    vf.start(V, p.v.row, 0, min(a.k_len, 64 * nt), p.d);
+    auto issue = [&](uint32_t stage) __attribute__((always_inline)) {
+      copy.copy(w, ks0 + stage, vs0 + stage, kf.next(), vf.next());
+    };
     f32x16 s, dp;
-    bf16x8 ds[2];
-    // step u: keys 32u .. 32u + 31
-    auto scores = [&](int u) __attribute__((always_inline)) {
-      if (32 * u >= wave_keys) return;
-      const uint32_t stage = stage_of<STAGES>(u >> 1) * (SL * 16) + 32 * (u & 1) * T::NC * 16;
+    bf16x8 ds[2], first[AHEAD];
+    // step u: keys 32u .. 32u + 31, half a tile, at `at` in the rings
+    auto fetch = [&](uint32_t at) __attribute__((always_inline)) {
+#pragma unroll
+      for (int f = 0; f < AHEAD / 2; ++f) {
+        first[2 * f] = rread.get(rread.base(ks0 + at, f), 0);
+        first[2 * f + 1] = rread.get(rread.base(vs0 + at, f), 0);
+      }
+    };
+    auto scores = [&](uint32_t at) __attribute__((always_inline)) {
       s = dp = zero16();
 #pragma unroll
       for (int f = 0; f < T::KF; ++f) {
-        s = mfma(rread.get(rread.base(ks0 + stage, f), 0), q.f[f], s);
-        dp = mfma(rread.get(rread.base(vs0 + stage, f), 0), d_o.f[f], dp);
+        s = mfma(f < AHEAD / 2 ? first[2 * f] : rread.get(rread.base(ks0 + at, f), 0), q.f[f], s);
+        dp = mfma(f < AHEAD / 2 ? first[2 * f + 1] : rread.get(rread.base(vs0 + at, f), 0), d_o.f[f], dp);
       }
     };
     auto slopes = [&](int u) __attribute__((always_inline)) {
@@ -100,44 +100,66 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
       ds[0] = pack8(s, 0);
       ds[1] = pack8(s, 1);
     };
-    auto sums = [&](int u) __attribute__((always_inline)) {
-      if (32 * u >= wave_keys) return;
-      const uint32_t stage = stage_of<STAGES>(u >> 1);
-      if (by_pairs.value && 32 * u >= first_cut) {
-        add_pairs<DP, 32>(dq, ds, ks[stage] + 32 * (u & 1) * T::NC, l,
-                          [&](int r) { return 32 * u + r <= last_key; });
+    // scores of step u + 1 at `next`, sums of step u at `at`; with the first step of a tile, the
+    // tile after the next into `then`
+    auto products = [&](int u, uint32_t at, uint32_t next, uint32_t then, auto sends) __attribute__((always_inline)) {
+      if (32 * u >= wave_keys) {
+        if constexpr (sends.value) issue(then);
         return;
       }
-      const auto at = cread.base(ks0 + stage * (SL * 16) + 32 * (u & 1) * T::NC * 16);
+      scores(next);   // (past the wave's last step: of whatever lies there, for nobody)
+      if constexpr (sends.value) issue(then);
+      if (by_pairs.value && 32 * u >= first_cut) {
+        add_pairs<DP, 32>(dq, ds, &ks[0][0] + at / 16, l, [&](int r) { return 32 * u + r <= last_key; });
+        return;
+      }
+      const auto cols = cread.base(ks0 + at);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) dq[dt] = mfma(cread.get(at, 16 * j, dt), ds[j], dq[dt]);
+        for (int dt = 0; dt < DT; ++dt) dq[dt] = mfma(cread.get(cols, 16 * j, dt), ds[j], dq[dt]);
+      if constexpr (!by_pairs.value) {
+        // 2 KF products of scores, the first AHEAD of them fetched; 4 DT half reads and 2 DT sums
+        constexpr int REST = 2 * T::KF - AHEAD, EACH = (4 * DT + AHEAD - 1) / AHEAD;
+        order_step<REST, 1>();
+        order_step<AHEAD, EACH>();
+        order_step<2 * DT, 0>();
+      }
     };
-    // Slots as in the forward, two steps to a tile.  Tile x is read first by the early group in slot
-    // 4x - 1 and last by the late one in slot 4x + 4; it is sent for in slots 4x - 4 and 4x - 3, and
-    // waited for by the end of slot 4x - 2.
-    issue(0);
+    // Slots as in the forward, two steps to a tile.  Tile x is first read in the early group's slot
+    // 4x - 2 (the operands fetched ahead) and last in the late group's 4x + 4; it is sent for in the
+    // products of step 2x - 4, slots 4x - 7 and 4x - 6, and has arrived by the end of slot 4x - 3.
+    constexpr uint32_t HALF = 32 * T::NC * 16;
+    Ring ring;   // c: tile t
+    ring.start(SL * 16);
+    issue(ring.c);
+    issue(ring.a);
     wait_copies<0>();
     lds_barrier();
-    scores(0);
-    if (late) lds_barrier();
-    for (int t = 0; t < nt; ++t)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int u = 2 * t + b;
-        if (b == 0) issue(t + 1);
-        slopes(u);
-        if (b == 1 && !late) wait_copies<0>();
-        lds_barrier();
-        __builtin_amdgcn_s_setprio(1);
-        if (u + 1 < 2 * nt) scores(u + 1);
-        sums(u);
-        __builtin_amdgcn_s_setprio(0);
-        if (b == 0 && late) wait_copies<0>();
-        lds_barrier();
-      }
-    if (!late) lds_barrier();
+    if (wave_keys > 0) {
+      fetch(ring.c);
+      scores(ring.c);
+    }
+    if (late) bare_barrier();
+    for (int t = 0; t < nt; ++t) {
+      slopes(2 * t);
+      fetch(ring.c + HALF);
+      wait_copies<0>();
+      bare_barrier();
+      __builtin_amdgcn_s_setprio(1);
+      products(2 * t, ring.c, ring.c + HALF, ring.b, std::true_type());
+      __builtin_amdgcn_s_setprio(0);
+      bare_barrier();
+      slopes(2 * t + 1);
+      fetch(ring.a);
+      bare_barrier();
+      __builtin_amdgcn_s_setprio(1);
+      products(2 * t + 1, ring.c + HALF, ring.a, 0, std::false_type());
+      __builtin_amdgcn_s_setprio(0);
+      bare_barrier();
+      ring.next();
+    }
+    if (NWV == 8 && !late) bare_barrier();
   };
   walk(std::false_type());
   // a pair that does not count must not reach the sum: see add_pairs
@@ -153,16 +175,16 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
 // dK^T += Q^T dS.  Neither holds more than one accumulator of head_dim columns, one operand and
 // one tile of scores, so two waves fit a SIMD; they run on the same one (w and w + 4), and one's
 // products meet the other's exponentials.
-template <int DP>
+template <int DP, int NWV>
 __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) {
   using T = Tile<DP>;
   constexpr int SL = T::SLOTS, DT = T::DT;
-  __shared__ uint4 qs[STAGES][SL], ds_[STAGES][SL];
+  __shared__ uint4 qs[KSTAGES][SL], ds_[KSTAGES][SL];
   __shared__ uint4 weights[NWV / 2][4][64];      // P of one tile, bf16, as the lanes hold it
-  __shared__ __attribute__((aligned(16))) float nl2s[STAGES][64], nds[STAGES][64];
-  const AttnPlace a = attn_place(p, 1, kBackwardKRows);
+  __shared__ __attribute__((aligned(16))) float nl2s[KSTAGES][64], nds[KSTAGES][64];
+  const AttnPlace a = attn_place(p, 1, 16 * NWV);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
-  const int c = l & 31, h = l >> 5, pair = w & 3;
+  const int c = l & 31, h = l >> 5, pair = w % (NWV / 2);
   const bool second = w >= NWV / 2;
   const int shift = a.k_len - a.q_len;
   const int k0 = a.r0 + 32 * pair, row = min(k0 + c, a.k_len - 1);
@@ -175,83 +197,86 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   RowOp<DP> kv;
   load_row<DP>(kv, head_of(second ? p.v : p.k, a.head_k, a.k_row + row), p.d, h);
   PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.q.row, p.d_o.row);
+  copy.init(w, l, p.q.row, p.d_o.row, p.d);
   RowReads<DP> rread;
   rread.init(c, h);
   ColReads<DP> cread;
   cread.init(l);
   // the first wave's rows are of Q and columns of dO, the second's the other way round
   const uint32_t rows0 = second ? lds_at(ds_) : lds_at(qs), cols0 = second ? lds_at(qs) : lds_at(ds_);
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    if (t >= nt) return;
-    const int head = a.head_k * p.group + t / n_tiles, r0 = 64 * (t0 + t % n_tiles);
-    const uint32_t stage = stage_of<STAGES>(t);
-    const bf16* Q = head_of(p.q, head, a.q_row) + r0 * p.q.row;
-    const bf16* dO = head_of(p.d_o, head, a.q_row) + r0 * p.d_o.row;
-    const uint32_t at = stage * (SL * 16);
-#pragma unroll
-    for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
-      const bool of_q = copy.of_x(i, w);
-      copy.copy(i, w, l, (of_q ? lds_at(qs) : lds_at(ds_)) + at, of_q ? Q : dO, a.q_len - r0, p.d);
-    }
-    if (pair == 0) {
-      const float* X = p.delta + (int64_t)head * p.rows_q + a.q_row + min(r0 + l, a.q_len - 1);
-      if (second) X += (int64_t)p.heads_k * p.group * p.rows_q;
-      copy4(lds_at(second ? nds[stage] : nl2s[stage]), X);
-    }
-  };
-
+  constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // row reads before their products begin
   f32x16 acc[DT];
   auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
+    // tiles head by head: Q, dO, and of each query -lse * log2(e) (the first waves') or -dO . O
+    Feed qf, of;
+    uint64_t stats = 0;
+    int sent = 0;   // heads begun
+    uint32_t stage_sent = 0;
+    qf.left = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+      if (qf.left <= 0) {   // the next head, or past the last one nothing
+        const int head = a.head_k * p.group + min(sent, p.group - 1);
+        const bool more = sent < p.group && n_tiles > 0;
+        qf.start(head_of(p.q, head, a.q_row), p.q.row, t0, a.q_len, p.d);
+        of.start(head_of(p.d_o, head, a.q_row), p.d_o.row, t0, a.q_len, p.d);
+        if (!more) qf.left = of.left = 0;
+        stats = (uint64_t)(p.delta + ((second ? (int64_t)p.heads_k * p.group : 0) + head) * p.rows_q + a.q_row + 64 * t0);
+        ++sent;
+      }
+      const uint32_t n = qf.left > 1 ? 256u : qf.left == 1 ? 4u * (uint32_t)((a.q_len - 1) % 64 + 1) : 0u;
+      copy.copy(w, lds_at(qs) + stage_sent * (SL * 16), lds_at(ds_) + stage_sent * (SL * 16), qf.next(), of.next());
+      if (pair == 0)
+        copy4((second ? lds_at(nds) : lds_at(nl2s)) + 256 * stage_sent, 4 * l,
+              buffer_t{(uint32_t)stats, (uint32_t)(stats >> 32) & 0xffff, n, 0x00027000u});
+      stats += 256;
+      stage_sent = (stage_sent + 1) % KSTAGES;
+    };
     f32x16 s[2];
-    bf16x8 x[4];
-    auto q_of = [&](int t) { return 64 * (t0 + t % n_tiles); };
+    bf16x8 x[4], first[AHEAD];
+    int tile_t = 0;   // tile t's place among those of its head
     auto idle = [&](int r0) { return r0 + 63 < wave_q; };   // no query of the tile sees a key here
     auto cut = [&](int r0) { return r0 < whole_q || r0 + 64 > a.q_len; };
-    auto products = [&](int t) __attribute__((always_inline)) {
-      if (idle(q_of(t))) return;
-      const uint32_t stage = stage_of<STAGES>(t);
-      const uint32_t tile = rows0 + stage * (SL * 16);
+    auto fetch = [&](uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int q2 = 0; q2 < 2; ++q2) {
-        if (second) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(&nds[stage][32 * q2 + 8 * i + 4 * h]);
-            s[q2][4 * i] = v.x;
-            s[q2][4 * i + 1] = v.y;
-            s[q2][4 * i + 2] = v.z;
-            s[q2][4 * i + 3] = v.w;
-          }
-        } else {
-          s[q2] = zero16();
-        }
-      }
-#pragma unroll
-      for (int f = 0; f < T::KF; ++f) {
-        const uint32_t at = rread.base(tile, f);
-#pragma unroll
-        for (int q2 = 0; q2 < 2; ++q2) s[q2] = mfma(rread.get(at, 32 * q2), kv.f[f], s[q2]);
+      for (int f = 0; f < AHEAD / 2; ++f) {
+        const uint32_t b = rread.base(rows0 + at, f);
+        first[2 * f] = rread.get(b, 0);
+        first[2 * f + 1] = rread.get(b, 32);
       }
     };
-    auto form = [&](int t) __attribute__((always_inline)) {
-      const int r0 = q_of(t);
+    auto scores = [&](uint32_t at) __attribute__((always_inline)) {
+      s[0] = s[1] = zero16();
+#pragma unroll
+      for (int f = 0; f < AHEAD / 2; ++f)
+#pragma unroll
+        for (int q2 = 0; q2 < 2; ++q2) s[q2] = mfma(first[2 * f + q2], kv.f[f], s[q2]);
+#pragma unroll
+      for (int f = AHEAD / 2; f < T::KF; ++f) {
+        const uint32_t b = rread.base(rows0 + at, f);
+#pragma unroll
+        for (int q2 = 0; q2 < 2; ++q2) s[q2] = mfma(rread.get(b, 32 * q2), kv.f[f], s[q2]);
+      }
+    };
+    auto form = [&](int r0, int stage) __attribute__((always_inline)) {
       if (idle(r0)) return;
-      if (!second) {
-        const float* nl2 = nl2s[stage_of<STAGES>(t)];
+      const float* stats = second ? nds[stage] : nl2s[stage];
 #pragma unroll
-        for (int q2 = 0; q2 < 2; ++q2)
+      for (int q2 = 0; q2 < 2; ++q2)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(&nl2[32 * q2 + 8 * i + 4 * h]);
-            s[q2][4 * i] = exp2_fast(fmaf(s[q2][4 * i], sl2, v.x));
-            s[q2][4 * i + 1] = exp2_fast(fmaf(s[q2][4 * i + 1], sl2, v.y));
-            s[q2][4 * i + 2] = exp2_fast(fmaf(s[q2][4 * i + 2], sl2, v.z));
-            s[q2][4 * i + 3] = exp2_fast(fmaf(s[q2][4 * i + 3], sl2, v.w));
+        for (int i = 0; i < 4; ++i) {
+          const float4 v = *reinterpret_cast<const float4*>(&stats[32 * q2 + 8 * i + 4 * h]);
+          const float n[4] = {v.x, v.y, v.z, v.w};
+          if (second) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[q2][4 * i + e] += n[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[q2][4 * i + e] = exp2_fast(fmaf(s[q2][4 * i + e], sl2, n[e]));
           }
-      } else {
+        }
+      if (second) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 v = weights[pair][j][l];
@@ -278,44 +303,57 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
         for (int j = 0; j < 4; ++j) weights[pair][j][l] = *reinterpret_cast<const uint4*>(&x[j]);
       }
     };
-    auto sums = [&](int t) __attribute__((always_inline)) {
-      const int r0 = q_of(t);
+    // scores of the next tile, sums of this one
+    auto products = [&](int r0, uint32_t at, uint32_t next) __attribute__((always_inline)) {
+      scores(next);   // (past the last tile: of whatever lies there, for nobody)
+      issue();
       if (idle(r0)) return;
-      const uint32_t stage = stage_of<STAGES>(t);
       if (by_pairs.value && cut(r0)) {
-        add_pairs<DP, 64>(acc, x, second ? qs[stage] : ds_[stage], l,
+        add_pairs<DP, 64>(acc, x, (second ? &qs[0][0] : &ds_[0][0]) + at / 16, l,
                           [&](int r) { return r0 + r >= first_q && r0 + r < a.q_len; });
         return;
       }
-      const auto at = cread.base(cols0 + stage * (SL * 16));
+      const auto cols = cread.base(cols0 + at);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma(cread.get(at, 16 * j, dt), x[j], acc[dt]);
+        for (int dt = 0; dt < DT; ++dt) acc[dt] = mfma(cread.get(cols, 16 * j, dt), x[j], acc[dt]);
+      if constexpr (!by_pairs.value) {
+        // 2 KF products of scores, the first AHEAD of them fetched; 8 DT half reads and 4 DT sums
+        constexpr int REST = 2 * T::KF - AHEAD, LATER = 8 * DT - 2 * AHEAD;
+        order_step<REST, 1>();
+        order_step<AHEAD, 2>();
+        order_step<LATER / 2, 2>();
+        order_step<4 * DT - LATER / 2, 0>();
+      }
     };
     // The first waves form P of tile t in slot 2t and multiply in slot 2t + 1, the second ones a slot
-    // later.  Tile x is read from slot 2x - 1 to slot 2x + 2, sent for in slot 2x - 3 and waited
-    // for by the end of slot 2x - 2.
-    issue(0);
-    issue(1);
+    // later.  Tile x is read from slot 2x - 2 (the operands fetched ahead) to slot 2x + 2, sent for in
+    // slots 2x - 5 and 2x - 4, and has arrived by the end of slot 2x - 3.
+    issue();
+    issue();
+    issue();
     wait_copies<0>();
     lds_barrier();
-    if (nt > 0) products(0);
-    if (second) lds_barrier();
+    fetch(0);
+    scores(0);
+    if (second) bare_barrier();
     for (int t = 0; t < nt; ++t) {
-      if (second) issue(t + 2);
-      form(t);
-      if (!second) wait_copies<0>();
-      lds_barrier();
-      if (!second) issue(t + 2);
+      const int r0 = 64 * (t0 + tile_t);
+      uint32_t at = t % KSTAGES * (SL * 16), next = (t + 1) % KSTAGES * (SL * 16);
+      asm("" : "+s"(at), "+s"(next));
+      form(r0, t % KSTAGES);
+      asm volatile("" ::: "memory");
+      fetch(next);
+      wait_copies_and_writes<0, AHEAD>();
+      bare_barrier();
       __builtin_amdgcn_s_setprio(1);
-      if (t + 1 < nt) products(t + 1);
-      sums(t);
+      products(r0, at, next);
       __builtin_amdgcn_s_setprio(0);
-      if (second) wait_copies<0>();
-      lds_barrier();
+      bare_barrier();
+      if (++tile_t == n_tiles) tile_t = 0;
     }
-    if (!second) lds_barrier();
+    if (!second) bare_barrier();
   };
   walk(std::false_type());
   // a pair that does not count must not reach the sum: see add_pairs
@@ -324,27 +362,32 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   store_row<DP>(out_of(second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, second ? p.scale : 1.f, p.d, h);
 }
 
-template <class Kernel>
-hipError_t launch(Kernel kernel, const CausalArgs& a, int64_t blocks, hipStream_t s) {
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * NWV), 0, s, a);
+template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  const dim3 grid((unsigned)items * a.heads_k * a.group);
+  if (waves == 8) hipLaunchKernelGGL((causal_dq_kernel<DP, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((causal_dq_kernel<DP, 4>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  const dim3 grid((unsigned)items * a.heads_k);
+  if (waves == 8) hipLaunchKernelGGL((causal_dkdv_kernel<DP, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((causal_dkdv_kernel<DP, 4>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s) {
-  const int64_t n = (int64_t)items * a.heads_k * a.group;
-  return a.d <= 32   ? launch(causal_dq_kernel<32>, a, n, s)
-         : a.d <= 64 ? launch(causal_dq_kernel<64>, a, n, s)
-         : a.d <= 96 ? launch(causal_dq_kernel<96>, a, n, s)
-                     : launch(causal_dq_kernel<128>, a, n, s);
+hipError_t causal_bf16_dq(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  return a.d <= 32   ? launch_dq<32>(a, items, waves, s)
+         : a.d <= 64 ? launch_dq<64>(a, items, waves, s)
+         : a.d <= 96 ? launch_dq<96>(a, items, waves, s)
+                     : launch_dq<128>(a, items, waves, s);
 }
-hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s) {
-  const int64_t n = (int64_t)items * a.heads_k;
-  return a.d <= 32   ? launch(causal_dkdv_kernel<32>, a, n, s)
-         : a.d <= 64 ? launch(causal_dkdv_kernel<64>, a, n, s)
-         : a.d <= 96 ? launch(causal_dkdv_kernel<96>, a, n, s)
-                     : launch(causal_dkdv_kernel<128>, a, n, s);
+hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  return a.d <= 32   ? launch_dkdv<32>(a, items, waves, s)
+         : a.d <= 64 ? launch_dkdv<64>(a, items, waves, s)
+         : a.d <= 96 ? launch_dkdv<96>(a, items, waves, s)
+                     : launch_dkdv<128>(a, items, waves, s);
 }
 
 }  // namespace mpipe

@@ -6,20 +6,19 @@
 namespace mpipe {
 namespace {
 
-constexpr int NWV = 8;              // waves of a block, 32 queries each
-constexpr int ROWS = kForwardRows;
-static_assert(ROWS == 32 * NWV, "32 queries a wave");
 constexpr int STAGES = 3;
 
-template <int DP>
+// NWV waves of 32 queries each.
+template <int DP, int NWV>
 __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   using T = Tile<DP>;
   constexpr int SL = T::SLOTS, DT = T::DT;
   __shared__ uint4 ks[STAGES][SL], vs[STAGES][SL];
+  constexpr int ROWS = 32 * NWV;
   const AttnPlace a = attn_place(p, p.group, ROWS);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int c = l & 31, h = l >> 5;
-  const bool late = w >= NWV / 2;   // the group that runs a phase behind
+  const bool late = NWV == 8 && w >= NWV / 2;   // the group that runs a phase behind
   const int head = a.head_k * p.group + a.gq, shift = a.k_len - a.q_len;
   const int q0 = a.r0 + 32 * w, row = min(q0 + c, a.q_len - 1);
   const int last_key = row + shift;                            // that the lane's query sees
@@ -35,24 +34,13 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   RowOp<DP> q;
   load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
   PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.k.row, p.v.row);
+  copy.init(w, l, p.k.row, p.v.row, p.d);
   RowReads<DP> kread;
   kread.init(c, h);
   ColReads<DP> vread;
   vread.init(l);
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
-  // pair t: tile t of K and tile t - 1 of V, in stage t mod 3
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const uint32_t stage = stage_of<STAGES>(t) * (SL * 16);
-#pragma unroll
-    for (int i = 0; i < PairCopy<DP, NWV>::N; ++i) {
-      const bool of_k = copy.of_x(i, w);
-      const int tt = of_k ? t : t - 1;
-      if (tt >= 0 && tt < nt)
-        copy.copy(i, w, l, (of_k ? ks0 : vs0) + stage, (of_k ? K : V) + 64 * tt * (of_k ? p.k.row : p.v.row),
-                  a.k_len - 64 * tt, p.d);
-    }
-  };
+  constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // reads of K before their products begin
 
   float m, sum;
   f32x16 o[DT];
@@ -61,15 +49,34 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
     sum = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = zero16();
+    // pair t: tile t of K and tile t - 1 of V, in a stage of the ring
+    Feed kf, vf;
+    kf.start(K, p.k.row, 0, min(a.k_len, 64 * nt), p.d);
+    vf.start(V, p.v.row, 0, min(a.k_len, 64 * nt), p.d);
+    auto issue = [&](uint32_t stage) __attribute__((always_inline)) {
+      copy.copy(w, ks0 + stage, vs0 + stage, kf.next(), vf.next());
+    };
     f32x16 s[2];
     bf16x8 pb[4];
-    auto scores = [&](int t) __attribute__((always_inline)) {
-      if (64 * t >= wave_keys) return;
-      const uint32_t kt = ks0 + stage_of<STAGES>(t) * (SL * 16);
+    bf16x8 first[AHEAD];
+    // the first operands of a tile of K, and its scores
+    auto fetch = [&](uint32_t stage) __attribute__((always_inline)) {
+#pragma unroll
+      for (int f = 0; f < AHEAD / 2; ++f) {
+        const uint32_t at = kread.base(ks0 + stage, f);
+        first[2 * f] = kread.get(at, 0);
+        first[2 * f + 1] = kread.get(at, 32);
+      }
+    };
+    auto scores = [&](uint32_t stage) __attribute__((always_inline)) {
       s[0] = s[1] = zero16();
 #pragma unroll
-      for (int f = 0; f < T::KF; ++f) {
-        const uint32_t at = kread.base(kt, f);
+      for (int f = 0; f < AHEAD / 2; ++f)
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) s[k2] = mfma(first[2 * f + k2], q.f[f], s[k2]);
+#pragma unroll
+      for (int f = AHEAD / 2; f < T::KF; ++f) {
+        const uint32_t at = kread.base(ks0 + stage, f);
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) s[k2] = mfma(kread.get(at, 32 * k2), q.f[f], s[k2]);
       }
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
       for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[k2][i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = max_halves(mx);
       const float mt = mx * sl2;
       if (__any(mt > m + kSlack)) {
         const float mn = mt > m + kSlack ? mt : m;
@@ -111,68 +118,87 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) pb[j] = pack8(s[j >> 1], j & 1);
     };
-    auto values = [&](int t) __attribute__((always_inline)) {
-      if (64 * t >= wave_keys) return;
-      const uint32_t stage = stage_of<STAGES>(t + 1);
-      if (by_pairs.value && 64 * t >= first_cut) {
-        add_pairs<DP, 64>(o, pb, vs[stage], l, [&](int r) { return 64 * t + r <= last_key; });
+    // products of tile t from `stage`, pair t + 3 into `then`
+    auto products = [&](int t, uint32_t stage, uint32_t then) __attribute__((always_inline)) {
+      if (64 * t >= wave_keys) {
+        issue(then);
         return;
       }
-      const auto at = vread.base(vs0 + stage * (SL * 16));
+      scores(stage);   // (past the wave's last tile: of whatever the stage holds, for nobody)
+      issue(then);
+      if (by_pairs.value && 64 * t >= first_cut) {
+        add_pairs<DP, 64>(o, pb, &vs[0][0] + stage / 16, l, [&](int r) { return 64 * t + r <= last_key; });
+        return;
+      }
+      const auto at = vread.base(vs0 + stage);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] = mfma(vread.get(at, 16 * j, dt), pb[j], o[dt]);
+      if constexpr (!by_pairs.value) {
+        // 2 KF products of scores, the first AHEAD of them fetched; 8 DT half reads and 4 DT
+        // products of values
+        constexpr int REST = 2 * T::KF - AHEAD, LATER = 8 * DT - 2 * AHEAD;
+        order_step<REST, 1>();
+        order_step<AHEAD, 2>();
+        order_step<LATER / 2, 2>();
+        order_step<4 * DT - LATER / 2, 0>();
+      }
     };
-    // The early group's softmax of tile t meets the late group's products of tile t - 1 in a
-    // slot, and the other way round in the next: the matrix and the vector units work at once.
-    // Products of tile t are the scores of tile t + 1 and the values of tile t, both in pair
-    // t + 1.  It was sent for two slots before the early group reads it; its stage's last reader is the
-    // late group, one slot before that.
-    issue(0);
-    issue(1);
+    // In a slot the early group takes its softmax of tile t while the late group multiplies (tile
+    // t - 1), in the next one the other way round: the matrix and the vector units work at once.
+    // Products of tile t are the scores of tile t + 1 and the values of tile t, both in pair t + 1.
+    // A pair is sent for three tiles ahead, in the products' slot, where the stage's last reader was a
+    // slot before, and has arrived a tile before its first reader.
+    Ring ring;
+    ring.start(SL * 16);
+    copy.copy(w, ks0 + ring.c, vs0 + ring.c, kf.next(), buffer_t{0, 0, 0, 0x00027000u});
+    issue(ring.a);
+    issue(ring.b);
     wait_copies<0>();
     lds_barrier();
-    scores(0);
-    if (late) lds_barrier();
-    for (int t = 0; t < nt; ++t) {
-      issue(t + 2);
-      softmax(t);
-      if (!late) {   // pair t + 1 is there; t + 2, where it is a whole one, may be under way
-        if (t + 2 < nt) wait_copies<PairCopy<DP, NWV>::N>();
-        else wait_copies<0>();
-      }
-      lds_barrier();
-      __builtin_amdgcn_s_setprio(1);
-      if (t + 1 < nt) scores(t + 1);
-      values(t);
-      __builtin_amdgcn_s_setprio(0);
-      if (late) wait_copies<0>();
-      lds_barrier();
+    if (wave_keys > 0) {
+      fetch(ring.c);
+      scores(ring.c);
     }
-    if (!late) lds_barrier();
+    if (late) bare_barrier();
+    for (int t = 0; t < nt; ++t) {
+      softmax(t);
+      fetch(ring.a);
+      wait_copies<0>();
+      bare_barrier();
+      __builtin_amdgcn_s_setprio(1);
+      products(t, ring.a, ring.c);
+      __builtin_amdgcn_s_setprio(0);
+      bare_barrier();
+      ring.next();
+    }
+    if (NWV == 8 && !late) bare_barrier();
   };
   walk(std::false_type());
   // what a query does not see must not reach it: see add_pairs
   if (__syncthreads_or(!finite16(o))) walk(std::true_type());
-  sum += __shfl_xor(sum, 32);
+  sum = add_halves(sum);
   if (q0 + c >= a.q_len) return;
   const float inv = last_key < 0 ? 0.f : 1.0f / sum;
   store_row<DP>(out_of(p.o, head, a.q_row + row), o, inv, p.d, h);
   if (h == 0 && p.lse) p.lse[head * p.ld_lse + a.q_row + row] = (m + log2f(sum)) * kLn2;
 }
 
-template <int DP> hipError_t launch(const CausalArgs& a, int items, hipStream_t s) {
-  hipLaunchKernelGGL(causal_fwd_kernel<DP>, dim3((unsigned)items * a.heads_k * a.group),
-                     dim3(64 * NWV), 0, s, a);
+template <int DP> hipError_t launch(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  const dim3 grid((unsigned)items * a.heads_k * a.group);
+  if (waves == 8) hipLaunchKernelGGL((causal_fwd_kernel<DP, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((causal_fwd_kernel<DP, 4>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s) {
-  return a.d <= 32 ? launch<32>(a, items, s) : a.d <= 64 ? launch<64>(a, items, s)
-         : a.d <= 96 ? launch<96>(a, items, s) : launch<128>(a, items, s);
+hipError_t causal_bf16_fwd(const CausalArgs& a, int items, int waves, hipStream_t s) {
+  return a.d <= 32   ? launch<32>(a, items, waves, s)
+         : a.d <= 64 ? launch<64>(a, items, waves, s)
+         : a.d <= 96 ? launch<96>(a, items, waves, s)
+                     : launch<128>(a, items, waves, s);
 }
 
 }  // namespace mpipe
