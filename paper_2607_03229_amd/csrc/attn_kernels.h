@@ -44,12 +44,22 @@ hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStre
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
 
-// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip), in blocks of
-// 8 or 4 waves: items of 32 queries a wave, and for dkdv of 16 keys a wave.  dq writes to
-// `delta` what dkdv reads: -lse * log2(e), then -dO . O.
-hipError_t causal_bf16_fwd(const CausalArgs& a, int items, int waves, hipStream_t s);
-hipError_t causal_bf16_dq(const CausalArgs& a, int items, int waves, hipStream_t s);
-hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s);
+// bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip): items of 32
+// queries a wave, and for dkdv of 16 keys a wave.  dq writes to `delta` what dkdv reads: -lse *
+// log2(e), then -dO . O.
+hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s);
+hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s);
+// The width a head is padded to in the tiles.
+constexpr int causal_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
+// Waves of a block: four where the tiles' LDS lets two blocks share a CU (one's start and end then
+// meet the other's work, and half as many rows pad a sequence's last block), else eight, whose
+// two halves share the SIMDs.  Measured on MI355X, us with 8 -> 4 waves: forward, four sequences
+// of 8192, 8 heads of 64: 357 -> 309; 64 of 200, 16 heads of 80: 62 -> 53; 32 of 1024, 28/4 heads
+// of 128 (one block of either): 390 -> 585.  dK and dV (with dQ): 1158 -> 1096 at 64, 188 -> 232 at
+// 80, 1149 -> 1300 at 128.
+constexpr int causal_q_waves(int width) { return width <= 96 ? 4 : 8; }
+constexpr int causal_k_waves(int width) { return width <= 64 ? 4 : 8; }
 
 struct CacheRows {   // rows on their way into or out of a cache
   mpipe_kv_cache cache;

@@ -55,19 +55,14 @@ bool tiled(const CausalProblem& p, std::initializer_list<const HeadView*> views)
   return true;
 }
 
-int waves_of(const CausalProblem& p, int kind) {
-  const char* e = getenv("PROBE_WAVES");
-  return e ? e[kind] - '0' : 8;
-}
-
 }  // namespace
 
 hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
   if (tiled(p, {&p.q, &p.k, &p.v, &p.o})) {
-    const int waves = waves_of(p, 0);
-    return in_pieces(p, a, false, 32 * waves, p.q.heads, [&](const CausalArgs& b, int n) {
-      return causal_bf16_fwd(b, n, waves, s);
+    const int rows = 32 * causal_q_waves(causal_width(p.head_dim));
+    return in_pieces(p, a, false, rows, p.q.heads, [&](const CausalArgs& b, int n) {
+      return causal_bf16_fwd(b, n, s);
     });
   }
   return in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
@@ -83,14 +78,12 @@ size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int
 hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
   if (tiled(p, {&p.q, &p.k, &p.v, &p.o, &p.d_o, &p.dq, &p.dk, &p.dv})) {
-    const int wq = waves_of(p, 1), wk = waves_of(p, 2);
-    if (hipError_t e = in_pieces(p, a, false, 32 * wq, p.q.heads, [&](const CausalArgs& b, int n) {
-          return causal_bf16_dq(b, n, wq, s);
-        }))
+    const int width = causal_width(p.head_dim);
+    if (hipError_t e = in_pieces(p, a, false, 32 * causal_q_waves(width), p.q.heads,
+                                 [&](const CausalArgs& b, int n) { return causal_bf16_dq(b, n, s); }))
       return e;
-    return in_pieces(p, a, true, 16 * wk, p.k.heads, [&](const CausalArgs& b, int n) {
-      return causal_bf16_dkdv(b, n, wk, s);
-    });
+    return in_pieces(p, a, true, 16 * causal_k_waves(width), p.k.heads,
+                     [&](const CausalArgs& b, int n) { return causal_bf16_dkdv(b, n, s); });
   }
   if (hipError_t e = in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {
         return causal_general_dq(p.dtype, b, n, s);

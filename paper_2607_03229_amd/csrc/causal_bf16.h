@@ -311,11 +311,14 @@ template <int DP, int N, class Seen>
 __device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf16x8 (&w)[N / 16],
                                           const uint4* tile, int l, Seen seen) {
   const int c = l & 31, h = l >> 5;
+  const uint32_t* word = reinterpret_cast<const uint32_t*>(w);   // two weights each
+#pragma nounroll
   for (int row = 0; row < N; ++row) {
     const int half = row >> 5, i = ((row & 31) >> 3) * 4 + (row & 3), src = (row >> 2) & 1;
-    float x = 0.f;
+    uint32_t pair = 0;
 #pragma unroll
-    for (int n = 0; n < N / 2; ++n) x = n == 16 * half + i ? (float)w[n >> 3][n & 7] : x;
+    for (int n = 0; n < N / 4; ++n) pair = n == 8 * half + (i >> 1) ? word[n] : pair;
+    float x = __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16);
     x = __shfl(x, c + 32 * src);
     const bool in = seen(row);
 #pragma unroll
@@ -327,6 +330,7 @@ __device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf1
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           acc[dt][4 * q + e] = in ? fmaf(x, (float)y[e], acc[dt][4 * q + e]) : acc[dt][4 * q + e];
+        asm volatile("" ::: "memory");   // one read at a time: speed is not wanted, registers are
       }
   }
 }

@@ -33,13 +33,11 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
   const bf16* V = head_of(p.v, a.head_k, a.k_row);
   const float sl2 = p.scale * kLog2e;
 
-  RowOp<DP> q, d_o;
-  load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
-  load_row<DP>(d_o, head_of(p.d_o, head, a.q_row + row), p.d, h);
   float nd = 0.f;
   {
-    RowOp<DP> o;
+    RowOp<DP> o, d_o;
     load_row<DP>(o, head_of(p.o, head, a.q_row + row), p.d, h);
+    load_row<DP>(d_o, head_of(p.d_o, head, a.q_row + row), p.d, h);
 #pragma unroll
     for (int f = 0; f < T::KF; ++f)
 #pragma unroll
@@ -52,16 +50,24 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     out[0] = nl2;
     out[(int64_t)p.heads_k * p.group * p.rows_q] = nd;
   }
-  PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.k.row, p.v.row, p.d);
-  RowReads<DP> rread;
-  rread.init(c, h);
-  ColReads<DP> cread;
-  cread.init(l);
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
   constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // row reads before their products begin
   f32x16 dq[DT];
   auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
+    // (of each walk its own, and pair by pair of each step: over all of it they would have to
+    // leave the registers)
+    RowOp<DP> q, d_o;
+    auto operands = [&]() __attribute__((always_inline)) {
+      load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
+      load_row<DP>(d_o, head_of(p.d_o, head, a.q_row + row), p.d, h);
+    };
+    operands();
+    PairCopy<DP, NWV> copy;
+    copy.init(w, l, p.k.row, p.v.row, p.d);
+    RowReads<DP> rread;
+    rread.init(c, h);
+    ColReads<DP> cread;
+    cread.init(l);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt] = zero16();
     Feed kf, vf;
@@ -81,6 +87,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
       }
     };
     auto scores = [&](uint32_t at) __attribute__((always_inline)) {
+      if constexpr (by_pairs.value) operands();
       s = dp = zero16();
 #pragma unroll
       for (int f = 0; f < T::KF; ++f) {
@@ -185,58 +192,69 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   const AttnPlace a = attn_place(p, 1, 16 * NWV);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int c = l & 31, h = l >> 5, pair = w % (NWV / 2);
-  const bool second = w >= NWV / 2;
+  const bool of_second = w >= NWV / 2;
   const int shift = a.k_len - a.q_len;
   const int k0 = a.r0 + 32 * pair, row = min(k0 + c, a.k_len - 1);
   const int first_q = max(row - shift, 0);            // first query that sees the lane's key
   const int t0 = max(a.r0 - shift, 0) / 64;           // first tile with a query that sees any
   const int n_tiles = max((a.q_len + 63) / 64 - t0, 0), nt = n_tiles * p.group;
   const int whole_q = max(min(k0 + 31, a.k_len - 1) - shift, 0);   // sees all of the wave's keys
-  const int wave_q = k0 < a.k_len ? max(k0 - shift, 0) : INT32_MAX - 64;   // sees any
   const float sl2 = p.scale * kLog2e;
-  RowOp<DP> kv;
-  load_row<DP>(kv, head_of(second ? p.v : p.k, a.head_k, a.k_row + row), p.d, h);
-  PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.q.row, p.d_o.row, p.d);
-  RowReads<DP> rread;
-  rread.init(c, h);
-  ColReads<DP> cread;
-  cread.init(l);
-  // the first wave's rows are of Q and columns of dO, the second's the other way round
-  const uint32_t rows0 = second ? lds_at(ds_) : lds_at(qs), cols0 = second ? lds_at(qs) : lds_at(ds_);
+  const uint32_t qs0 = lds_at(qs), ds0 = lds_at(ds_), nl2s0 = lds_at(nl2s), nds0 = lds_at(nds);
   constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // row reads before their products begin
   f32x16 acc[DT];
-  auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
+  auto walk = [&](auto by_pairs, auto is_second) __attribute__((always_inline)) {
+    constexpr bool second = is_second.value;
+    // (of each walk its own: over both they would have to leave the registers)
+    RowOp<DP> kv;
+    load_row<DP>(kv, head_of(second ? p.v : p.k, a.head_k, a.k_row + row), p.d, h);
+    PairCopy<DP, NWV> copy;
+    copy.init(w, l, p.q.row, p.d_o.row, p.d);
+    RowReads<DP> rread;
+    rread.init(c, h);
+    ColReads<DP> cread;
+    cread.init(l);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = zero16();
-    // tiles head by head: Q, dO, and of each query -lse * log2(e) (the first waves') or -dO . O
+    // the first waves' rows are of Q and columns of dO, the second ones' the other way round
+    const uint32_t rows0 = second ? ds0 : qs0, cols0 = second ? qs0 : ds0;
+    // Tiles head by head: Q, dO, and of each query -lse * log2(e) (the first waves') or -dO . O
+    const int head0 = a.head_k * p.group;
     Feed qf, of;
-    uint64_t stats = 0;
-    int sent = 0;   // heads begun
-    uint32_t stage_sent = 0;
-    qf.left = 0;
-    auto issue = [&]() __attribute__((always_inline)) {
-      if (qf.left <= 0) {   // the next head, or past the last one nothing
-        const int head = a.head_k * p.group + min(sent, p.group - 1);
-        const bool more = sent < p.group && n_tiles > 0;
-        qf.start(head_of(p.q, head, a.q_row), p.q.row, t0, a.q_len, p.d);
-        of.start(head_of(p.d_o, head, a.q_row), p.d_o.row, t0, a.q_len, p.d);
-        if (!more) qf.left = of.left = 0;
-        stats = (uint64_t)(p.delta + ((second ? (int64_t)p.heads_k * p.group : 0) + head) * p.rows_q + a.q_row + 64 * t0);
-        ++sent;
+    qf.start(head_of(p.q, head0, a.q_row), p.q.row, t0, a.q_len, p.d);
+    of.start(head_of(p.d_o, head0, a.q_row), p.d_o.row, t0, a.q_len, p.d);
+    uint64_t stats = (uint64_t)(p.delta + ((second ? (int64_t)p.heads_k * p.group : 0) + head0) * p.rows_q + a.q_row + 64 * t0);
+    const uint32_t stats_tail = 4u * (uint32_t)((a.q_len - 1) % 64 + 1);
+    int heads_left = n_tiles > 0 ? p.group - 1 : 0;
+    struct Next {
+      buffer_t q, d_o, stats;
+    };
+    auto next_tile = [&]() __attribute__((always_inline)) {
+      if (qf.left == 0 && heads_left > 0) {   // on to the next head's first tile
+        --heads_left;
+        qf.left = of.left = n_tiles;
+        qf.base += 2 * p.q.head - n_tiles * qf.step;
+        of.base += 2 * p.d_o.head - n_tiles * of.step;
+        stats += 4 * p.rows_q - 256 * (int64_t)n_tiles;
       }
-      const uint32_t n = qf.left > 1 ? 256u : qf.left == 1 ? 4u * (uint32_t)((a.q_len - 1) % 64 + 1) : 0u;
-      copy.copy(w, lds_at(qs) + stage_sent * (SL * 16), lds_at(ds_) + stage_sent * (SL * 16), qf.next(), of.next());
-      if (pair == 0)
-        copy4((second ? lds_at(nds) : lds_at(nl2s)) + 256 * stage_sent, 4 * l,
-              buffer_t{(uint32_t)stats, (uint32_t)(stats >> 32) & 0xffff, n, 0x00027000u});
+      Next x;
+      x.stats = buffer_t{(uint32_t)stats, (uint32_t)(stats >> 32) & 0xffff,
+                         qf.left > 1 ? 256u : qf.left == 1 ? stats_tail : 0u, 0x00027000u};
+      x.q = qf.next();
+      x.d_o = of.next();
       stats += 256;
+      return x;
+    };
+    uint32_t stage_sent = 0;
+    auto issue = [&](const Next& x) __attribute__((always_inline)) {
+      copy.copy(w, qs0 + stage_sent * (SL * 16), ds0 + stage_sent * (SL * 16), x.q, x.d_o);
+      // (64 values; each of the waves that read them sends for all, rather than one by a branch)
+      copy4((second ? nds0 : nl2s0) + 256 * stage_sent, 4 * l, x.stats);
       stage_sent = (stage_sent + 1) % KSTAGES;
     };
     f32x16 s[2];
     bf16x8 x[4], first[AHEAD];
     int tile_t = 0;   // tile t's place among those of its head
-    auto idle = [&](int r0) { return r0 + 63 < wave_q; };   // no query of the tile sees a key here
     auto cut = [&](int r0) { return r0 < whole_q || r0 + 64 > a.q_len; };
     auto fetch = [&](uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
@@ -260,23 +278,19 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
       }
     };
     auto form = [&](int r0, int stage) __attribute__((always_inline)) {
-      if (idle(r0)) return;
-      const float* stats = second ? nds[stage] : nl2s[stage];
+      const float* of_row = second ? nds[stage] : nl2s[stage];
 #pragma unroll
       for (int q2 = 0; q2 < 2; ++q2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float4 v = *reinterpret_cast<const float4*>(&stats[32 * q2 + 8 * i + 4 * h]);
-          const float n[4] = {v.x, v.y, v.z, v.w};
-          if (second) {
+          const f32x4 n = *reinterpret_cast<const f32x4*>(&of_row[32 * q2 + 8 * i + 4 * h]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[q2][4 * i + e] += n[e];
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[q2][4 * i + e] = exp2_fast(fmaf(s[q2][4 * i + e], sl2, n[e]));
+          for (int e = 0; e < 4; ++e) {
+            float& v = reinterpret_cast<float*>(&s[q2])[4 * i + e];
+            v = second ? v + n[e] : exp2_fast(fmaf(v, sl2, n[e]));
           }
         }
-      if (second) {
+      if constexpr (second) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 v = weights[pair][j][l];
@@ -298,16 +312,15 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = pack8(s[j >> 1], j & 1);
-      if (!second) {
+      if constexpr (!second) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) weights[pair][j][l] = *reinterpret_cast<const uint4*>(&x[j]);
       }
     };
     // scores of the next tile, sums of this one
-    auto products = [&](int r0, uint32_t at, uint32_t next) __attribute__((always_inline)) {
+    auto products = [&](int r0, uint32_t at, uint32_t next, const Next& then) __attribute__((always_inline)) {
       scores(next);   // (past the last tile: of whatever lies there, for nobody)
-      issue();
-      if (idle(r0)) return;
+      issue(then);
       if (by_pairs.value && cut(r0)) {
         add_pairs<DP, 64>(acc, x, (second ? &qs[0][0] : &ds_[0][0]) + at / 16, l,
                           [&](int r) { return r0 + r >= first_q && r0 + r < a.q_len; });
@@ -330,64 +343,73 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
     // The first waves form P of tile t in slot 2t and multiply in slot 2t + 1, the second ones a slot
     // later.  Tile x is read from slot 2x - 2 (the operands fetched ahead) to slot 2x + 2, sent for in
     // slots 2x - 5 and 2x - 4, and has arrived by the end of slot 2x - 3.
-    issue();
-    issue();
-    issue();
+    issue(next_tile());
+    issue(next_tile());
+    issue(next_tile());
     wait_copies<0>();
     lds_barrier();
     fetch(0);
     scores(0);
-    if (second) bare_barrier();
+    if constexpr (second) bare_barrier();
     for (int t = 0; t < nt; ++t) {
       const int r0 = 64 * (t0 + tile_t);
+      if (++tile_t == n_tiles) tile_t = 0;
       uint32_t at = t % KSTAGES * (SL * 16), next = (t + 1) % KSTAGES * (SL * 16);
       asm("" : "+s"(at), "+s"(next));
       form(r0, t % KSTAGES);
+      const Next then = next_tile();
       asm volatile("" ::: "memory");
       fetch(next);
       wait_copies_and_writes<0, AHEAD>();
       bare_barrier();
       __builtin_amdgcn_s_setprio(1);
-      products(r0, at, next);
+      products(r0, at, next, then);
       __builtin_amdgcn_s_setprio(0);
       bare_barrier();
-      if (++tile_t == n_tiles) tile_t = 0;
     }
-    if (!second) bare_barrier();
+    if constexpr (!second) bare_barrier();
   };
-  walk(std::false_type());
+  if (of_second) walk(std::false_type(), std::true_type());
+  else walk(std::false_type(), std::false_type());
   // a pair that does not count must not reach the sum: see add_pairs
-  if (__syncthreads_or(!finite16(acc))) walk(std::true_type());
+  if (__syncthreads_or(!finite16(acc))) {
+    if (of_second) walk(std::true_type(), std::true_type());
+    else walk(std::true_type(), std::false_type());
+  }
   if (k0 + c >= a.k_len) return;
-  store_row<DP>(out_of(second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, second ? p.scale : 1.f, p.d, h);
+  store_row<DP>(out_of(of_second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, of_second ? p.scale : 1.f, p.d, h);
 }
 
-template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  const dim3 grid((unsigned)items * a.heads_k * a.group);
-  if (waves == 8) hipLaunchKernelGGL((causal_dq_kernel<DP, 8>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((causal_dq_kernel<DP, 4>), grid, dim3(256), 0, s, a);
+template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, hipStream_t s) {
+  constexpr int NWV = causal_q_waves(DP);
+  hipLaunchKernelGGL((causal_dq_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
+                     dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
 }
-template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  const dim3 grid((unsigned)items * a.heads_k);
-  if (waves == 8) hipLaunchKernelGGL((causal_dkdv_kernel<DP, 8>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((causal_dkdv_kernel<DP, 4>), grid, dim3(256), 0, s, a);
+template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, hipStream_t s) {
+  constexpr int NWV = causal_k_waves(DP);
+  hipLaunchKernelGGL((causal_dkdv_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k), dim3(64 * NWV),
+                     0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t causal_bf16_dq(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  return a.d <= 32   ? launch_dq<32>(a, items, waves, s)
-         : a.d <= 64 ? launch_dq<64>(a, items, waves, s)
-         : a.d <= 96 ? launch_dq<96>(a, items, waves, s)
-                     : launch_dq<128>(a, items, waves, s);
+hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s) {
+  switch (causal_width(a.d)) {
+    case 32: return launch_dq<32>(a, items, s);
+    case 64: return launch_dq<64>(a, items, s);
+    case 96: return launch_dq<96>(a, items, s);
+    default: return launch_dq<128>(a, items, s);
+  }
 }
-hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  return a.d <= 32   ? launch_dkdv<32>(a, items, waves, s)
-         : a.d <= 64 ? launch_dkdv<64>(a, items, waves, s)
-         : a.d <= 96 ? launch_dkdv<96>(a, items, waves, s)
-                     : launch_dkdv<128>(a, items, waves, s);
+hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s) {
+  switch (causal_width(a.d)) {
+    case 32: return launch_dkdv<32>(a, items, s);
+    case 64: return launch_dkdv<64>(a, items, s);
+    case 96: return launch_dkdv<96>(a, items, s);
+    default: return launch_dkdv<128>(a, items, s);
+  }
 }
 
 }  // namespace mpipe

@@ -31,20 +31,21 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   const float sl2 = p.scale * kLog2e;
   constexpr float kSlack = 8.0f;
 
-  RowOp<DP> q;
-  load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
-  PairCopy<DP, NWV> copy;
-  copy.init(w, l, p.k.row, p.v.row, p.d);
-  RowReads<DP> kread;
-  kread.init(c, h);
-  ColReads<DP> vread;
-  vread.init(l);
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
   constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // reads of K before their products begin
 
   float m, sum;
   f32x16 o[DT];
   auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
+    // (of each walk its own: over both they would have to leave the registers)
+    RowOp<DP> q;
+    load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
+    PairCopy<DP, NWV> copy;
+    copy.init(w, l, p.k.row, p.v.row, p.d);
+    RowReads<DP> kread;
+    kread.init(c, h);
+    ColReads<DP> vread;
+    vread.init(l);
     m = -INFINITY;
     sum = 0.f;
 #pragma unroll
@@ -185,20 +186,22 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   if (h == 0 && p.lse) p.lse[head * p.ld_lse + a.q_row + row] = (m + log2f(sum)) * kLn2;
 }
 
-template <int DP> hipError_t launch(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  const dim3 grid((unsigned)items * a.heads_k * a.group);
-  if (waves == 8) hipLaunchKernelGGL((causal_fwd_kernel<DP, 8>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((causal_fwd_kernel<DP, 4>), grid, dim3(256), 0, s, a);
+template <int DP> hipError_t launch(const CausalArgs& a, int items, hipStream_t s) {
+  constexpr int NWV = causal_q_waves(DP);
+  hipLaunchKernelGGL((causal_fwd_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
+                     dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t causal_bf16_fwd(const CausalArgs& a, int items, int waves, hipStream_t s) {
-  return a.d <= 32   ? launch<32>(a, items, waves, s)
-         : a.d <= 64 ? launch<64>(a, items, waves, s)
-         : a.d <= 96 ? launch<96>(a, items, waves, s)
-                     : launch<128>(a, items, waves, s);
+hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s) {
+  switch (causal_width(a.d)) {
+    case 32: return launch<32>(a, items, s);
+    case 64: return launch<64>(a, items, s);
+    case 96: return launch<96>(a, items, s);
+    default: return launch<128>(a, items, s);
+  }
 }
 
 }  // namespace mpipe
