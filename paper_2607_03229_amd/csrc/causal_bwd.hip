@@ -51,7 +51,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
     out[(int64_t)p.heads_k * p.group * p.rows_q] = nd;
   }
   const uint32_t ks0 = lds_at(ks), vs0 = lds_at(vs);
-  constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 8;   // row reads before their products begin
+  constexpr int AHEAD = T::KF < 4 ? 2 * T::KF : 6;   // row reads before their products begin
   f32x16 dq[DT];
   auto walk = [&](auto by_pairs) __attribute__((always_inline)) {
     // (of each walk its own, and pair by pair of each step: over all of it they would have to
