@@ -2,8 +2,8 @@
 //
 // Every key and value is read once, so HBM is the bound; the products (a group's query heads, up
 // to 16 at a time, against 16 keys) take a small part of the MFMA rate.  The work is one line of
-// units, TILE tokens of one (sequence, key head) each, sequences one behind the other; block b of
-// W takes the units [U b / W, U (b + 1) / W), so that every block reads as much whatever the
+// units, TILE tokens of one (sequence, key head) each, sequences one behind the other; of U units
+// each block takes ceil(U / blocks) in turn, so that every block reads as much whatever the
 // lengths.  U comes from the device's lengths: every block adds them up itself, and nothing has to
 // be known on the host.  A block that covers a head's whole length writes its output; otherwise
 // it leaves (maximum, sum, weighted values) of its part, and a second kernel joins a head's
@@ -82,9 +82,13 @@ __device__ __forceinline__ int64_t scan_units(const Args& p, int64_t* sums, Foun
 // to 1 notices
 __device__ __forceinline__ float exp2_any(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Where a part begins: the first unit of block b.
-__device__ __forceinline__ int64_t first_unit(int64_t units, int b, int blocks) {
-  return units * b / blocks;
+// Units of a block.
+__device__ __forceinline__ int64_t units_each(int64_t units, int blocks) {
+  const int64_t n = units + blocks - 1;
+  return n >> 32 ? n / blocks : (int64_t)((uint32_t)n / (uint32_t)blocks);
+}
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
 template <int DP> struct PartOf {
@@ -119,22 +123,52 @@ template <int DP> struct Query<float, DP> {
   }
 };
 
-template <class T, int DP, bool F8>
-__global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
+// A bf16 wave's 32 rows of V in LDS: 16-byte chunk c of row R at c ^ mix(R), so that the transposing
+// reads (8 rows x 32 bytes at a time) and the writes of whole rows meet no bank twice.
+template <int DP> __device__ __forceinline__ int mix(int row) {
+  return DP == 64 ? (row >> 1 & 3) << 1 : (row & 7) << 1;
+}
+
+// Where the 32 tokens from k0 of a sequence lie, for one key head: the row of d values of token
+// k0 + i (tokens past the last: the last one's).  SMALL pages: lane i knows row i.  Otherwise a
+// page holds all 32 and `first` is the row of k0, the same for every lane.
+template <bool SMALL> struct Rows32 {
+  int64_t first;
+  int last;
+  __device__ __forceinline__ void find(const CachePlaces& at, const int32_t* table, int k0, int len, int head,
+                                       int l, bool& bad) {
+    last = min(31, len - 1 - k0);
+    const int tok = SMALL ? k0 + min(l & 31, last) : k0;
+    int32_t page = table[tok >> at.shift];
+    if ((uint32_t)page >= (uint32_t)at.n_pages) {
+      bad = true;
+      page = 0;
+    }
+    first = at.in_page(page, tok, head);
+    if constexpr (!SMALL)
+      first = (int64_t)__builtin_amdgcn_readfirstlane((int)first) & 0xffffffffll |
+              (int64_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32;
+  }
+  __device__ __forceinline__ int64_t row(int i) const {
+    return SMALL ? __shfl(first, i) : first + min(i, last);
+  }
+};
+
+template <class T, int DP, bool F8, bool SMALL>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args p) {
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int NDT = DP / 16, NC = DP / 8;
-  __shared__ uint4 vt[NW][32 * NC];   // bf16: a wave's 32 rows of V
+  constexpr int NDT = DP / 16, NC = DP / 8, NF = BF ? DP / 32 : DP / 16, NV = NC / 2;
+  __shared__ uint4 vt[NW][32 * NC];
   __shared__ float ml[NW][2][QG];
   __shared__ int64_t sums[4];
   __shared__ int start_seq;
   __shared__ int64_t start_before;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4, r = l & 15;
+  const int tid = threadIdx.x, l = tid & 63, g = l >> 4, r = l & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d = p.at.d, heads_v = p.at.heads * p.col_blocks;   // (key head, column block) pairs
-  if (tid == 0) start_seq = -1;
-  __syncthreads();
   // the sequence that holds the block's first unit (of heads_v * the sequence's units)
   const int64_t units = heads_v * scan_units(p, sums, [&](int s, int64_t before, int64_t all) {
-    const int64_t u0 = first_unit(heads_v * all, blockIdx.x, p.blocks);
+    const int64_t u0 = blockIdx.x * units_each(heads_v * all, p.blocks);
     const int64_t lo = heads_v * before, hi = lo + (int64_t)heads_v * units_of(p, s);
     if (u0 >= lo && u0 < hi) {
       start_seq = s;
@@ -142,108 +176,130 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
     }
   });
   __syncthreads();
-  int64_t u = first_unit(units, blockIdx.x, p.blocks);
-  const int64_t u_end = first_unit(units, blockIdx.x + 1, p.blocks);
+  const int64_t each = units_each(units, p.blocks);
+  int64_t u = blockIdx.x * each;
+  const int64_t u_end = min(u + each, units);
   if (u >= u_end) return;
-  int seq = start_seq;
+  int seq = __builtin_amdgcn_readfirstlane(start_seq);
   int64_t seq_u0 = start_before;
   const float sl2 = p.scale * kLog2e;
 
   while (u < u_end) {
     bool all_there;
-    const int len = tokens_of(p, seq, all_there), nt = (len + TILE - 1) / TILE;
+    const int len = __builtin_amdgcn_readfirstlane(tokens_of(p, seq, all_there)), nt = (len + TILE - 1) / TILE;
     if (nt == 0) {   // (a sequence without tokens has no units)
       ++seq;
       continue;
     }
-    const int hv = (int)((u - seq_u0) / nt), tile0 = (int)((u - seq_u0) % nt);
-    const int tile1 = (int)min((int64_t)nt, tile0 + (u_end - u));
+    const int hv = __builtin_amdgcn_readfirstlane((int)quotient(u - seq_u0, nt));
+    const int tile0 = __builtin_amdgcn_readfirstlane((int)(u - seq_u0 - (int64_t)hv * nt));
+    const int tile1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)nt, tile0 + (u_end - u)));
     const int head_k = hv / p.col_blocks, col = hv % p.col_blocks;
     const int nq = min(QG, p.group - QG * col);
     const int head_q = head_k * p.group + QG * col;
-    // queries: column r of the products
+    const int32_t* table = p.at.table + seq * p.at.ld_table;
+    bool bad = !all_there;
+
+    // one tile's keys as the products' row operand, and its values as they lie
+    Rows32<SMALL> rows;
+    uint4 kr[2][F8 ? 1 : NF], vr[F8 ? 1 : NV];
+    uint2 kr8[2][F8 ? NF : 1], vr8[F8 ? NV : 1];   // (fp32 with e4m3: four bytes of each)
+    float scale_k = 1.f, scale_v = 1.f;            // of token l % 32
+    auto fetch = [&](int k0) __attribute__((always_inline)) {
+      if constexpr (F8) {
+        const int64_t row = SMALL ? rows.first : rows.row(l & 31);
+        scale_k = e8m0(p.sk[row]);
+        scale_v = e8m0(p.sv[row]);
+      }
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq) {
+        const int64_t at = rows.row(16 * kq + r) * d;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const int c = BF ? 32 * f + 8 * g : 16 * f + 4 * g;
+          if constexpr (F8) {
+            const uint8_t* x = reinterpret_cast<const uint8_t*>(p.k) + at + c;
+            if (c < d) kr8[kq][f] = BF ? *reinterpret_cast<const uint2*>(x) : make_uint2(*reinterpret_cast<const uint32_t*>(x), 0);
+            else kr8[kq][f] = make_uint2(0, 0);
+          } else {
+            if (c < d) kr[kq][f] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.k) + at + c);
+            else kr[kq][f] = make_uint4(0, 0, 0, 0);
+          }
+        }
+      }
+      if constexpr (BF) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int slot = 64 * i + l, c = slot % NC * 8;
+          const int64_t at = rows.row(slot / NC) * d + c;
+          if constexpr (F8) {
+            vr8[i] = make_uint2(0, 0);
+            if (c < d) vr8[i] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(p.v) + at);
+          } else {
+            vr[i] = make_uint4(0, 0, 0, 0);
+            if (c < d) vr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.v) + at);
+          }
+        }
+      }
+    };
+    // wave w's tokens of tile t
+    auto start = [&](int t) { return t * TILE + 32 * w; };
+    if (start(tile0) < len) {
+      rows.find(p.at, table, start(tile0), len, head_k, l, bad);
+      fetch(start(tile0));
+    }
     Query<T, DP> q;
     q.load(reinterpret_cast<const T*>(p.q.p) + p.q.row * seq + p.q.head * (head_q + min(r, nq - 1)), d, g);
-    const int32_t* table = p.at.table + seq * p.at.ld_table;
     float m = -INFINITY, sum = 0.f;
-    bool bad = !all_there;
     f32x4 o[NDT];
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     for (int t = tile0; t < tile1; ++t) {
-      const int k0 = t * TILE + 32 * w;
+      const int k0 = start(t);
       if (k0 >= len) break;
-      // lane l < 32 (and l + 32 again) knows where token k0 + l lies
-      int64_t place;
-      {
-        const int tok = min(k0 + (l & 31), len - 1);
-        int32_t page = table[tok >> p.at.shift];
-        if ((uint32_t)page >= (uint32_t)p.at.n_pages) {
-          bad = true;
-          page = 0;
-        }
-        place = p.at.in_page(page, tok, head_k);
-      }
+      const Rows32<SMALL> here = rows;
+      const float scale_here = scale_v;
+      const bool more = t + 1 < tile1 && start(t + 1) < len;
+      if (more) rows.find(p.at, table, start(t + 1), len, head_k, l, bad);
       f32x4 s[2];
 #pragma unroll
       for (int kq = 0; kq < 2; ++kq) {
-        const int64_t row = __shfl(place, 16 * kq + r);
         s[kq] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (!BF) {
+        const float scale = F8 ? __shfl(scale_k, 16 * kq + r) : 1.f;
 #pragma unroll
-          for (int f = 0; f < DP / 16; ++f) {
-            const int c = 16 * f + 4 * g;
-            f32x4 kf = {0.f, 0.f, 0.f, 0.f};
-            if (c < d) {
-              if constexpr (F8) kf = load4_e4m3(reinterpret_cast<const uint8_t*>(p.k) + row * d + c, e8m0(p.sk[row]));
-              else kf = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(p.k) + row * d + c);
-            }
+        for (int f = 0; f < NF; ++f) {
+          if constexpr (BF) {
+            bf16x8 kf;
+            if constexpr (F8) kf = bf16_of_e4m3(kr8[kq][f], scale);
+            else kf = *reinterpret_cast<const bf16x8*>(&kr[kq][f]);
+            s[kq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.f[f], s[kq], 0, 0, 0);
+          } else {
+            f32x4 kf;
+            if constexpr (F8) kf = f32_of_e4m3(kr8[kq][f].x, scale);
+            else kf = *reinterpret_cast<const f32x4*>(&kr[kq][f]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               s[kq] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q.f[f][e], s[kq], 0, 0, 0);
           }
-        } else
-#pragma unroll
-        for (int f = 0; f < DP / 32; ++f) {
-          const int c = 32 * f + 8 * g;
-          bf16x8 kf;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) kf[e] = (bf16)0.f;
-          if (c < d) {
-            if constexpr (F8) {
-              float x[8];
-              load8_e4m3(reinterpret_cast<const uint8_t*>(p.k) + row * d + c, e8m0(p.sk[row]), x);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) kf[e] = (bf16)x[e];
-            } else {
-              kf = *reinterpret_cast<const bf16x8*>(reinterpret_cast<const bf16*>(p.k) + row * d + c);
-            }
-          }
-          s[kq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.f[f], s[kq], 0, 0, 0);
         }
       }
-      // V rows into LDS
-      if constexpr (BF)
+      if constexpr (BF) {
 #pragma unroll
-      for (int i = 0; i < 32 * NC / 64; ++i) {
-        const int slot = 64 * i + l, vr = slot / NC, c = slot % NC;
-        const int64_t row = __shfl(place, vr);
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (8 * c < d && k0 + vr < len) {
+        for (int i = 0; i < NV; ++i) {
+          const int slot = 64 * i + l, row = slot / NC;
+          uint4 x;
           if constexpr (F8) {
-            float y[8];
-            load8_e4m3(reinterpret_cast<const uint8_t*>(p.v) + row * d + 8 * c, e8m0(p.sv[row]), y);
-            bf16x8 z;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = (bf16)y[e];
-            x = *reinterpret_cast<uint4*>(&z);
+            const bf16x8 y = bf16_of_e4m3(vr8[i], __shfl(scale_here, row));
+            x = *reinterpret_cast<const uint4*>(&y);
           } else {
-            x = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.v) + row * d + 8 * c);
+            x = vr[i];
           }
+          if (k0 + row >= len) x = make_uint4(0, 0, 0, 0);   // 0 times the last row again could be NaN
+          vt[w][row * NC + (slot % NC ^ mix<DP>(row))] = x;
         }
-        vt[w][slot] = x;
       }
+      if (more) fetch(start(t + 1));
       float mx = -INFINITY;
 #pragma unroll
       for (int kq = 0; kq < 2; ++kq)
@@ -271,29 +327,33 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
         bf16x8 pb;
 #pragma unroll
         for (int e = 0; e < 8; ++e) pb[e] = (bf16)s[e / 4][e % 4];
+        const char* base = reinterpret_cast<const char*>(vt[w]);
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           // V^T: column 16 dt + r, tokens 4g .. 4g + 3 and 16 + 4g ..
           bf16x8 a;
-          const bf16* base = reinterpret_cast<const bf16*>(vt[w]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a[e] = base[(4 * g + e) * DP + 16 * dt + r];
-            a[4 + e] = base[(16 + 4 * g + e) * DP + 16 * dt + r];
+          for (int i = 0; i < 2; ++i) {
+            const int row = 16 * i + 4 * g + (r >> 2), chunk = 2 * dt + ((r & 3) >> 1);
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(base + (row * NC + (chunk ^ mix<DP>(row))) * 16 + (r & 1) * 8));
+            const bf16* y = reinterpret_cast<const bf16*>(&x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[4 * i + e] = y[e];
           }
           o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[dt], 0, 0, 0);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int vr = 16 * (i / 4) + 4 * g + i % 4;
-          const int64_t row = __shfl(place, vr);
-          const float scale = F8 ? e8m0(p.sv[row]) : 1.f;
+          const int vrow = 16 * (i / 4) + 4 * g + i % 4;
+          const int64_t row = here.row(vrow);
+          const float scale = F8 ? __shfl(scale_here, vrow) : 1.f;
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             const int col_v = 16 * dt + r;
             float a = 0.f;
-            if (col_v < d && k0 + vr < len) {
+            if (col_v < d && k0 + vrow < len) {
               if constexpr (F8)
                 a = scale * __builtin_amdgcn_cvt_f32_fp8(reinterpret_cast<const uint8_t*>(p.v)[row * d + col_v], 0);
               else
@@ -319,17 +379,20 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
     const float ref = M == -INFINITY ? 0.f : M, mine = exp2_any(m - ref);
 #pragma unroll
     for (int i = 0; i < NW; ++i) tot += ml[i][1][r] * exp2_any(ml[i][0][r] - ref);
-    float* red = reinterpret_cast<float*>(vt);   // [QG][DP], a wave at a time
-    for (int i = 0; i < NW; ++i) {
-      if (w == i) {
+    float* red = reinterpret_cast<float*>(vt);   // a wave's [QG][DP + 4]
+    constexpr int RP = DP + 4;
+    static_assert(QG * RP * sizeof(float) <= sizeof(vt) / 2, "two waves' values");
+    // two waves at a time
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
+    for (int half = 0; half < 2; ++half) {
+      if (w / 2 == half) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = m == -INFINITY ? 0.f : o[dt][e] * mine;
-            float* at = red + r * DP + 16 * dt + 4 * g + e;
-            *at = i == 0 ? x : *at + x;
-          }
+        for (int dt = 0; dt < NDT; ++dt) {
+          f32x4 x = m == -INFINITY ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt] * mine;
+          f32x4* at = reinterpret_cast<f32x4*>(red + ((w & 1) * QG + r) * RP + 16 * dt + 4 * g);
+          if (half) x += *at;
+          *at = x;
+        }
       }
       __syncthreads();
     }
@@ -342,15 +405,18 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
         ml[0][1][r] = tot;
       }
       __syncthreads();
-      for (int i = tid; i < nq * d; i += 256) {
-        const int h = i / d, c = i % d;
+      for (int i = tid; i < nq * DP; i += 256) {
+        const int h = i / DP, c = i % DP;
         T* O = reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * (head_q + h);
-        O[c] = (T)(red[h * DP + c] / ml[0][1][h]);
+        if (c < d) O[c] = (T)((red[h * RP + c] + red[(QG + h) * RP + c]) / ml[0][1][h]);
       }
       if (p.lse && tid < nq)
         p.lse[(head_q + tid) * p.ld_lse + seq] = (ml[0][0][tid] + log2f(ml[0][1][tid])) * kLn2;
     } else {
-      for (int i = tid; i < nq * DP; i += 256) part[i / DP * PartOf<DP>::ROW + i % DP] = red[i];
+      for (int i = tid; i < nq * DP; i += 256) {
+        const int h = i / DP, c = i % DP;
+        part[h * PartOf<DP>::ROW + c] = red[h * RP + c] + red[(QG + h) * RP + c];
+      }
       if (w == 0 && g == 0 && r < nq) {
         part[r * PartOf<DP>::ROW + DP] = M;
         part[r * PartOf<DP>::ROW + DP + 1] = tot;
@@ -368,9 +434,11 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(Args p) {
 // Joins the parts of one (sequence, query head); sequences without tokens get their outputs here.
 template <class T, int DP>
 __global__ __launch_bounds__(256) void join_kernel(Args p) {
+  constexpr int LANES = 256 / DP;   // threads to a column
   __shared__ int64_t sums[4];
   __shared__ int64_t before_s;
-  const int heads_q = p.at.heads * p.group, heads_v = p.at.heads * p.col_blocks, d = p.at.d;
+  __shared__ float weight[MAX_BLOCKS], top[4], total[4], cols[256];
+  const int tid = threadIdx.x, heads_q = p.at.heads * p.group, heads_v = p.at.heads * p.col_blocks, d = p.at.d;
   const int seq = blockIdx.x / heads_q, head = blockIdx.x % heads_q;
   const int head_k = head / p.group, col = head % p.group / QG, h = head % p.group % QG;
   const int64_t units = heads_v * scan_units(p, sums, [&](int s, int64_t before, int64_t) {
@@ -382,50 +450,68 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   T* O = reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * head;
   if (nt == 0) {
     const float x = all_there ? 0.f : NAN;
-    for (int c = threadIdx.x; c < d; c += 256) O[c] = (T)x;
-    if (p.lse && threadIdx.x == 0) p.lse[head * p.ld_lse + seq] = all_there ? -INFINITY : NAN;
+    for (int c = tid; c < d; c += 256) O[c] = (T)x;
+    if (p.lse && tid == 0) p.lse[head * p.ld_lse + seq] = all_there ? -INFINITY : NAN;
     return;
   }
-  const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt, u1 = u0 + nt;
-  // the block of a unit: the largest b with first_unit(b) <= u
-  auto block_of = [&](int64_t x) {
-    int64_t b = (x * p.blocks) / units;
-    while (b + 1 < p.blocks && first_unit(units, (int)b + 1, p.blocks) <= x) ++b;
-    while (first_unit(units, (int)b, p.blocks) > x) --b;
-    return (int)b;
+  const int64_t each = units_each(units, p.blocks);
+  const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt;
+  const int b0 = (int)quotient(u0, each), n = (int)quotient(u0 + nt - 1, each) - b0 + 1;
+  if (n == 1) return;   // written by its block
+  // part i: of block b0 + i; the first block's begins the head, the others' begin the block
+  auto part_of = [&](int i) {
+    return p.part + ((int64_t)(2 * (b0 + i) + (i == 0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
   };
-  const int b0 = block_of(u0), b1 = block_of(u1 - 1);
-  if (b0 == b1) return;   // written by that block
-  auto part_of = [&](int b) {
-    return p.part + ((int64_t)(2 * b + (b == b0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
-  };
-  float M = -INFINITY, tot = 0.f;
-  for (int b = b0; b <= b1; ++b)
-    if (first_unit(units, b, p.blocks) < first_unit(units, b + 1, p.blocks)) M = fmaxf(M, part_of(b)[DP]);
-  const float ref = M == -INFINITY ? 0.f : M;
-  for (int c = threadIdx.x; c < DP; c += 256) {
-    float x = 0.f;
-    tot = 0.f;
-    for (int b = b0; b <= b1; ++b) {
-      if (first_unit(units, b, p.blocks) == first_unit(units, b + 1, p.blocks)) continue;
-      const float* a = part_of(b);
-      const float wt = exp2_any(a[DP] - ref);
-      tot += a[DP + 1] * wt;
-      x += a[c] * wt;
-    }
-    if (c < d) O[c] = (T)(x / tot);
+  float m = -INFINITY;
+  for (int i = tid; i < n; i += 256) {
+    weight[i] = part_of(i)[DP];
+    m = fmaxf(m, weight[i]);
   }
-  if (p.lse && threadIdx.x == 0) p.lse[head * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
+  m = warp_max(m);
+  if (tid % 64 == 0) top[tid / 64] = m;
+  __syncthreads();
+  const float M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), ref = M == -INFINITY ? 0.f : M;
+  float tot = 0.f;
+  for (int i = tid; i < n; i += 256) {
+    weight[i] = exp2_any(weight[i] - ref);
+    tot += part_of(i)[DP + 1] * weight[i];
+  }
+  tot = warp_sum(tot);
+  if (tid % 64 == 0) total[tid / 64] = tot;
+  __syncthreads();
+  tot = total[0] + total[1] + total[2] + total[3];
+  const int c = tid % DP;
+  float x = 0.f;
+#pragma unroll 8
+  for (int i = tid / DP; i < n; i += LANES) x = fmaf(part_of(i)[c], weight[i], x);
+  if constexpr (LANES > 1) {
+    cols[tid] = x;
+    __syncthreads();
+    if (tid >= DP) return;
+#pragma unroll
+    for (int i = 1; i < LANES; ++i) x += cols[i * DP + c];
+  }
+  if (c < d) O[c] = (T)(x / tot);
+  if (p.lse && tid == 0) p.lse[head * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
 }
 
-template <class T, int DP, bool F8>
-hipError_t launch(const Args& a, int n_blocks, int joins, hipStream_t s) {
-  if (n_blocks > 0) {
-    hipLaunchKernelGGL((cache_attn_kernel<T, DP, F8>), dim3(n_blocks), dim3(256), 0, s, a);
+template <class T, int DP, bool F8, bool SMALL>
+hipError_t launch(const Args& a, int joins, hipStream_t s) {
+  if (a.blocks > 0) {
+    hipLaunchKernelGGL((cache_attn_kernel<T, DP, F8, SMALL>), dim3(a.blocks), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
   hipLaunchKernelGGL((join_kernel<T, DP>), dim3(joins), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+template <class T, bool F8, bool SMALL>
+hipError_t by_width(const Args& a, int joins, hipStream_t s) {
+  return a.at.d <= 64    ? launch<T, 64, F8, SMALL>(a, joins, s)
+         : a.at.d <= 128 ? launch<T, 128, F8, SMALL>(a, joins, s)
+                         : launch<T, 256, F8, SMALL>(a, joins, s);
+}
+template <class T, bool F8> hipError_t by_page(const Args& a, int joins, hipStream_t s) {
+  return a.at.shift < 5 ? by_width<T, F8, true>(a, joins, s) : by_width<T, F8, false>(a, joins, s);
 }
 
 int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -456,14 +542,9 @@ hipError_t cache_attention(const CacheAttention& p, hipStream_t s) {
   const int64_t units = ((int64_t)p.width * p.cache.page + TILE - 1) / TILE * p.cache.heads * a.col_blocks;
   a.blocks = (int)(units >= MAX_BLOCKS ? MAX_BLOCKS : units * p.n_seq >= MAX_BLOCKS ? MAX_BLOCKS : units * p.n_seq);
   const int joins = p.n_seq * p.q.heads;
-#define MPIPE_DECODE(T, F8)                                                          \
-  (p.cache.head_dim <= 64    ? launch<T, 64, F8>(a, a.blocks, joins, s)              \
-   : p.cache.head_dim <= 128 ? launch<T, 128, F8>(a, a.blocks, joins, s)             \
-                             : launch<T, 256, F8>(a, a.blocks, joins, s))
   const bool f8 = p.cache.dtype == MPIPE_E4M3;
-  if (p.dtype == DT_BF16) return f8 ? MPIPE_DECODE(bf16, true) : MPIPE_DECODE(bf16, false);
-  return f8 ? MPIPE_DECODE(float, true) : MPIPE_DECODE(float, false);
-#undef MPIPE_DECODE
+  if (p.dtype == DT_BF16) return f8 ? by_page<bf16, true>(a, joins, s) : by_page<bf16, false>(a, joins, s);
+  return f8 ? by_page<float, true>(a, joins, s) : by_page<float, false>(a, joins, s);
 }
 
 }  // namespace mpipe

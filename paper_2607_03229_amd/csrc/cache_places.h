@@ -62,11 +62,19 @@ __device__ __forceinline__ void load8_e4m3(const uint8_t* p, float scale, float 
   x[0] = a[0] * scale; x[1] = a[1] * scale; x[2] = b[0] * scale; x[3] = b[1] * scale;
   x[4] = c[0] * scale; x[5] = c[1] * scale; x[6] = d[0] * scale; x[7] = d[1] * scale;
 }
-__device__ __forceinline__ f32x4 load4_e4m3(const uint8_t* p, float scale) {
+// Values times a power of two, in fp32 and (exact there too) in bf16.
+__device__ __forceinline__ f32x4 f32_of_e4m3(uint32_t w, float scale) {
   typedef __attribute__((ext_vector_type(2))) float f32x2;
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
   const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   return f32x4{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
+}
+__device__ __forceinline__ bf16x8 bf16_of_e4m3(uint2 w, float scale) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 }  // namespace mpipe
