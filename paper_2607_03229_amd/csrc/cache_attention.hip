@@ -13,6 +13,8 @@
 // maxima and sums are lane exchanges within a column, and P^T is already the operand of
 // O^T += V^T P^T.  K comes from memory in operand order; V goes through LDS, from which the
 // transposing reads take it.  The next tokens' loads are in flight meanwhile.
+#include <type_traits>
+
 #include "cache_places.h"
 
 namespace mpipe {
@@ -20,7 +22,7 @@ namespace {
 
 constexpr int NW = 4, TILE = 32 * NW;   // waves of a block, tokens of a unit
 constexpr int QG = 16;                  // query heads of a column block
-constexpr int MAX_BLOCKS = 512;
+constexpr int MAX_BLOCKS = 768;          // of any variant: three a CU
 
 struct Args {
   const void *k, *v;
@@ -97,31 +99,40 @@ template <int DP> struct PartOf {
 
 // The queries as the products' column operand, and the products themselves: bf16 in steps of 32
 // columns, fp32 in steps of 16 (four MFMAs each).
-template <class T, int DP> struct Query;
-template <int DP> struct Query<bf16, DP> {
+// (8-bit keys: in the order in which lanes hold 16 of them at once, see fetch)
+template <class T, int DP, bool F8> struct Query;
+template <int DP, bool F8> struct Query<bf16, DP, F8> {
   bf16x8 f[DP / 32];
   __device__ __forceinline__ void load(const bf16* Q, int d, int g) {
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = 32 * i + 8 * g + e;
+        const int c = F8 ? 64 * (i / 2) + 16 * g + 8 * (i % 2) + e : 32 * i + 8 * g + e;
         f[i][e] = c < d ? Q[c] : (bf16)0.f;
       }
   }
 };
-template <int DP> struct Query<float, DP> {
+template <int DP, bool F8> struct Query<float, DP, F8> {
   f32x4 f[DP / 16];
   __device__ __forceinline__ void load(const float* Q, int d, int g) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int c = 16 * i + 4 * g + e;
+        const int c = F8 ? 64 * (i / 4) + 16 * g + 4 * (i % 4) + e : 16 * i + 4 * g + e;
         f[i][e] = c < d ? Q[c] : 0.f;
       }
   }
 };
+// Sixteen 8-bit values, columns c .. of d; EXACT: all there and aligned.
+template <bool EXACT> __device__ __forceinline__ uint4 load_e4m3x16(const uint8_t* x, int c, int d) {
+  if constexpr (EXACT) return *reinterpret_cast<const uint4*>(x + c);
+  uint2 a = make_uint2(0, 0), b = a;
+  if (c < d) a = *reinterpret_cast<const uint2*>(x + c);
+  if (c + 8 < d) b = *reinterpret_cast<const uint2*>(x + c + 8);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
 
 // A bf16 wave's 32 rows of V in LDS: 16-byte chunk c of row R at c ^ mix(R), so that the transposing
 // reads (8 rows x 32 bytes at a time) and the writes of whole rows meet no bank twice.
@@ -133,32 +144,44 @@ template <int DP> __device__ __forceinline__ int mix(int row) {
 // k0 + i (tokens past the last: the last one's).  SMALL pages: lane i knows row i.  Otherwise a
 // page holds all 32 and `first` is the row of k0, the same for every lane.
 template <bool SMALL> struct Rows32 {
+  int32_t page;    // as read, of lane l's token (SMALL) or of all
   int64_t first;
   int last;
-  __device__ __forceinline__ void find(const CachePlaces& at, const int32_t* table, int k0, int len, int head,
-                                       int l, bool& bad) {
+  __device__ __forceinline__ void look(const CachePlaces& at, const int32_t* table, int k0, int len, int l) {
     last = min(31, len - 1 - k0);
-    const int tok = SMALL ? k0 + min(l & 31, last) : k0;
-    int32_t page = table[tok >> at.shift];
-    if ((uint32_t)page >= (uint32_t)at.n_pages) {
-      bad = true;
-      page = 0;
-    }
-    first = at.in_page(page, tok, head);
+    page = table[(SMALL ? k0 + min(l & 31, last) : k0) >> at.shift];
+  }
+  __device__ __forceinline__ void find(const CachePlaces& at, int k0, int head, int l, bool& bad) {
+    const bool out = (uint32_t)page >= (uint32_t)at.n_pages;
+    bad |= out;
+    first = at.in_page(out ? 0 : page, SMALL ? k0 + min(l & 31, last) : k0, head);
     if constexpr (!SMALL)
       first = (int64_t)__builtin_amdgcn_readfirstlane((int)first) & 0xffffffffll |
               (int64_t)__builtin_amdgcn_readfirstlane((int)(first >> 32)) << 32;
   }
-  __device__ __forceinline__ int64_t row(int i) const {
-    return SMALL ? __shfl(first, i) : first + min(i, last);
+  // where row i of d values is, FULL: all 32 tokens are there
+  template <bool FULL> __device__ __forceinline__ int64_t at(int i, int d) const {
+    if constexpr (SMALL) return __shfl(first, i) * d;
+    else return first * d + (FULL ? i : min(i, last)) * d;
   }
 };
 
+// Blocks that share a CU: eight bits leave half as many bytes under way in a wave, and take fewer
+// registers.  Measured on MI355X, two -> three blocks a CU (768 in all): four sequences of up to
+// 131072, 4 key heads of 128, e4m3: 146 -> 129 us; 64 of 8192, 8 of 64: 138 -> 118; bf16, 64 of up
+// to 16384, 8 of 128: 426 -> 445.
+constexpr int blocks_per_cu(int width, bool eight, bool bf) {
+  return width == 256 ? 1 : eight && (bf || width == 64) ? 3 : 2;
+}
+
 template <class T, int DP, bool F8, bool SMALL>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args p) {
+__global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void cache_attn_kernel(Args p) {
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int NDT = DP / 16, NC = DP / 8, NF = BF ? DP / 32 : DP / 16, NV = NC / 2;
-  __shared__ uint4 vt[NW][32 * NC];
+  // V's rows in LDS: NC chunks of 16 bytes, PC apart (fp32: so that four rows four apart, which
+  // a read takes at once, lie in different banks)
+  constexpr int NDT = DP / 16, NF = BF ? DP / 32 : DP / 16;
+  constexpr int NC = BF ? DP / 8 : DP / 4, PC = BF ? NC : NC + 1;
+  __shared__ uint4 vt[NW][32 * PC];
   __shared__ float ml[NW][2][QG];
   __shared__ int64_t sums[4];
   __shared__ int start_seq;
@@ -201,54 +224,60 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args
     bool bad = !all_there;
 
     // one tile's keys as the products' row operand, and its values as they lie
-    Rows32<SMALL> rows;
-    uint4 kr[2][F8 ? 1 : NF], vr[F8 ? 1 : NV];
-    uint2 kr8[2][F8 ? NF : 1], vr8[F8 ? NV : 1];   // (fp32 with e4m3: four bytes of each)
-    float scale_k = 1.f, scale_v = 1.f;            // of token l % 32
-    auto fetch = [&](int k0) __attribute__((always_inline)) {
+    Rows32<SMALL> rows, ahead;   // of the tile under way, and of the one after it
+    // (of 8 bits, a lane holds 16 values of a row at once: 64 f + 16 g .. of its key)
+    constexpr int NK = F8 ? DP / 64 : NF, NV = F8 ? DP / 32 : NC / 2, VE = F8 ? 16 : BF ? 8 : 4;
+    constexpr int VS = DP / VE;                     // slots of V's rows
+    uint4 kr[2][NK], vr[NV];
+    uint8_t scale_k = 0, scale_v = 0;               // of token l % 32, as stored
+    auto fetch_as = [&](auto exact, auto full) __attribute__((always_inline)) {
+      constexpr bool EXACT = exact.value, FULL = full.value;
       if constexpr (F8) {
-        const int64_t row = SMALL ? rows.first : rows.row(l & 31);
-        scale_k = e8m0(p.sk[row]);
-        scale_v = e8m0(p.sv[row]);
+        const int64_t row = SMALL ? rows.first : rows.first + min(l & 31, rows.last);
+        scale_k = p.sk[row];
+        scale_v = p.sv[row];
       }
 #pragma unroll
       for (int kq = 0; kq < 2; ++kq) {
-        const int64_t at = rows.row(16 * kq + r) * d;
+        const int64_t at = rows.template at<FULL>(16 * kq + r, d);
 #pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          const int c = BF ? 32 * f + 8 * g : 16 * f + 4 * g;
+        for (int f = 0; f < NK; ++f) {
           if constexpr (F8) {
-            const uint8_t* x = reinterpret_cast<const uint8_t*>(p.k) + at + c;
-            if (c < d) kr8[kq][f] = BF ? *reinterpret_cast<const uint2*>(x) : make_uint2(*reinterpret_cast<const uint32_t*>(x), 0);
-            else kr8[kq][f] = make_uint2(0, 0);
+            kr[kq][f] = load_e4m3x16<EXACT>(reinterpret_cast<const uint8_t*>(p.k) + at, 64 * f + 16 * g, d);
           } else {
-            if (c < d) kr[kq][f] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.k) + at + c);
-            else kr[kq][f] = make_uint4(0, 0, 0, 0);
+            const int c = BF ? 32 * f + 8 * g : 16 * f + 4 * g;
+            if (!EXACT) kr[kq][f] = make_uint4(0, 0, 0, 0);
+            if (EXACT || c < d) kr[kq][f] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.k) + at + c);
           }
         }
       }
-      if constexpr (BF) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int slot = 64 * i + l, c = slot % NC * 8;
-          const int64_t at = rows.row(slot / NC) * d + c;
-          if constexpr (F8) {
-            vr8[i] = make_uint2(0, 0);
-            if (c < d) vr8[i] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(p.v) + at);
-          } else {
-            vr[i] = make_uint4(0, 0, 0, 0);
-            if (c < d) vr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.v) + at);
-          }
+      for (int i = 0; i < NV; ++i) {
+        const int slot = 64 * i + l, c = slot % VS * VE;
+        const int64_t at = rows.template at<FULL>(slot / VS, d);
+        if constexpr (F8) {
+          vr[i] = load_e4m3x16<EXACT>(reinterpret_cast<const uint8_t*>(p.v) + at, c, d);
+        } else {
+          if (!EXACT) vr[i] = make_uint4(0, 0, 0, 0);
+          if (EXACT || c < d) vr[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.v) + at + c);
         }
       }
     };
+    auto fetch = [&]() __attribute__((always_inline)) {
+      // (plain fp32 has no registers for a second form)
+      if ((!BF && !F8) || d < DP || rows.last < 31) fetch_as(std::false_type(), std::false_type());
+      else fetch_as(std::true_type(), std::true_type());
+    };
     // wave w's tokens of tile t
     auto start = [&](int t) { return t * TILE + 32 * w; };
-    if (start(tile0) < len) {
-      rows.find(p.at, table, start(tile0), len, head_k, l, bad);
-      fetch(start(tile0));
+    auto there = [&](int t) { return t < tile1 && start(t) < len; };
+    if (there(tile0)) {
+      rows.look(p.at, table, start(tile0), len, l);
+      if (there(tile0 + 1)) ahead.look(p.at, table, start(tile0 + 1), len, l);
+      rows.find(p.at, start(tile0), head_k, l, bad);
+      fetch();
     }
-    Query<T, DP> q;
+    Query<T, DP, F8> q;
     q.load(reinterpret_cast<const T*>(p.q.p) + p.q.row * seq + p.q.head * (head_q + min(r, nq - 1)), d, g);
     float m = -INFINITY, sum = 0.f;
     f32x4 o[NDT];
@@ -258,48 +287,60 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args
     for (int t = tile0; t < tile1; ++t) {
       const int k0 = start(t);
       if (k0 >= len) break;
-      const Rows32<SMALL> here = rows;
-      const float scale_here = scale_v;
-      const bool more = t + 1 < tile1 && start(t + 1) < len;
-      if (more) rows.find(p.at, table, start(t + 1), len, head_k, l, bad);
+      const float scale_kt = F8 ? e8m0(scale_k) : 1.f, scale_vt = F8 ? e8m0(scale_v) : 1.f;
       f32x4 s[2];
 #pragma unroll
       for (int kq = 0; kq < 2; ++kq) {
         s[kq] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const float scale = F8 ? __shfl(scale_k, 16 * kq + r) : 1.f;
+        const float scale = F8 ? __shfl(scale_kt, 16 * kq + r) : 1.f;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
+          const uint32_t* word = reinterpret_cast<const uint32_t*>(&kr[kq][F8 ? (BF ? f / 2 : f / 4) : f]);
           if constexpr (BF) {
             bf16x8 kf;
-            if constexpr (F8) kf = bf16_of_e4m3(kr8[kq][f], scale);
-            else kf = *reinterpret_cast<const bf16x8*>(&kr[kq][f]);
+            if constexpr (F8) kf = bf16_of_e4m3(make_uint2(word[2 * (f % 2)], word[2 * (f % 2) + 1]), scale);
+            else kf = *reinterpret_cast<const bf16x8*>(word);
             s[kq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q.f[f], s[kq], 0, 0, 0);
           } else {
             f32x4 kf;
-            if constexpr (F8) kf = f32_of_e4m3(kr8[kq][f].x, scale);
-            else kf = *reinterpret_cast<const f32x4*>(&kr[kq][f]);
+            if constexpr (F8) kf = f32_of_e4m3(word[f % 4], scale);
+            else kf = *reinterpret_cast<const f32x4*>(word);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               s[kq] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], q.f[f][e], s[kq], 0, 0, 0);
           }
         }
       }
-      if constexpr (BF) {
+      if (k0 + 32 > len) {   // rows past the last token: 0 times the last one again could be NaN
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int slot = 64 * i + l, row = slot / NC;
-          uint4 x;
-          if constexpr (F8) {
-            const bf16x8 y = bf16_of_e4m3(vr8[i], __shfl(scale_here, row));
+        for (int i = 0; i < NV; ++i)
+          if (k0 + (64 * i + l) / VS >= len) vr[i] = make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int slot = 64 * i + l, row = slot / VS;
+        const float scale = F8 ? __shfl(scale_vt, row) : 1.f;
+        const uint32_t word[4] = {vr[i].x, vr[i].y, vr[i].z, vr[i].w};
+#pragma unroll
+        for (int j = 0; j < (F8 ? (BF ? 2 : 4) : 1); ++j) {
+          uint4 x = vr[i];
+          if constexpr (F8 && BF) {
+            const bf16x8 y = bf16_of_e4m3(make_uint2(word[2 * j], word[2 * j + 1]), scale);
             x = *reinterpret_cast<const uint4*>(&y);
-          } else {
-            x = vr[i];
+          } else if constexpr (F8) {
+            const f32x4 y = f32_of_e4m3(word[j], scale);
+            x = *reinterpret_cast<const uint4*>(&y);
           }
-          if (k0 + row >= len) x = make_uint4(0, 0, 0, 0);   // 0 times the last row again could be NaN
-          vt[w][row * NC + (slot % NC ^ mix<DP>(row))] = x;
+          const int chunk = slot % VS * (F8 ? (BF ? 2 : 4) : 1) + j;
+          vt[w][row * PC + (BF ? chunk ^ mix<DP>(row) : chunk)] = x;
         }
       }
-      if (more) fetch(start(t + 1));
+      if (there(t + 1)) {   // the next tile's bytes on their way, and where the one after it lies
+        rows = ahead;
+        rows.find(p.at, start(t + 1), head_k, l, bad);
+        if (there(t + 2)) ahead.look(p.at, table, start(t + 2), len, l);
+        fetch();
+      }
       float mx = -INFINITY;
 #pragma unroll
       for (int kq = 0; kq < 2; ++kq)
@@ -321,8 +362,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args
           s[kq][e] = exp2_any(s[kq][e] - ref);
           sum += s[kq][e];
         }
+      if (__any(c != 1.f)) {   // a new maximum somewhere
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) o[dt] *= c;
+        for (int dt = 0; dt < NDT; ++dt) o[dt] *= c;
+      }
       if constexpr (BF) {
         bf16x8 pb;
 #pragma unroll
@@ -344,24 +387,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void cache_attn_kernel(Args
           o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb, o[dt], 0, 0, 0);
         }
       } else {
+        const float* base = reinterpret_cast<const float*>(vt[w]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int vrow = 16 * (i / 4) + 4 * g + i % 4;
-          const int64_t row = here.row(vrow);
-          const float scale = F8 ? __shfl(scale_here, vrow) : 1.f;
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
-            const int col_v = 16 * dt + r;
-            float a = 0.f;
-            if (col_v < d && k0 + vrow < len) {
-              if constexpr (F8)
-                a = scale * __builtin_amdgcn_cvt_f32_fp8(reinterpret_cast<const uint8_t*>(p.v)[row * d + col_v], 0);
-              else
-                a = reinterpret_cast<const float*>(p.v)[row * d + col_v];
-            }
+            const float a = base[(16 * (i / 4) + 4 * g + i % 4) * (4 * PC) + 16 * dt + r];
             o[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[i / 4][i % 4], o[dt], 0, 0, 0);
           }
-        }
       }
     }
     // the block's four waves, in order
@@ -496,7 +529,9 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
 }
 
 template <class T, int DP, bool F8, bool SMALL>
-hipError_t launch(const Args& a, int joins, hipStream_t s) {
+hipError_t launch(Args& a, int64_t units, int joins, hipStream_t s) {
+  a.blocks = (int)(units < 256 * blocks_per_cu(DP, F8, sizeof(T) == 2) ? units : 256 * blocks_per_cu(DP, F8, sizeof(T) == 2));
+  static_assert(256 * blocks_per_cu(DP, F8, sizeof(T) == 2) <= MAX_BLOCKS, "parts and weights");
   if (a.blocks > 0) {
     hipLaunchKernelGGL((cache_attn_kernel<T, DP, F8, SMALL>), dim3(a.blocks), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
@@ -505,13 +540,13 @@ hipError_t launch(const Args& a, int joins, hipStream_t s) {
   return hipGetLastError();
 }
 template <class T, bool F8, bool SMALL>
-hipError_t by_width(const Args& a, int joins, hipStream_t s) {
-  return a.at.d <= 64    ? launch<T, 64, F8, SMALL>(a, joins, s)
-         : a.at.d <= 128 ? launch<T, 128, F8, SMALL>(a, joins, s)
-                         : launch<T, 256, F8, SMALL>(a, joins, s);
+hipError_t by_width(Args& a, int64_t units, int joins, hipStream_t s) {
+  return a.at.d <= 64    ? launch<T, 64, F8, SMALL>(a, units, joins, s)
+         : a.at.d <= 128 ? launch<T, 128, F8, SMALL>(a, units, joins, s)
+                         : launch<T, 256, F8, SMALL>(a, units, joins, s);
 }
-template <class T, bool F8> hipError_t by_page(const Args& a, int joins, hipStream_t s) {
-  return a.at.shift < 5 ? by_width<T, F8, true>(a, joins, s) : by_width<T, F8, false>(a, joins, s);
+template <class T, bool F8> hipError_t by_page(Args& a, int64_t units, int joins, hipStream_t s) {
+  return a.at.shift < 5 ? by_width<T, F8, true>(a, units, joins, s) : by_width<T, F8, false>(a, units, joins, s);
 }
 
 int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -538,13 +573,12 @@ hipError_t cache_attention(const CacheAttention& p, hipStream_t s) {
   a.scale = p.scale;
   a.group = p.q.heads / p.cache.heads;
   a.col_blocks = (a.group + QG - 1) / QG;
-  // no more blocks than units there can be
-  const int64_t units = ((int64_t)p.width * p.cache.page + TILE - 1) / TILE * p.cache.heads * a.col_blocks;
-  a.blocks = (int)(units >= MAX_BLOCKS ? MAX_BLOCKS : units * p.n_seq >= MAX_BLOCKS ? MAX_BLOCKS : units * p.n_seq);
+  // (no more blocks than units there can be)
+  const int64_t units = ((int64_t)p.width * p.cache.page + TILE - 1) / TILE * p.cache.heads * a.col_blocks * p.n_seq;
   const int joins = p.n_seq * p.q.heads;
   const bool f8 = p.cache.dtype == MPIPE_E4M3;
-  if (p.dtype == DT_BF16) return f8 ? by_page<bf16, true>(a, joins, s) : by_page<bf16, false>(a, joins, s);
-  return f8 ? by_page<float, true>(a, joins, s) : by_page<float, false>(a, joins, s);
+  if (p.dtype == DT_BF16) return f8 ? by_page<bf16, true>(a, units, joins, s) : by_page<bf16, false>(a, units, joins, s);
+  return f8 ? by_page<float, true>(a, units, joins, s) : by_page<float, false>(a, units, joins, s);
 }
 
 }  // namespace mpipe
