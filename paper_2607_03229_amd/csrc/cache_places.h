@@ -10,6 +10,17 @@ namespace mpipe {
 constexpr int64_t kCacheNone = -1;   // a row that is left out
 constexpr int64_t kCacheBad = -2;    // a place outside the tables or the pool
 
+// n / d for n below 2^32 (d at most 2^17) by a product: n (2^49 / d rounded up) / 2^49, off by less
+// than n / 2^49 < 1 / d.  Larger n are divided.
+struct Divide {
+  uint64_t mul;
+  uint32_t d;
+  __device__ __forceinline__ int64_t quotient(int64_t n) const {
+    return n >> 32 ? n / d : (int64_t)(__umul64hi((uint64_t)n << 15, mul));
+  }
+};
+inline Divide divide_by(uint32_t d) { return {((uint64_t(1) << 49) + d - 1) / d, d}; }
+
 struct CachePlaces {
   const int32_t *table, *seq, *pos;
   int64_t ld_table, first;   // first: added to the row, for its seq and pos
@@ -19,15 +30,25 @@ struct CachePlaces {
   __device__ __forceinline__ int64_t in_page(int32_t page, int32_t token, int head) const {
     return (((int64_t)page * heads + head) << shift) + (token & ((1 << shift) - 1));
   }
-  __device__ __forceinline__ int64_t of(int64_t row, int head) const {
-    row += first;
-    const int32_t t = pos[row];
-    const int64_t s = seq ? (int64_t)seq[row] : row;
-    if (t < 0 || s < 0) return kCacheNone;
-    if (s >= n_seq || (t >> shift) >= width) return kCacheBad;
-    const int32_t page = table[s * ld_table + (t >> shift)];
-    if (page < 0 || page >= n_pages) return kCacheBad;
-    return in_page(page, t, head);
+  // Of U rows at once.
+  template <int U>
+  __device__ __forceinline__ void of(const int64_t (&row)[U], const int (&head)[U], int64_t (&place)[U]) const {
+    int32_t t[U], page[U];
+    int64_t s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      t[u] = pos[row[u] + first];
+      s[u] = seq ? (int64_t)seq[row[u] + first] : row[u] + first;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      place[u] = t[u] < 0 || s[u] < 0 ? kCacheNone : s[u] >= n_seq || (t[u] >> shift) >= width ? kCacheBad : 0;
+      page[u] = place[u] == 0 ? table[s[u] * ld_table + (t[u] >> shift)] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (place[u] == 0) place[u] = page[u] < 0 || page[u] >= n_pages ? kCacheBad : in_page(page[u], t[u], head[u]);
+    }
   }
 };
 

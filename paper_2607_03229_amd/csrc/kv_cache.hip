@@ -1,8 +1,8 @@
 // Keys and values into and out of the pages of a cache (mpipe_op_cache_write / _read).
 //
-// A token's head is a unit of work: LPU lanes (the power of two that holds head_dim / 8) move
-// eight values each, so that the largest magnitude of a head is a few lane exchanges away when it
-// is quantised.  A power of two as its scale makes every step exact but the one rounding to
+// A token's head, its key and its value, is a unit of work: LPU lanes (the power of two that holds
+// head_dim / 8) move eight values of each, so that the largest magnitude of a head is a few lane
+// exchanges away when it is quantised.  A power of two as its scale makes every step exact but the one rounding to
 // e4m3, and what is read back is exact in bf16.  Bound by HBM for prompts, by one chain of loads
 // (position, page, row) for single tokens.
 #include "attn_kernels.h"
@@ -21,6 +21,7 @@ struct RowArgs {
   AttnView k, v;
   CachePlaces at;
   int64_t rows;
+  Divide by_heads;
   int32_t* status;
 };
 
@@ -57,7 +58,7 @@ __device__ __forceinline__ int scale_exponent(float top) {
   return top == 0.f ? -120 : min(max(e, -120), 120);
 }
 
-// Eight values of a unit; `lane` counts within it.  Every lane of a unit calls this.
+// Eight values of a head, and its scale; `lane` counts within it.  Every lane of a unit calls this.
 template <int LPU>
 __device__ __forceinline__ void store_e4m3(uint8_t* p, uint8_t* scale, float (&x)[8], int lane,
                                            bool real) {
@@ -80,71 +81,113 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, uint8_t* scale, float (&x
   w = 0;
   w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * f, x[5] * f, w, false);
   out.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[6] * f, x[7] * f, w, true);
-  *reinterpret_cast<uint2*>(p + 8 * lane) = out;
+  *reinterpret_cast<uint2*>(p) = out;
   if (lane == 0) *scale = (uint8_t)(e + 127);
 }
 
-// A unit: (row, key or value, head), heads fastest, so that neighbours read one row of a product.
-template <class T, class C, int LPU, bool WRITE>
+// A unit: (row, head), its key and its value; heads fastest, so that neighbours read one row of a
+// product.  A thread takes U units, so that their chains of loads (position, page, values) run
+// beside each other.
+template <class T, class C, int LPU, int U, bool WRITE>
 __global__ __launch_bounds__(256) void rows_kernel(RowArgs a) {
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPU;
   const int lane = threadIdx.x % LPU, heads = a.at.heads, d = a.at.d;
-  int64_t row = unit / (2 * heads);
-  const bool in = row < a.rows;
-  row = in ? row : a.rows - 1;
-  const int rest = (int)(unit % (2 * heads)), side = rest / heads, head = rest % heads;
-  const int64_t place = in ? a.at.of(row, head) : kCacheNone;
-  const bool real = place >= 0 && 8 * lane < d;
-  if (in && place == kCacheBad && rest == 0 && lane == 0 && a.status) *a.status = 1;
-  const AttnView& v = side ? a.v : a.k;
-  T* x = reinterpret_cast<T*>(const_cast<void*>(v.p)) + v.row * row + v.head * head + 8 * lane;
-  C* c = reinterpret_cast<C*>(side ? a.cv : a.ck) + (place >= 0 ? place : 0) * d;
-  uint8_t* s = (side ? a.sv : a.sk) + (place >= 0 ? place : 0);
-  float y[8];
+  const int64_t unit0 = ((int64_t)blockIdx.x * 256 * U + threadIdx.x) / LPU;
+  bool in[U];
+  int64_t row[U], place[U];
+  int head[U];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = 0.f;
-  if constexpr (WRITE) {
-    if (real) load8(x, y);
-    if constexpr (sizeof(C) == 1) store_e4m3<LPU>(reinterpret_cast<uint8_t*>(c), s, y, lane, real);
-    else if (real) store8(c + 8 * lane, y);
-  } else {
-    if (place == kCacheNone || 8 * lane >= d) return;
-    if (place == kCacheBad) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = NAN;
-    } else if constexpr (sizeof(C) == 1) {
-      load8_e4m3(reinterpret_cast<const uint8_t*>(c) + 8 * lane, e8m0(*s), y);
-    } else {
-      load8(c + 8 * lane, y);
-    }
-    store8(x, y);
+  for (int u = 0; u < U; ++u) {
+    const int64_t unit = unit0 + u * (256 / LPU);
+    row[u] = a.by_heads.quotient(unit);
+    head[u] = (int)(unit - row[u] * heads);
+    in[u] = row[u] < a.rows;
+    row[u] = in[u] ? row[u] : a.rows - 1;
   }
+  a.at.template of<U>(row, head, place);
+  float y[U][2][8];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!in[u]) place[u] = kCacheNone;
+    if (place[u] == kCacheBad && head[u] == 0 && lane == 0 && a.status) *a.status = 1;
+    const float none = WRITE || place[u] != kCacheBad ? 0.f : NAN;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[u][i / 8][i % 8] = none;
+    if (place[u] >= 0 && 8 * lane < d) {
+      if constexpr (WRITE) {
+        load8(reinterpret_cast<const T*>(a.k.p) + a.k.row * row[u] + a.k.head * head[u] + 8 * lane, y[u][0]);
+        load8(reinterpret_cast<const T*>(a.v.p) + a.v.row * row[u] + a.v.head * head[u] + 8 * lane, y[u][1]);
+      } else if constexpr (sizeof(C) == 1) {
+        const int64_t at = place[u] * d + 8 * lane;
+        load8_e4m3(reinterpret_cast<const uint8_t*>(a.ck) + at, e8m0(a.sk[place[u]]), y[u][0]);
+        load8_e4m3(reinterpret_cast<const uint8_t*>(a.cv) + at, e8m0(a.sv[place[u]]), y[u][1]);
+      } else {
+        const int64_t at = place[u] * d + 8 * lane;
+        load8(reinterpret_cast<const C*>(a.ck) + at, y[u][0]);
+        load8(reinterpret_cast<const C*>(a.cv) + at, y[u][1]);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const bool real = place[u] >= 0 && 8 * lane < d;
+    if constexpr (WRITE) {
+      const int64_t safe = place[u] >= 0 ? place[u] : 0, at = safe * d + 8 * lane;
+      if constexpr (sizeof(C) == 1) {
+        store_e4m3<LPU>(reinterpret_cast<uint8_t*>(a.ck) + at, a.sk + safe, y[u][0], lane, real);
+        store_e4m3<LPU>(reinterpret_cast<uint8_t*>(a.cv) + at, a.sv + safe, y[u][1], lane, real);
+      } else if (real) {
+        store8(reinterpret_cast<C*>(a.ck) + at, y[u][0]);
+        store8(reinterpret_cast<C*>(a.cv) + at, y[u][1]);
+      }
+    } else if (place[u] != kCacheNone && 8 * lane < d) {
+      store8(static_cast<T*>(const_cast<void*>(a.k.p)) + a.k.row * row[u] + a.k.head * head[u] + 8 * lane, y[u][0]);
+      store8(static_cast<T*>(const_cast<void*>(a.v.p)) + a.v.row * row[u] + a.v.head * head[u] + 8 * lane, y[u][1]);
+    }
+  }
+}
+
+// From eight blocks a CU on, a thread takes two units of an 8-bit cache, whose loads are short.
+// Measured on MI355X, us of write / read at one, two and four units a thread, 65,536 bf16 rows of
+// 8 heads of 128: 8 bits 103 / 93, 91 / 90, 102 / 102 (4.5 TB/s); bf16 95 / 94 (5.7 TB/s),
+// 100 / 100, 106 / 111.  A key and its value in units of their own, each with a chain of its own:
+// 141 / 148 and 118 / 123.
+constexpr int64_t MANY_BLOCKS = 2048;
+
+template <class T, class C, int LPU, bool WRITE>
+hipError_t launch_units(const RowArgs& a, hipStream_t s) {
+  constexpr int MANY = sizeof(C) == 1 ? 2 : 1;
+  const int64_t blocks = (a.rows * a.at.heads * LPU + 255) / 256;
+  if (MANY == 1 || blocks < MANY_BLOCKS)
+    hipLaunchKernelGGL((rows_kernel<T, C, LPU, 1, WRITE>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((rows_kernel<T, C, LPU, MANY, WRITE>), dim3((unsigned)((blocks + MANY - 1) / MANY)),
+                       dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 template <class T, class C, bool WRITE>
 hipError_t launch(const RowArgs& a, hipStream_t s) {
   int lpu = 1;
   while (8 * lpu < a.at.d) lpu *= 2;
-  // units of a launch: 2^23 blocks at most
+  // lanes of a launch: 2^31 at most
   RowArgs b = a;
-  const int64_t step = ((int64_t(1) << 31) / lpu) / (2 * a.at.heads);
+  const int64_t step = ((int64_t(1) << 31) / lpu) / a.at.heads;
   for (int64_t r = 0; r < a.rows; r += step) {
     b.rows = a.rows - r < step ? a.rows - r : step;
     b.at.first = r;
     const int esz = sizeof(T);
     b.k.p = (const char*)a.k.p + r * a.k.row * esz;
     b.v.p = (const char*)a.v.p + r * a.v.row * esz;
-    const int64_t blocks = (b.rows * 2 * a.at.heads * lpu + 255) / 256;
-    const dim3 grid((unsigned)blocks), block(256);
+    hipError_t e;
     switch (lpu) {
-      case 1: hipLaunchKernelGGL((rows_kernel<T, C, 1, WRITE>), grid, block, 0, s, b); break;
-      case 2: hipLaunchKernelGGL((rows_kernel<T, C, 2, WRITE>), grid, block, 0, s, b); break;
-      case 4: hipLaunchKernelGGL((rows_kernel<T, C, 4, WRITE>), grid, block, 0, s, b); break;
-      case 8: hipLaunchKernelGGL((rows_kernel<T, C, 8, WRITE>), grid, block, 0, s, b); break;
-      case 16: hipLaunchKernelGGL((rows_kernel<T, C, 16, WRITE>), grid, block, 0, s, b); break;
-      default: hipLaunchKernelGGL((rows_kernel<T, C, 32, WRITE>), grid, block, 0, s, b); break;
+      case 1: e = launch_units<T, C, 1, WRITE>(b, s); break;
+      case 2: e = launch_units<T, C, 2, WRITE>(b, s); break;
+      case 4: e = launch_units<T, C, 4, WRITE>(b, s); break;
+      case 8: e = launch_units<T, C, 8, WRITE>(b, s); break;
+      case 16: e = launch_units<T, C, 16, WRITE>(b, s); break;
+      default: e = launch_units<T, C, 32, WRITE>(b, s); break;
     }
-    if (hipError_t e = hipGetLastError()) return e;
+    if (e) return e;
   }
   return hipSuccess;
 }
@@ -160,6 +203,7 @@ hipError_t rows(const CacheRows& p, hipStream_t s) {
   a.v = {p.v.p, p.v.row, p.v.head};
   a.at = cache_places(p.cache, p.table, p.ld_table, p.n_seq, p.width, p.seq, p.pos);
   a.rows = p.rows;
+  a.by_heads = divide_by(p.cache.heads);
   a.status = p.status;
   if (p.dtype == DT_BF16) {
     switch (p.cache.dtype) {
