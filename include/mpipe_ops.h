@@ -278,7 +278,7 @@ mpipe_status mpipe_op_causal_attention_fwd(int32_t dtype, int32_t head_dim, int6
 
 /* Its backward: dq, dk, dv overwritten (a key that no query sees gets 0) from d_o, the gradient
  * of o, and the forward's inputs, o and lse.  lse itself has no gradient here.  The gradients of a
- * key head are summed over the query heads of its group, in a fixed order.  scratch:
+ * key head are summed over the query heads of its group, in an order that the arguments fix.  scratch:
  * mpipe_op_causal_attention_scratch_bytes, aligned to 16 bytes, not kept. */
 mpipe_status mpipe_op_causal_attention_bwd(int32_t dtype, int32_t head_dim, int64_t rows_q,
                                            int64_t rows_k, const mpipe_heads* d_o,

@@ -33,9 +33,10 @@ struct CausalArgs {
   AttnView q, k, v, o, d_o, dq, dk, dv;
   float* lse;
   float* delta;   // backward: [2][heads][rows_q] of what one kernel leaves to the next
+  float* partial;   // dkdv in parts: [blocks][keys of a block][2][width] as the lanes hold them
   int64_t ld_lse, rows_q;
   float scale;
-  int d, heads_k, group;
+  int d, heads_k, group, parts;   // parts: blocks that share a key tile's queries, of dkdv
 };
 static_assert(sizeof(CausalArgs) <= 4000, "a launch's arguments");
 // Any dtype, alignment and head_dim of at most 256 (causal_general.hip): items of kGeneralRows.

@@ -1,5 +1,6 @@
 // Causal attention with grouped heads over sequences (mpipe_op_causal_attention_fwd / _bwd):
 // the launches.
+#include <algorithm>
 #include <initializer_list>
 
 #include "attn_kernels.h"
@@ -23,6 +24,8 @@ CausalArgs args_of(const CausalProblem& p) {
   a.lse = p.lse;
   a.ld_lse = p.ld_lse;
   a.delta = p.scratch;
+  a.partial = nullptr;
+  a.parts = 1;
   a.rows_q = p.rows_q;
   a.scale = p.scale;
   a.d = p.head_dim;
@@ -30,6 +33,22 @@ CausalArgs args_of(const CausalProblem& p) {
   a.group = p.q.heads / p.k.heads;
   return a;
 }
+
+// Blocks of dK and dV in parts, at most, and query tiles of a part, at least: few key tiles (single
+// or short sequences, few key heads) leave CUs without one, so the queries of a key tile, of all
+// heads of its group, are cut and the parts' sums joined.  Measured on MI355X, us of a whole
+// backward without parts, with 256, 512 and 1024 blocks, one sequence, 28/4 heads of 128: 1024
+// rows 194, 85, 91, 120; 4096 rows 734, 516, 440, 460; 8192 rows 1866, 1862, 1494, 1506.  Two to
+// twelve tiles: within 10 %.
+constexpr int64_t kSplitBlocks = 512, kPartTiles = 4;
+int64_t split_blocks(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k, int d) {
+  if (heads_k == 0) return 0;
+  const int rows = 16 * causal_k_waves(causal_width(d));
+  const int64_t parts = (rows_q + 63) / 64 * (heads_q / heads_k) / kPartTiles;
+  const int64_t tiles = (rows_k + rows - 1) / rows * heads_k;
+  return parts < 2 || tiles > kSplitBlocks / 2 ? 0 : std::min(kSplitBlocks, parts * tiles);
+}
+int64_t delta_bytes(int64_t rows_q, int heads_q) { return (rows_q * heads_q * 8 + 31) / 16 * 16; }
 
 // All items, as many to a launch as its arguments and 2^23 blocks hold.
 template <class Launch>
@@ -72,7 +91,10 @@ hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
 
 size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k,
                                 int head_dim) {
-  return (size_t)rows_q * heads_q * 2 * sizeof(float) + 16;
+  const int width = causal_width(head_dim);
+  return (size_t)(delta_bytes(rows_q, heads_q) +
+                  (head_dim > 128 ? 0 : split_blocks(rows_q, heads_q, rows_k, heads_k, head_dim) *
+                                            16 * causal_k_waves(width) * 2 * width * 4));
 }
 
 hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
@@ -82,7 +104,16 @@ hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
     if (hipError_t e = in_pieces(p, a, false, 32 * causal_q_waves(width), p.q.heads,
                                  [&](const CausalArgs& b, int n) { return causal_bf16_dq(b, n, s); }))
       return e;
-    return in_pieces(p, a, true, 16 * causal_k_waves(width), p.k.heads,
+    const int rows = 16 * causal_k_waves(width);
+    int64_t tiles = 0, longest = 0;
+    for (const AttnSeq& q : p.seqs) {
+      tiles += (q.k_len + rows - 1) / rows * p.k.heads;
+      longest = std::max<int64_t>(longest, (q.q_len + 63) / 64 * a.group);
+    }
+    const int64_t blocks = split_blocks(p.rows_q, p.q.heads, p.rows_k, p.k.heads, p.head_dim);
+    if (tiles > 0) a.parts = (int)std::max<int64_t>(1, std::min(blocks / tiles, longest / kPartTiles));
+    a.partial = p.scratch + delta_bytes(p.rows_q, p.q.heads) / 4;
+    return in_pieces(p, a, true, rows, p.k.heads * a.parts,
                      [&](const CausalArgs& b, int n) { return causal_bf16_dkdv(b, n, s); });
   }
   if (hipError_t e = in_pieces(p, a, false, kGeneralRows, 8 * p.q.heads, [&](const CausalArgs& b, int n) {

@@ -335,19 +335,26 @@ __device__ __forceinline__ void add_pairs(f32x16 (&acc)[Tile<DP>::DT], const bf1
   }
 }
 
-// Row c of an output from accumulators that hold its columns as rows, times f.
+// Columns 32 dt .. 32 dt + 31 of row c of an output from an accumulator that holds them as rows,
+// times f.
+__device__ __forceinline__ void store_columns(bf16* row, const f32x16& acc, float f, int dt, int d, int h) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (32 * dt + 8 * i >= d) continue;
+    bf16 x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (bf16)(acc[4 * i + e] * f);
+    *reinterpret_cast<uint2*>(row + 32 * dt + 8 * i + 4 * h) = *reinterpret_cast<uint2*>(x);
+  }
+}
 template <int DP>
 __device__ __forceinline__ void store_row(bf16* row, const f32x16 (&acc)[Tile<DP>::DT], float f, int d, int h) {
 #pragma unroll
-  for (int dt = 0; dt < Tile<DP>::DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (32 * dt + 8 * i >= d) continue;
-      bf16 x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (bf16)(acc[dt][4 * i + e] * f);
-      *reinterpret_cast<uint2*>(row + 32 * dt + 8 * i + 4 * h) = *reinterpret_cast<uint2*>(x);
-    }
+  for (int dt = 0; dt < Tile<DP>::DT; ++dt) store_columns(row, acc[dt], f, dt, d, h);
+}
+// Values 4 i .. 4 i + 3 of an accumulator.
+__device__ __forceinline__ f32x4 f32x4_of(const f32x16& acc, int i) {
+  return f32x4{acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
 }
 
 }  // namespace mpipe

@@ -181,7 +181,8 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
 // dO^T P; the second, a slot behind, dP = dO V^T, dS from the P that the first left in LDS, and
 // dK^T += Q^T dS.  Neither holds more than one accumulator of head_dim columns, one operand and
 // one tile of scores, so two waves fit a SIMD; they run on the same one (w and w + 4), and one's
-// products meet the other's exponentials.
+// products meet the other's exponentials.  Where there are few key tiles, p.parts blocks share one,
+// and a kernel of its own adds what they leave in fp32 (67 MB at most: 12 us).
 template <int DP, int NWV>
 __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) {
   using T = Tile<DP>;
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   __shared__ uint4 qs[KSTAGES][SL], ds_[KSTAGES][SL];
   __shared__ uint4 weights[NWV / 2][4][64];      // P of one tile, bf16, as the lanes hold it
   __shared__ __attribute__((aligned(16))) float nl2s[KSTAGES][64], nds[KSTAGES][64];
-  const AttnPlace a = attn_place(p, 1, 16 * NWV);
+  const AttnPlace a = attn_place(p, p.parts, 16 * NWV);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
   const int c = l & 31, h = l >> 5, pair = w % (NWV / 2);
   const bool of_second = w >= NWV / 2;
@@ -197,7 +198,11 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   const int k0 = a.r0 + 32 * pair, row = min(k0 + c, a.k_len - 1);
   const int first_q = max(row - shift, 0);            // first query that sees the lane's key
   const int t0 = max(a.r0 - shift, 0) / 64;           // first tile with a query that sees any
-  const int n_tiles = max((a.q_len + 63) / 64 - t0, 0), nt = n_tiles * p.group;
+  const int n_tiles = max((a.q_len + 63) / 64 - t0, 0);
+  // the block's part of the group's tiles, and where it begins
+  const int first_t = (int)((int64_t)n_tiles * p.group * a.gq / p.parts);
+  const int nt = (int)((int64_t)n_tiles * p.group * (a.gq + 1) / p.parts) - first_t;
+  const int first_head = nt > 0 ? first_t / n_tiles : 0, first_tile = nt > 0 ? first_t % n_tiles : 0;
   const int whole_q = max(min(k0 + 31, a.k_len - 1) - shift, 0);   // sees all of the wave's keys
   const float sl2 = p.scale * kLog2e;
   const uint32_t qs0 = lds_at(qs), ds0 = lds_at(ds_), nl2s0 = lds_at(nl2s), nds0 = lds_at(nds);
@@ -219,13 +224,13 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
     // the first waves' rows are of Q and columns of dO, the second ones' the other way round
     const uint32_t rows0 = second ? ds0 : qs0, cols0 = second ? qs0 : ds0;
     // Tiles head by head: Q, dO, and of each query -lse * log2(e) (the first waves') or -dO . O
-    const int head0 = a.head_k * p.group;
+    const int head0 = a.head_k * p.group + first_head, t1 = t0 + first_tile;
     Feed qf, of;
-    qf.start(head_of(p.q, head0, a.q_row), p.q.row, t0, a.q_len, p.d);
-    of.start(head_of(p.d_o, head0, a.q_row), p.d_o.row, t0, a.q_len, p.d);
-    uint64_t stats = (uint64_t)(p.delta + ((second ? (int64_t)p.heads_k * p.group : 0) + head0) * p.rows_q + a.q_row + 64 * t0);
+    qf.start(head_of(p.q, head0, a.q_row), p.q.row, t1, a.q_len, p.d);
+    of.start(head_of(p.d_o, head0, a.q_row), p.d_o.row, t1, a.q_len, p.d);
+    uint64_t stats = (uint64_t)(p.delta + ((second ? (int64_t)p.heads_k * p.group : 0) + head0) * p.rows_q + a.q_row + 64 * t1);
     const uint32_t stats_tail = 4u * (uint32_t)((a.q_len - 1) % 64 + 1);
-    int heads_left = n_tiles > 0 ? p.group - 1 : 0;
+    int heads_left = nt > 0 ? p.group - 1 - first_head : 0;
     struct Next {
       buffer_t q, d_o, stats;
     };
@@ -254,7 +259,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
     };
     f32x16 s[2];
     bf16x8 x[4], first[AHEAD];
-    int tile_t = 0;   // tile t's place among those of its head
+    int tile_t = first_tile;   // tile t's place among those of its head
     auto cut = [&](int r0) { return r0 < whole_q || r0 + 64 > a.q_len; };
     auto fetch = [&](uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
@@ -376,8 +381,39 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
     if (of_second) walk(std::true_type(), std::true_type());
     else walk(std::true_type(), std::false_type());
   }
+  if (p.parts > 1) {
+    f32x4* out = reinterpret_cast<f32x4*>(p.partial) + ((int64_t)blockIdx.x * NWV + w) * (256 * DT) + l;
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) out[64 * i] = f32x4_of(acc[i >> 2], i & 3);
+    return;
+  }
   if (k0 + c >= a.k_len) return;
   store_row<DP>(out_of(of_second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, of_second ? p.scale : 1.f, p.d, h);
+}
+
+// The sums of a key tile's parts, in their order, 32 columns a block; lanes as above.
+template <int DP, int NWV>
+__global__ __launch_bounds__(64 * NWV) void causal_parts_kernel(CausalArgs p) {
+  constexpr int DT = Tile<DP>::DT;
+  const AttnPlace a = attn_place(p, 1, 16 * NWV);
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, c = l & 31, h = l >> 5, dt = blockIdx.y;
+  const int row = a.r0 + 32 * (w % (NWV / 2)) + c;
+  const bool of_second = w >= NWV / 2;
+  const int64_t item = blockIdx.x / p.heads_k;
+  f32x16 acc = zero16();
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i) {
+    const int64_t block = (item * p.parts + i) * p.heads_k + a.head_k;
+    const f32x4* in = reinterpret_cast<const f32x4*>(p.partial) + (block * NWV + w) * (256 * DT) + 256 * dt + l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 x = in[64 * j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[4 * j + e] += x[e];
+    }
+  }
+  if (row >= a.k_len) return;
+  store_columns(out_of(of_second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, of_second ? p.scale : 1.f, dt, p.d, h);
 }
 
 template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, hipStream_t s) {
@@ -388,8 +424,11 @@ template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, hipStream
 }
 template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, hipStream_t s) {
   constexpr int NWV = causal_k_waves(DP);
-  hipLaunchKernelGGL((causal_dkdv_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k), dim3(64 * NWV),
-                     0, s, a);
+  hipLaunchKernelGGL((causal_dkdv_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.parts),
+                     dim3(64 * NWV), 0, s, a);
+  if (a.parts > 1)
+    hipLaunchKernelGGL((causal_parts_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k, DP / 32),
+                       dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
 }
 
