@@ -36,7 +36,9 @@ struct CausalArgs {
   float* partial;   // dkdv in parts: [blocks][keys of a block][2][width] as the lanes hold them
   int64_t ld_lse, rows_q;
   float scale;
-  int d, heads_k, group, parts;   // parts: blocks that share a key tile's queries, of dkdv
+  int d, heads_k, group;
+  int q_waves;   // of a block of 32 queries each, fwd and dq
+  int parts;     // parts: blocks that share a key tile's queries, of dkdv
 };
 static_assert(sizeof(CausalArgs) <= 4000, "a launch's arguments");
 // Any dtype, alignment and head_dim of at most 256 (causal_general.hip): items of kGeneralRows.

@@ -11,6 +11,20 @@ namespace {
 
 AttnView view(const HeadView& v) { return {v.p, v.row, v.head}; }
 
+// Waves of a block of fwd and dq.  A width of 96 at most: see causal_q_waves.  At 128 a CU has one
+// block of either kind, so four waves pay only where even blocks of eight leave most CUs idle.
+// Measured on MI355X, us of forward and dQ, one sequence, 28/4 heads of 128, 8 -> 4 waves: 256 rows
+// (28 blocks) 17 -> 15 and 23 -> 18; 512 rows 22 -> 21 and 31 -> 26; 1024 rows (112 blocks) 34 -> 35
+// and 45 -> 41; 2048 rows 59 -> 70 and 79 -> 85.
+constexpr int64_t kFewBlocks = 64;
+int q_waves(const CausalProblem& p) {
+  const int most = causal_q_waves(causal_width(p.head_dim));
+  if (most == 4) return 4;
+  int64_t blocks = 0;
+  for (const AttnSeq& q : p.seqs) blocks += (q.q_len + 255) / 256 * p.q.heads;
+  return blocks > kFewBlocks ? most : 4;
+}
+
 CausalArgs args_of(const CausalProblem& p) {
   CausalArgs a;
   a.q = view(p.q);
@@ -26,6 +40,7 @@ CausalArgs args_of(const CausalProblem& p) {
   a.delta = p.scratch;
   a.partial = nullptr;
   a.parts = 1;
+  a.q_waves = q_waves(p);
   a.rows_q = p.rows_q;
   a.scale = p.scale;
   a.d = p.head_dim;
@@ -79,8 +94,7 @@ bool tiled(const CausalProblem& p, std::initializer_list<const HeadView*> views)
 hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
   if (tiled(p, {&p.q, &p.k, &p.v, &p.o})) {
-    const int rows = 32 * causal_q_waves(causal_width(p.head_dim));
-    return in_pieces(p, a, false, rows, p.q.heads, [&](const CausalArgs& b, int n) {
+    return in_pieces(p, a, false, 32 * a.q_waves, p.q.heads, [&](const CausalArgs& b, int n) {
       return causal_bf16_fwd(b, n, s);
     });
   }
@@ -101,7 +115,7 @@ hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
   if (tiled(p, {&p.q, &p.k, &p.v, &p.o, &p.d_o, &p.dq, &p.dk, &p.dv})) {
     const int width = causal_width(p.head_dim);
-    if (hipError_t e = in_pieces(p, a, false, 32 * causal_q_waves(width), p.q.heads,
+    if (hipError_t e = in_pieces(p, a, false, 32 * a.q_waves, p.q.heads,
                                  [&](const CausalArgs& b, int n) { return causal_bf16_dq(b, n, s); }))
       return e;
     const int rows = 16 * causal_k_waves(width);

@@ -416,8 +416,7 @@ __global__ __launch_bounds__(64 * NWV) void causal_parts_kernel(CausalArgs p) {
   store_columns(out_of(of_second ? p.dk : p.dv, a.head_k, a.k_row + row), acc, of_second ? p.scale : 1.f, dt, p.d, h);
 }
 
-template <int DP> hipError_t launch_dq(const CausalArgs& a, int items, hipStream_t s) {
-  constexpr int NWV = causal_q_waves(DP);
+template <int DP, int NWV> hipError_t launch_dq(const CausalArgs& a, int items, hipStream_t s) {
   hipLaunchKernelGGL((causal_dq_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
                      dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
@@ -436,10 +435,10 @@ template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, hipStre
 
 hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s) {
   switch (causal_width(a.d)) {
-    case 32: return launch_dq<32>(a, items, s);
-    case 64: return launch_dq<64>(a, items, s);
-    case 96: return launch_dq<96>(a, items, s);
-    default: return launch_dq<128>(a, items, s);
+    case 32: return launch_dq<32, 4>(a, items, s);
+    case 64: return launch_dq<64, 4>(a, items, s);
+    case 96: return launch_dq<96, 4>(a, items, s);
+    default: return a.q_waves == 4 ? launch_dq<128, 4>(a, items, s) : launch_dq<128, 8>(a, items, s);
   }
 }
 hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s) {

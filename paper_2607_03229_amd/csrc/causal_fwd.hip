@@ -186,8 +186,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
   if (h == 0 && p.lse) p.lse[head * p.ld_lse + a.q_row + row] = (m + log2f(sum)) * kLn2;
 }
 
-template <int DP> hipError_t launch(const CausalArgs& a, int items, hipStream_t s) {
-  constexpr int NWV = causal_q_waves(DP);
+template <int DP, int NWV> hipError_t launch(const CausalArgs& a, int items, hipStream_t s) {
   hipLaunchKernelGGL((causal_fwd_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
                      dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
@@ -197,10 +196,10 @@ template <int DP> hipError_t launch(const CausalArgs& a, int items, hipStream_t 
 
 hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s) {
   switch (causal_width(a.d)) {
-    case 32: return launch<32>(a, items, s);
-    case 64: return launch<64>(a, items, s);
-    case 96: return launch<96>(a, items, s);
-    default: return launch<128>(a, items, s);
+    case 32: return launch<32, 4>(a, items, s);
+    case 64: return launch<64, 4>(a, items, s);
+    case 96: return launch<96, 4>(a, items, s);
+    default: return a.q_waves == 4 ? launch<128, 4>(a, items, s) : launch<128, 8>(a, items, s);
   }
 }
 
