@@ -48,8 +48,8 @@ hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStrea
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);
 
 // bf16, 16-byte aligned views, head_dim of at most 128 (causal_fwd.hip, causal_bwd.hip): items of 32
-// queries a wave, and for dkdv of 16 keys a wave.  dq writes to `delta` what dkdv reads: -lse *
-// log2(e), then -dO . O.
+// queries a wave, and for dkdv of 16 keys a wave.  dq writes to
+// `delta` what dkdv reads of each query.
 hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s);

@@ -33,6 +33,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
   const bf16* V = head_of(p.v, a.head_k, a.k_row);
   const float sl2 = p.scale * kLog2e;
 
+  const float nl2 = -p.lse[head * p.ld_lse + a.q_row + row] * kLog2e;
   float nd = 0.f;
   {
     RowOp<DP> o, d_o;
@@ -43,8 +44,30 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dq_kernel(CausalArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) nd = fmaf((float)o.f[f][e], -(float)d_o.f[f][e], nd);
     nd = add_halves(nd);
+    if (wave_keys > 0 && wave_keys <= 32) {
+      // dO . O is the sum of P dP, but for the rounding of O.  Of few keys O is as large as their
+      // values, and its rounding as large as that of all else: what the sum of P (dP - dO . O)
+      // leaves is taken off.  (350 rows of normal values: error of dQ 0.0028 -> 0.0024, of which
+      // 0.0017 is its own rounding.)
+      RowOp<DP> q, k, v;
+      load_row<DP>(q, head_of(p.q, head, a.q_row + row), p.d, h);
+      load_row<DP>(k, K + min(c, a.k_len - 1) * p.k.row, p.d, h);
+      load_row<DP>(v, V + min(c, a.k_len - 1) * p.v.row, p.d, h);
+      f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+      for (int f = 0; f < T::KF; ++f) {
+        s = mfma(k.f[f], q.f[f], s);
+        dp = mfma(v.f[f], d_o.f[f], dp);
+      }
+      float off = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = exp2_fast(fmaf(s[i], sl2, nl2)) * (dp[i] + nd);
+        off += acc_row(i, 0) <= last_key - 4 * h ? x : 0.f;
+      }
+      nd -= add_halves(off);
+    }
   }
-  const float nl2 = -p.lse[head * p.ld_lse + a.q_row + row] * kLog2e;
   if (h == 0 && q0 + c < a.q_len) {
     float* out = p.delta + (int64_t)head * p.rows_q + a.q_row + row;
     out[0] = nl2;
@@ -188,7 +211,9 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
   using T = Tile<DP>;
   constexpr int SL = T::SLOTS, DT = T::DT;
   __shared__ uint4 qs[KSTAGES][SL], ds_[KSTAGES][SL];
-  __shared__ uint4 weights[NWV / 2][4][64];      // P of one tile, bf16, as the lanes hold it
+  // P of one tile as the lanes hold it: the upper 16 bits of fp32, and the next eight.  (Rounded to
+  // bf16, as it enters dV, it would also be dS's largest error: dK's 0.0024 -> 0.0030.)
+  __shared__ uint4 weights[NWV / 2][4][64], weights_low[NWV / 2][2][64];
   __shared__ __attribute__((aligned(16))) float nl2s[KSTAGES][64], nds[KSTAGES][64];
   const AttnPlace a = attn_place(p, p.parts, 16 * NWV);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
@@ -296,12 +321,19 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
           }
         }
       if constexpr (second) {
+        const uint4 v2[2] = {weights_low[pair][0][l], weights_low[pair][1][l]};
+        const uint32_t* low = reinterpret_cast<const uint32_t*>(v2);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint4 v = weights[pair][j][l];
-          const bf16x8 pw = *reinterpret_cast<const bf16x8*>(&v);
+          const uint32_t* up = reinterpret_cast<const uint32_t*>(&v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s[j >> 1][8 * (j & 1) + e] *= (float)pw[e];
+          for (int e = 0; e < 8; ++e) {
+            // (selector bytes 0 to 3 are of the second word, 4 to 7 of the first, 12 is zero)
+            const uint32_t which = (e & 1 ? 0x0706000cu : 0x0504000cu) | (e & 3) << 8;
+            s[j >> 1][8 * (j & 1) + e] *=
+                __uint_as_float(__builtin_amdgcn_perm(up[e >> 1], low[2 * j + (e >> 2)], which));
+          }
         }
       }
       // (a weight that does not count is 0; its dS only needs to be told where dP is not finite)
@@ -315,12 +347,25 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_dkdv_kernel(CausalArgs p) 
             s[q2][i] = r >= lo && r < hi ? s[q2][i] : 0.f;
           }
       }
+      if constexpr (!second) {
+        uint32_t up[16], low[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(s[i >> 2][4 * (i & 3) + e]);
+          up[2 * i] = __builtin_amdgcn_perm(v[1], v[0], 0x07060302u);
+          up[2 * i + 1] = __builtin_amdgcn_perm(v[3], v[2], 0x07060302u);
+          low[i] = __builtin_amdgcn_perm(v[3], v[2], 0x05010c0cu) | __builtin_amdgcn_perm(v[1], v[0], 0x0c0c0501u);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) weights[pair][j][l] = make_uint4(up[4 * j], up[4 * j + 1], up[4 * j + 2], up[4 * j + 3]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          weights_low[pair][j][l] = make_uint4(low[4 * j], low[4 * j + 1], low[4 * j + 2], low[4 * j + 3]);
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = pack8(s[j >> 1], j & 1);
-      if constexpr (!second) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) weights[pair][j][l] = *reinterpret_cast<const uint4*>(&x[j]);
-      }
     };
     // scores of the next tile, sums of this one
     auto products = [&](int r0, uint32_t at, uint32_t next, const Next& then) __attribute__((always_inline)) {
