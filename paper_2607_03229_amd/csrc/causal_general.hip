@@ -56,26 +56,32 @@ __device__ __forceinline__ Rows<T> rows_of(const AttnView& v, int head, int row0
 template <int DP> struct RowForm {
   f32x4 v[DP / 16];
 };
-template <int DP, class T>
+// (EXACT: d is DP.  All loads are made, of the row's own values where there is no column: a branch
+// around each took as long as the products.)
+template <int DP, bool EXACT, class T>
 __device__ __forceinline__ void load_rows(RowForm<DP>& R, const Rows<T>& X, int row, int g) {
   const T* p = X.p + (int64_t)min(row, X.last) * X.ld + 4 * g;
 #pragma unroll
-  for (int f = 0; f < DP / 16; ++f)
-    R.v[f] = 16 * f + 4 * g < X.d ? load4(p + 16 * f) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int f = 0; f < DP / 16; ++f) {
+    const bool in = EXACT || 16 * f + 4 * g < X.d;
+    const f32x4 x = load4(p + (in ? 16 * f : 0));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) R.v[f][e] = in ? x[e] : 0.f;
+  }
 }
-// Rows past the last are zero.
+// Rows past the last are the last's, and columns past d the row's first ones: no pair of the
+// former counts, and nobody stores the sums of the latter.
 template <int DP> struct ColForm {
   float v[4][DP / 16];
 };
-template <int DP, class T>
+template <int DP, bool EXACT, class T>
 __device__ __forceinline__ void load_cols(ColForm<DP>& C, const Rows<T>& X, int r0, int g, int r) {
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    const int row = r0 + 4 * g + s;
-    const T* p = X.p + (int64_t)min(row, X.last) * X.ld + r;
+    const T* p = X.p + (int64_t)min(r0 + 4 * g + s, X.last) * X.ld;
 #pragma unroll
     for (int dt = 0; dt < DP / 16; ++dt)
-      C.v[s][dt] = row <= X.last && 16 * dt + r < X.d ? (float)p[16 * dt] : 0.f;
+      C.v[s][dt] = (float)p[EXACT || 16 * dt + r < X.d ? 16 * dt + r : r & 7];
   }
 }
 // element s of lane (g, r): sum over d of A[row 4g + s][d] B[row r][d]
@@ -175,7 +181,7 @@ __device__ __forceinline__ Place place_of(const CausalArgs& p, int per_head) {
 }
 
 // ---- forward: S^T = K Q^T (a query per column), online softmax per wave, O^T += V^T P^T -----
-template <class T, int DP>
+template <class T, int DP, bool EXACT>
 __global__ __launch_bounds__(256) void fwd_kernel(CausalArgs p) {
   constexpr int ND = DP / 16;
   __shared__ f32x4 red[ND][64];
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(CausalArgs p) {
   const Rows<T> V = rows_of<T>(p.v, a.head_k, a.k_row, a.k_len, p.d);
   RowForm<DP> q, k;
   ColForm<DP> v;
-  load_rows<DP>(q, Q, a.r0 + r, g);
+  load_rows<DP, EXACT>(q, Q, a.r0 + r, g);
   float m, sum;
   f32x4 o[ND];
   auto walk = [&](bool by_pairs) {
@@ -202,8 +208,8 @@ __global__ __launch_bounds__(256) void fwd_kernel(CausalArgs p) {
     clear(o);
     for (int t = w; t < nt; t += 4) {
       const int k0 = 16 * t;
-      load_rows<DP>(k, K, k0 + r, g);
-      load_cols<DP>(v, V, k0, g, r);
+      load_rows<DP, EXACT>(k, K, k0 + r, g);
+      load_cols<DP, EXACT>(v, V, k0, g, r);
       f32x4 s = dot_rows<DP>(k, q);
       int seen = 0;
 #pragma unroll
@@ -257,8 +263,12 @@ __global__ __launch_bounds__(256) void fwd_kernel(CausalArgs p) {
   if (g == 0 && p.lse) p.lse[head * p.ld_lse + a.q_row + row] = M + logf(tot);
 }
 
+// Whether the backward's registers leave a SIMD one wave only, which then loads a tile while it works
+// on the one before.  (Wider heads spill as it is.)
+template <int DP> constexpr bool alone = DP == 128;
+
 // ---- backward: dQ^T += K^T dS^T over the keys; delta = dO . O of the block's queries ---------
-template <class T, int DP>
+template <class T, int DP, bool EXACT>
 __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
   constexpr int ND = DP / 16;
   __shared__ f32x4 red[ND][64];
@@ -274,9 +284,9 @@ __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
   const Rows<T> V = rows_of<T>(p.v, a.head_k, a.k_row, a.k_len, p.d);
   RowForm<DP> q, d_o, k, v;
   ColForm<DP> kt;
-  load_rows<DP>(q, rows_of<T>(p.q, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
-  load_rows<DP>(d_o, rows_of<T>(p.d_o, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
-  load_rows<DP>(k, rows_of<T>(p.o, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
+  load_rows<DP, EXACT>(q, rows_of<T>(p.q, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
+  load_rows<DP, EXACT>(d_o, rows_of<T>(p.d_o, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
+  load_rows<DP, EXACT>(k, rows_of<T>(p.o, head, a.q_row, a.q_len, p.d), a.r0 + r, g);
   float del = 0.f;
 #pragma unroll
   for (int f = 0; f < ND; ++f)
@@ -289,12 +299,23 @@ __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
   f32x4 dq[ND];
   auto walk = [&](bool by_pairs) {
     clear(dq);
+    auto rows = [&](int k0) {
+      load_rows<DP, EXACT>(k, K, k0 + r, g);
+      load_rows<DP, EXACT>(v, V, k0 + r, g);
+    };
+    auto cols = [&](int k0) { load_cols<DP, EXACT>(kt, K, k0, g, r); };
+    if (alone<DP> && w < nt) {
+      rows(16 * w);
+      cols(16 * w);
+    }
     for (int t = w; t < nt; t += 4) {
       const int k0 = 16 * t;
-      load_rows<DP>(k, K, k0 + r, g);
-      load_rows<DP>(v, V, k0 + r, g);
-      load_cols<DP>(kt, K, k0, g, r);
+      if constexpr (!alone<DP>) {
+        rows(k0);
+        cols(k0);
+      }
       const f32x4 s = dot_rows<DP>(k, q), dp = dot_rows<DP>(v, d_o);
+      if constexpr (alone<DP>) rows(k0 + 64);   // past the last row: that one
       f32x4 ds;
       int seen = 0;
 #pragma unroll
@@ -305,6 +326,7 @@ __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
       }
       if (by_pairs && __any(seen != 15)) accum_pairs<DP>(dq, K, k0, ds, seen, g, r);
       else accum_cols<DP>(dq, kt, ds);
+      if constexpr (alone<DP>) cols(k0 + 64);
     }
   };
   walk(false);
@@ -320,7 +342,7 @@ __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
 
 // ---- backward: per 16 keys, over the group's heads and the queries that see them -------------
 // S = Q K^T (a key per column), dV^T += dO^T P, dK^T += Q^T dS
-template <class T, int DP>
+template <class T, int DP, bool EXACT>
 __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
   constexpr int ND = DP / 16;
   __shared__ f32x4 red[ND][64];
@@ -333,41 +355,67 @@ __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
   const int nt = max((a.q_len + 15) / 16 - t0, 0);
   RowForm<DP> k, v, q, d_o;
   ColForm<DP> qt, dt_;
-  load_rows<DP>(k, rows_of<T>(p.k, a.head_k, a.k_row, a.k_len, p.d), a.r0 + r, g);
-  load_rows<DP>(v, rows_of<T>(p.v, a.head_k, a.k_row, a.k_len, p.d), a.r0 + r, g);
-  f32x4 dk[ND], dv[ND];
+  load_rows<DP, EXACT>(k, rows_of<T>(p.k, a.head_k, a.k_row, a.k_len, p.d), a.r0 + r, g);
+  load_rows<DP, EXACT>(v, rows_of<T>(p.v, a.head_k, a.k_row, a.k_len, p.d), a.r0 + r, g);
+  f32x4 dk[ND], dv[ND], lse, del;
   auto walk = [&](bool by_pairs) {
     clear(dk);
     clear(dv);
+    // tile c of the group's heads, one head behind the other; past the last, that one
+    struct At {
+      int head, r0;
+    };
+    auto at_tile = [&](int c) {
+      c = min(c, nt * p.group - 1);
+      return At{a.head_k * p.group + c / nt, 16 * (t0 + c % nt)};
+    };
+    auto q_of = [&](const At& x) { return rows_of<T>(p.q, x.head, a.q_row, a.q_len, p.d); };
+    auto do_of = [&](const At& x) { return rows_of<T>(p.d_o, x.head, a.q_row, a.q_len, p.d); };
+    auto rows = [&](const At& x) {
+      load_rows<DP, EXACT>(q, q_of(x), x.r0 + r, g);
+      load_rows<DP, EXACT>(d_o, do_of(x), x.r0 + r, g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t i = a.q_row + min(x.r0 + 4 * g + e, a.q_len - 1);
+        lse[e] = p.lse[x.head * p.ld_lse + i];
+        del[e] = p.delta[x.head * p.rows_q + i];
+      }
+    };
+    auto cols = [&](const At& x) {
+      load_cols<DP, EXACT>(qt, q_of(x), x.r0, g, r);
+      load_cols<DP, EXACT>(dt_, do_of(x), x.r0, g, r);
+    };
+    if (alone<DP> && w < nt * p.group) {
+      rows(at_tile(w));
+      cols(at_tile(w));
+    }
     for (int c = w; c < nt * p.group; c += 4) {
-      const int head = a.head_k * p.group + c / nt, r0 = 16 * (t0 + c % nt);
-      const Rows<T> Q = rows_of<T>(p.q, head, a.q_row, a.q_len, p.d);
-      const Rows<T> dO = rows_of<T>(p.d_o, head, a.q_row, a.q_len, p.d);
-      const float* LSE = p.lse + head * p.ld_lse + a.q_row;
-      const float* DEL = p.delta + head * p.rows_q + a.q_row;
-      load_rows<DP>(q, Q, r0 + r, g);
-      load_rows<DP>(d_o, dO, r0 + r, g);
-      load_cols<DP>(qt, Q, r0, g, r);
-      load_cols<DP>(dt_, dO, r0, g, r);
+      const At x = at_tile(c);
+      if constexpr (!alone<DP>) {
+        rows(x);
+        cols(x);
+      }
       const f32x4 s = dot_rows<DP>(q, k), dp = dot_rows<DP>(d_o, v);
       f32x4 pr, ds;
       int seen = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int qr = r0 + 4 * g + e, qc = min(qr, a.q_len - 1);
+        const int qr = x.r0 + 4 * g + e;
         const bool in = qr >= first_q && qr < a.q_len;
         seen |= in ? 1 << e : 0;
-        const float pe = expf(s[e] * p.scale - LSE[qc]);
+        const float pe = expf(s[e] * p.scale - lse[e]);
         pr[e] = in ? pe : 0.f;
-        ds[e] = in ? pe * (dp[e] - DEL[qc]) : 0.f;
+        ds[e] = in ? pe * (dp[e] - del[e]) : 0.f;
       }
+      if constexpr (alone<DP>) rows(at_tile(c + 4));
       if (by_pairs && __any(seen != 15)) {
-        accum_pairs<DP>(dv, dO, r0, pr, seen, g, r);
-        accum_pairs<DP>(dk, Q, r0, ds, seen, g, r);
+        accum_pairs<DP>(dv, do_of(x), x.r0, pr, seen, g, r);
+        accum_pairs<DP>(dk, q_of(x), x.r0, ds, seen, g, r);
       } else {
         accum_cols<DP>(dv, dt_, pr);
         accum_cols<DP>(dk, qt, ds);
       }
+      if constexpr (alone<DP>) cols(at_tile(c + 4));
     }
   };
   walk(false);
@@ -394,15 +442,17 @@ hipError_t launch(Kernel kernel, const CausalArgs& a, int64_t blocks, hipStream_
 
 }  // namespace
 
-#define MPIPE_GENERAL(KERNEL, BLOCKS)                                                     \
-  const int64_t blocks = (BLOCKS);                                                        \
-  if (dtype == DT_BF16)                                                                   \
-    return a.d <= 64    ? launch(KERNEL<bf16, 64>, a, blocks, s)                          \
-           : a.d <= 128 ? launch(KERNEL<bf16, 128>, a, blocks, s)                         \
-                        : launch(KERNEL<bf16, 256>, a, blocks, s);                        \
-  return a.d <= 64    ? launch(KERNEL<float, 64>, a, blocks, s)                           \
-         : a.d <= 128 ? launch(KERNEL<float, 128>, a, blocks, s)                          \
-                      : launch(KERNEL<float, 256>, a, blocks, s);
+#define MPIPE_GENERAL_WIDTH(KERNEL, T, DP) \
+  (a.d == DP ? launch(KERNEL<T, DP, true>, a, blocks, s) : launch(KERNEL<T, DP, false>, a, blocks, s))
+#define MPIPE_GENERAL_TYPE(KERNEL, T)                       \
+  (a.d <= 32    ? MPIPE_GENERAL_WIDTH(KERNEL, T, 32)        \
+   : a.d <= 64  ? MPIPE_GENERAL_WIDTH(KERNEL, T, 64)        \
+   : a.d <= 96  ? MPIPE_GENERAL_WIDTH(KERNEL, T, 96)        \
+   : a.d <= 128 ? MPIPE_GENERAL_WIDTH(KERNEL, T, 128)       \
+                : MPIPE_GENERAL_WIDTH(KERNEL, T, 256))
+#define MPIPE_GENERAL(KERNEL, BLOCKS)                       \
+  const int64_t blocks = (BLOCKS);                          \
+  return dtype == DT_BF16 ? MPIPE_GENERAL_TYPE(KERNEL, bf16) : MPIPE_GENERAL_TYPE(KERNEL, float);
 
 hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStream_t s) {
   MPIPE_GENERAL(fwd_kernel, (int64_t)items * SUB * a.heads_k * a.group)
@@ -414,5 +464,7 @@ hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStr
   MPIPE_GENERAL(dkdv_kernel, (int64_t)items * SUB * a.heads_k)
 }
 #undef MPIPE_GENERAL
+#undef MPIPE_GENERAL_TYPE
+#undef MPIPE_GENERAL_WIDTH
 
 }  // namespace mpipe
