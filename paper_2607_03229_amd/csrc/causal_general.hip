@@ -60,11 +60,11 @@ template <int DP> struct RowForm {
 // around each took as long as the products.)
 template <int DP, bool EXACT, class T>
 __device__ __forceinline__ void load_rows(RowForm<DP>& R, const Rows<T>& X, int row, int g) {
-  const T* p = X.p + (int64_t)min(row, X.last) * X.ld + 4 * g;
+  const T* p = X.p + (int64_t)min(row, X.last) * X.ld;
 #pragma unroll
   for (int f = 0; f < DP / 16; ++f) {
     const bool in = EXACT || 16 * f + 4 * g < X.d;
-    const f32x4 x = load4(p + (in ? 16 * f : 0));
+    const f32x4 x = load4(p + (in ? 16 * f + 4 * g : 4 * (g & 1)));   // (d is at least 8)
 #pragma unroll
     for (int e = 0; e < 4; ++e) R.v[f][e] = in ? x[e] : 0.f;
   }

@@ -151,6 +151,21 @@ def test_many_sequences():
     run(BF, 2, 1, 64, [1 + i % 9 for i in range(500)], bwd=True)
 
 
+@pytest.mark.parametrize("d", [32, 64, 80, 128])
+def test_few_key_heads(d):
+    """Key tiles whose queries, of all heads of a group, go to several blocks: parts that begin and
+    end inside a head, and keys that only a few of the last queries see."""
+    run(BF, 14, 2, d, [300, 5, 700])
+    run(BF, 16, 1, d, [129], prefix=[500])
+
+
+@pytest.mark.parametrize("d", [48, 80, 104, 128])
+def test_many_heads(d):
+    """As many query tiles and key tiles as fill the chip by themselves."""
+    run(BF, 28, 4, d, [700, 257, 300, 33], gap=2)
+    run(BF, 16, 16, d, [100 + 11 * i for i in range(20)])
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 def test_sharp_scores(dtype):
     """Weights near one hot, scores of thousands: maxima move by a lot from tile to tile."""
