@@ -509,6 +509,12 @@ def test_decode_many_sequences():
     decode(BF, BF, 2, 1, 64, 16, [(i * 37) % 90 for i in range(700)])
 
 
+@pytest.mark.parametrize("dtype,cache_dtype,hq,hk", [(BF, BF, 6, 3), (FP, "e4m3", 34, 2)])
+def test_decode_more_heads_than_blocks(dtype, cache_dtype, hq, hk):
+    """Most key heads lie in one block, some in two."""
+    decode(dtype, cache_dtype, hq, hk, 64, 16, [(i * 61) % 400 for i in range(360)])
+
+
 @pytest.mark.parametrize("layout", ["wide", "heads_first", "odd"])
 def test_decode_layouts(layout):
     for dtype in (BF, FP):
