@@ -37,12 +37,12 @@ struct CausalArgs {
   int64_t ld_lse, rows_q;
   float scale;
   int d, heads_k, group;
+  int sub;       // 16-row blocks of an item, causal_general.hip
   int q_waves;   // of a block of 32 queries each, fwd and dq
   int parts;     // parts: blocks that share a key tile's queries, of dkdv
 };
 static_assert(sizeof(CausalArgs) <= 4000, "a launch's arguments");
-// Any dtype, alignment and head_dim of at most 256 (causal_general.hip): items of kGeneralRows.
-constexpr int kGeneralRows = 128;
+// Any dtype, alignment and head_dim of at most 256 (causal_general.hip): items of 16 * sub rows.
 hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s);

@@ -23,8 +23,6 @@
 namespace mpipe {
 namespace {
 
-constexpr int SUB = kGeneralRows / 16;   // 16-row blocks of a work item
-
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 typedef __attribute__((ext_vector_type(4), aligned(2))) bf16 bf16x4_any;
 
@@ -170,13 +168,13 @@ __device__ __forceinline__ Place place_of(const CausalArgs& p, int per_head) {
   b /= p.heads_k;
   a.gq = b % per_head;
   b /= per_head;
-  const uint32_t it = (uint32_t)p.pool.word[kAttnWords - 1 - b / SUB];
+  const uint32_t it = (uint32_t)p.pool.word[kAttnWords - 1 - b / p.sub];
   const int32_t* s = p.pool.word + 4 * (it & 255);
   a.q_row = s[0];
   a.q_len = s[1];
   a.k_row = s[2];
   a.k_len = s[3];
-  a.r0 = (int)(it >> 8) * kGeneralRows + 16 * (b % SUB);
+  a.r0 = 16 * ((int)(it >> 8) * p.sub + b % p.sub);
   return a;
 }
 
@@ -455,13 +453,13 @@ hipError_t launch(Kernel kernel, const CausalArgs& a, int64_t blocks, hipStream_
   return dtype == DT_BF16 ? MPIPE_GENERAL_TYPE(KERNEL, bf16) : MPIPE_GENERAL_TYPE(KERNEL, float);
 
 hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStream_t s) {
-  MPIPE_GENERAL(fwd_kernel, (int64_t)items * SUB * a.heads_k * a.group)
+  MPIPE_GENERAL(fwd_kernel, (int64_t)items * a.sub * a.heads_k * a.group)
 }
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s) {
-  MPIPE_GENERAL(dq_kernel, (int64_t)items * SUB * a.heads_k * a.group)
+  MPIPE_GENERAL(dq_kernel, (int64_t)items * a.sub * a.heads_k * a.group)
 }
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s) {
-  MPIPE_GENERAL(dkdv_kernel, (int64_t)items * SUB * a.heads_k)
+  MPIPE_GENERAL(dkdv_kernel, (int64_t)items * a.sub * a.heads_k)
 }
 #undef MPIPE_GENERAL
 #undef MPIPE_GENERAL_TYPE
