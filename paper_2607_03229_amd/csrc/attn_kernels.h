@@ -33,7 +33,7 @@ struct CausalArgs {
   AttnView q, k, v, o, d_o, dq, dk, dv;
   float* lse;
   float* delta;   // backward: [2][heads][rows_q] of what one kernel leaves to the next
-  float* partial;   // dkdv in parts: [blocks][keys of a block][2][width] as the lanes hold them
+  float* partial;   // dkdv in parts: [blocks][2][width][keys of a block] as the lanes hold them
   int64_t ld_lse, rows_q;
   float scale;
   int d, heads_k, group;
@@ -54,7 +54,7 @@ hipError_t causal_bf16_fwd(const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_bf16_dq(const CausalArgs& a, int items, hipStream_t s);
 hipError_t causal_bf16_dkdv(const CausalArgs& a, int items, hipStream_t s);
 // The width a head is padded to in the tiles.
-constexpr int causal_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
+constexpr int causal_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
 // Waves of a block: four where the tiles' LDS lets two blocks share a CU (one's start and end then
 // meet the other's work, and half as many rows pad a sequence's last block), else eight, whose
 // two halves share the SIMDs.  Measured on MI355X, us with 8 -> 4 waves: forward, four sequences

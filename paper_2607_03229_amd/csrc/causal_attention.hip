@@ -58,11 +58,30 @@ CausalArgs args_of(const CausalProblem& p) {
 // twelve tiles: within 10 %.
 constexpr int64_t kSplitBlocks = 512, kPartTiles = 4;
 int64_t split_blocks(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k, int d) {
-  if (heads_k == 0) return 0;
+  if (heads_k == 0 || d > 128) return 0;
   const int rows = 16 * causal_k_waves(causal_width(d));
   const int64_t parts = (rows_q + 63) / 64 * (heads_q / heads_k) / kPartTiles;
   const int64_t tiles = (rows_k + rows - 1) / rows * heads_k;
   return parts < 2 || tiles > kSplitBlocks / 2 ? 0 : std::min(kSplitBlocks, parts * tiles);
+}
+// The same for the general kernels, whose tiles have 16 rows and whose four waves cut a part again.
+// Without parts, with 1024, 2048 and 4096 blocks, fp32, one sequence of 2048: 8/1 heads of 64 686,
+// 255, 248, 275; 16/1 of 128 2626, 1032, 1066, 1153; four of 500, 28/4 of 128 586, 599, 615, 681.
+constexpr int64_t kGeneralSplit = 1024, kGeneralPartTiles = 16;
+int64_t general_split_blocks(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k) {
+  if (heads_k == 0) return 0;
+  const int64_t parts = (rows_q + 15) / 16 * (heads_q / heads_k) / kGeneralPartTiles;
+  const int64_t tiles = (rows_k + 15) / 16 * heads_k;
+  return parts < 2 || tiles > kGeneralSplit / 2 ? 0 : std::min(kGeneralSplit, parts * tiles);
+}
+// Parts of every key tile, so that they are `blocks` in all, of `least` query tiles at least.
+int parts_of(const CausalProblem& p, int key_rows, int query_rows, int64_t blocks, int64_t least) {
+  int64_t tiles = 0, longest = 0;
+  for (const AttnSeq& q : p.seqs) {
+    tiles += (q.k_len + key_rows - 1) / key_rows * (int64_t)p.k.heads;
+    longest = std::max<int64_t>(longest, (q.q_len + query_rows - 1) / query_rows * (int64_t)(p.q.heads / p.k.heads));
+  }
+  return tiles == 0 ? 1 : (int)std::max<int64_t>(1, std::min(blocks / tiles, longest / least));
 }
 int64_t delta_bytes(int64_t rows_q, int heads_q) { return (rows_q * heads_q * 8 + 31) / 16 * 16; }
 
@@ -117,27 +136,21 @@ hipError_t causal_attention_fwd(const CausalProblem& p, hipStream_t s) {
 size_t causal_attention_scratch(int64_t rows_q, int heads_q, int64_t rows_k, int heads_k,
                                 int head_dim) {
   const int width = causal_width(head_dim);
-  return (size_t)(delta_bytes(rows_q, heads_q) +
-                  (head_dim > 128 ? 0 : split_blocks(rows_q, heads_q, rows_k, heads_k, head_dim) *
-                                            16 * causal_k_waves(width) * 2 * width * 4));
+  const int64_t tiled = split_blocks(rows_q, heads_q, rows_k, heads_k, head_dim) * 16 * causal_k_waves(width);
+  const int64_t general = general_split_blocks(rows_q, heads_q, rows_k, heads_k) * 16;
+  return (size_t)(delta_bytes(rows_q, heads_q) + std::max(tiled, general) * 2 * width * 4);
 }
 
 hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
   CausalArgs a = args_of(p);
+  a.partial = p.scratch + delta_bytes(p.rows_q, p.q.heads) / 4;
   if (tiled(p, {&p.q, &p.k, &p.v, &p.o, &p.d_o, &p.dq, &p.dk, &p.dv})) {
     const int width = causal_width(p.head_dim);
     if (hipError_t e = in_pieces(p, a, false, 32 * a.q_waves, p.q.heads,
                                  [&](const CausalArgs& b, int n) { return causal_bf16_dq(b, n, s); }))
       return e;
     const int rows = 16 * causal_k_waves(width);
-    int64_t tiles = 0, longest = 0;
-    for (const AttnSeq& q : p.seqs) {
-      tiles += (q.k_len + rows - 1) / rows * p.k.heads;
-      longest = std::max<int64_t>(longest, (q.q_len + 63) / 64 * a.group);
-    }
-    const int64_t blocks = split_blocks(p.rows_q, p.q.heads, p.rows_k, p.k.heads, p.head_dim);
-    if (tiles > 0) a.parts = (int)std::max<int64_t>(1, std::min(blocks / tiles, longest / kPartTiles));
-    a.partial = p.scratch + delta_bytes(p.rows_q, p.q.heads) / 4;
+    a.parts = parts_of(p, rows, 64, split_blocks(p.rows_q, p.q.heads, p.rows_k, p.k.heads, p.head_dim), kPartTiles);
     return in_pieces(p, a, true, rows, p.k.heads * a.parts,
                      [&](const CausalArgs& b, int n) { return causal_bf16_dkdv(b, n, s); });
   }
@@ -147,7 +160,9 @@ hipError_t causal_attention_bwd(const CausalProblem& p, hipStream_t s) {
       }))
     return e;
   a.sub = general_sub(p, true);
-  return in_pieces(p, a, true, 16 * a.sub, a.sub * p.k.heads, [&](const CausalArgs& b, int n) {
+  a.parts = parts_of(p, 16 * a.sub, 16, general_split_blocks(p.rows_q, p.q.heads, p.rows_k, p.k.heads) / a.sub,
+                     kGeneralPartTiles);
+  return in_pieces(p, a, true, 16 * a.sub, a.sub * p.k.heads * a.parts, [&](const CausalArgs& b, int n) {
     return causal_general_dkdv(p.dtype, b, n, s);
   });
 }

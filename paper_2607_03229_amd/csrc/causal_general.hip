@@ -339,18 +339,21 @@ __global__ __launch_bounds__(256) void dq_kernel(CausalArgs p) {
 }
 
 // ---- backward: per 16 keys, over the group's heads and the queries that see them -------------
-// S = Q K^T (a key per column), dV^T += dO^T P, dK^T += Q^T dS
+// S = Q K^T (a key per column), dV^T += dO^T P, dK^T += Q^T dS.  Where there are few keys, p.parts
+// blocks share 16 of them.
 template <class T, int DP, bool EXACT>
 __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
   constexpr int ND = DP / 16;
   __shared__ f32x4 red[ND][64];
-  const Place a = place_of(p, 1);
+  const Place a = place_of(p, p.parts);
   if (a.r0 >= a.k_len) return;
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63, g = l >> 4, r = l & 15;
   const int row = min(a.r0 + r, a.k_len - 1), shift = a.k_len - a.q_len;
   const int first_q = row - shift;                // first query that sees the lane's key
   const int t0 = max(a.r0 - shift, 0) / 16;       // first tile with one that sees any of them
   const int nt = max((a.q_len + 15) / 16 - t0, 0);
+  const int c0 = (int)((int64_t)nt * p.group * a.gq / p.parts);         // the block's part of the
+  const int c1 = (int)((int64_t)nt * p.group * (a.gq + 1) / p.parts);   // group's tiles
   RowForm<DP> k, v, q, d_o;
   ColForm<DP> qt, dt_;
   load_rows<DP, EXACT>(k, rows_of<T>(p.k, a.head_k, a.k_row, a.k_len, p.d), a.r0 + r, g);
@@ -383,11 +386,11 @@ __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
       load_cols<DP, EXACT>(qt, q_of(x), x.r0, g, r);
       load_cols<DP, EXACT>(dt_, do_of(x), x.r0, g, r);
     };
-    if (alone<DP> && w < nt * p.group) {
-      rows(at_tile(w));
-      cols(at_tile(w));
+    if (alone<DP> && c0 + w < c1) {
+      rows(at_tile(c0 + w));
+      cols(at_tile(c0 + w));
     }
-    for (int c = w; c < nt * p.group; c += 4) {
+    for (int c = c0 + w; c < c1; c += 4) {
       const At x = at_tile(c);
       if constexpr (!alone<DP>) {
         rows(x);
@@ -420,6 +423,16 @@ __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
   if (!(all_finite(dk) && all_finite(dv))) walk(true);
   add_waves<ND>(dk, red, w, l);
   add_waves<ND>(dv, red, w, l);
+  if (p.parts > 1) {
+    f32x4* out = reinterpret_cast<f32x4*>(p.partial) + (int64_t)blockIdx.x * (2 * ND * 64) + l;
+    if (w > 0) return;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) {
+      out[64 * i] = dk[i];
+      out[64 * (ND + i)] = dv[i];
+    }
+    return;
+  }
   if (w > 0 || a.r0 + r >= a.k_len) return;
   const int64_t at = a.k_row + row;
   T* dK = reinterpret_cast<T*>(const_cast<void*>(p.dk.p)) + p.dk.head * a.head_k + p.dk.row * at + 4 * g;
@@ -430,6 +443,27 @@ __global__ __launch_bounds__(256) void dkdv_kernel(CausalArgs p) {
       store4(dK + 16 * dt, dk[dt] * p.scale);
       store4(dV + 16 * dt, dv[dt]);
     }
+}
+
+// The sums of 16 keys' parts, in their order.
+template <class T, int DP, bool EXACT>
+__global__ __launch_bounds__(256) void parts_kernel(CausalArgs p) {
+  constexpr int ND = DP / 16;
+  const Place a = place_of(p, 1);
+  const int64_t tile = blockIdx.x / p.heads_k;
+  for (int i = threadIdx.x; i < 2 * ND * 64; i += 256) {
+    const int l = i & 63, g = l >> 4, r = l & 15, dt = i / 64 % ND;
+    if (a.r0 + r >= a.k_len || 16 * dt + 4 * g >= p.d) continue;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int j = 0; j < p.parts; ++j)
+      x += reinterpret_cast<const f32x4*>(p.partial)[((tile * p.parts + j) * p.heads_k + a.head_k) * (2 * ND * 64) + i];
+    const bool of_k = i < ND * 64;
+    const AttnView& out = of_k ? p.dk : p.dv;
+    store4(reinterpret_cast<T*>(const_cast<void*>(out.p)) + out.head * a.head_k +
+               out.row * (int64_t)(a.k_row + a.r0 + r) + 16 * dt + 4 * g,
+           of_k ? x * p.scale : x);
+  }
 }
 
 template <class Kernel>
@@ -458,8 +492,15 @@ hipError_t causal_general_fwd(int dtype, const CausalArgs& a, int items, hipStre
 hipError_t causal_general_dq(int dtype, const CausalArgs& a, int items, hipStream_t s) {
   MPIPE_GENERAL(dq_kernel, (int64_t)items * a.sub * a.heads_k * a.group)
 }
+static hipError_t general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s) {
+  MPIPE_GENERAL(dkdv_kernel, (int64_t)items * a.sub * a.heads_k * a.parts)
+}
+static hipError_t general_parts(int dtype, const CausalArgs& a, int items, hipStream_t s) {
+  MPIPE_GENERAL(parts_kernel, (int64_t)items * a.sub * a.heads_k)
+}
 hipError_t causal_general_dkdv(int dtype, const CausalArgs& a, int items, hipStream_t s) {
-  MPIPE_GENERAL(dkdv_kernel, (int64_t)items * a.sub * a.heads_k)
+  const hipError_t e = general_dkdv(dtype, a, items, s);
+  return e || a.parts == 1 ? e : general_parts(dtype, a, items, s);
 }
 #undef MPIPE_GENERAL
 #undef MPIPE_GENERAL_TYPE

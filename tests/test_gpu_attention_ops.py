@@ -151,12 +151,12 @@ def test_many_sequences():
     run(BF, 2, 1, 64, [1 + i % 9 for i in range(500)], bwd=True)
 
 
-@pytest.mark.parametrize("d", [32, 64, 80, 128])
-def test_few_key_heads(d):
+@pytest.mark.parametrize("dtype,d", [(BF, 32), (BF, 64), (BF, 80), (BF, 128), (BF, 136), (FP, 64), (FP, 128)])
+def test_few_key_heads(dtype, d):
     """Key tiles whose queries, of all heads of a group, go to several blocks: parts that begin and
     end inside a head, and keys that only a few of the last queries see."""
-    run(BF, 14, 2, d, [300, 5, 700])
-    run(BF, 16, 1, d, [129], prefix=[500])
+    run(dtype, 14, 2, d, [300, 5, 700])
+    run(dtype, 16, 1, d, [129], prefix=[500])
 
 
 @pytest.mark.parametrize("d", [48, 80, 104, 128])
