@@ -265,8 +265,8 @@ mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad
  * A query that sees no key gets o = 0 and lse = -infinity, and gradients of 0.  A key that a
  * query does not see does not count for it, whatever its values.  Rows of no sequence keep what
  * they held in every output.  Scores, statistics and sums are fp32; in bf16 the weights and the
- * score gradients are rounded to bf16 (half a step of 2^-8 each) before their products.  The
- * same call gives the same bits.  Outputs are apart from every other buffer but each other's
+ * score gradients are rounded to bf16 (half a step, 2^-8 of the value at most) before their products.
+ * The same call gives the same bits.  Outputs are apart from every other buffer but each other's
  * columns of one product, side by side. */
 mpipe_status mpipe_op_causal_attention_fwd(int32_t dtype, int32_t head_dim, int64_t rows_q,
                                            int64_t rows_k, const mpipe_heads* q,
@@ -315,7 +315,8 @@ typedef struct {
  * sequence seq[i] (device int32; seq null: sequence i).  Rounded to nearest even where the cache
  * is narrower.  In e4m3 the power of two is the least that brings the largest finite magnitude
  * of the head to 448 or less, its exponent between -120 and 120; values that are infinite or not
- * a number are kept as not a number.  A row with pos[i] < 0 or seq[i] < 0 is left out (padding).
+ * a number are kept as not a number, and magnitudes from 3.3e38 on round to 2^128, which reads as
+ * infinite.  A row with pos[i] < 0 or seq[i] < 0 is left out (padding).
  * A row whose sequence is not below n_seq, whose page is not in the table's width or whose page
  * number is not in the pool is left out too, and *status (device int32, nullable, not cleared by the
  * call) becomes 1.  Rows of one call are of different places (or what such a place holds is

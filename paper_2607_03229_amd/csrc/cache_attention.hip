@@ -13,6 +13,12 @@
 // maxima and sums are lane exchanges within a column, and P^T is already the operand of
 // O^T += V^T P^T.  K comes from memory in operand order; V goes through LDS, from which the
 // transposing reads take it.  The next tokens' loads are in flight meanwhile.
+//
+// Scores, maxima, sums and outputs are fp32; the weights of a bf16 query are rounded to bf16 (half a
+// step of 2^-8) for the matrix unit.  Measured on MI355X: 64 sequences of up to 16384, 32/8 heads of
+// 128, bf16, pages of 32: 410 us, 5.8 TB/s, and 9 us to join (first kernel 730); four of up to
+// 131072, 28/4 heads, e4m3: 98 us, 4.8 TB/s, and 8 (first 320); eight of up to 1000: 11 us, a chain
+// of loads (length, page, keys), and 5 (first 27).
 #include <type_traits>
 
 #include "cache_places.h"

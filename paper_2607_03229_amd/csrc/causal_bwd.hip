@@ -1,5 +1,14 @@
 // Causal attention backward, bf16: dQ over query tiles, then dK and dV over key tiles.  Both
 // recompute the weights from q, k and lse; no atomics, every sum in a fixed order.
+//   P = exp(scale q k - lse), D = dO . O, dS = P (dO v - D)
+//   dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO, the last two over the heads of a group
+// Scores, D and all sums are fp32; P and dS are rounded to bf16 (half a step of 2^-8) as operands of
+// their products, and P enters dS with 24 bits.
+//
+// Bound by the matrix unit: 6 d operations a pair in dQ and 8 d in dK and dV (a kernel of its own
+// for dQ: added to by many key tiles at once it would need atomics, or ordered turns).  Measured on
+// MI355X, eight sequences of up to 8192, 28/4 heads of 128: dQ 3.43 ms, 1.19 PFLOP/s of the pairs
+// that count; dK and dV 5.07 ms, 1.07 PFLOP/s (first kernels: 336 ms for both).
 #include <type_traits>
 
 #include "causal_bf16.h"

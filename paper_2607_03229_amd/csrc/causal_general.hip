@@ -13,6 +13,11 @@
 // so scores never leave their registers.  Values are widened to fp32 as they are read: bf16
 // products are then exact and weights are not rounded.
 //
+// Bound by the fp32 MFMA rate (157 TFLOP/s) and, below some 1000 rows, by one tile's chain of loads
+// and products.  Measured on MI355X, eight fp32 sequences of 2048, 8 heads of 64: forward 0.43 ms,
+// 81 TFLOP/s; backward 1.62 ms, 53 TFLOP/s of five products (seven are made); five of up to 333, 6
+// heads of 64: 12.7, 17.0 and 20.8 us.
+//
 // A key that a query does not see has weight 0, but 0 times an infinity or a NaN of its value
 // would still reach the sum.  Only tiles that the diagonal cuts hold such pairs, and only an
 // output that is not finite can be touched: a wave that finds one goes over its tiles again and
