@@ -15,6 +15,15 @@ BF, FP = torch.bfloat16, torch.float32
 GUARD = 7.0     # what rows of no sequence hold, before and after
 
 
+@pytest.fixture(autouse=True)
+def float32_default():
+    """Other test modules change torch's default type as they are imported."""
+    old = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(old)
+
+
 def normal(gen, *shape, dtype=BF):
     return torch.randn(shape, generator=gen).to(dtype)
 
@@ -275,11 +284,34 @@ def test_shared_keys_in_the_forward(dtype):
 
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
 def test_the_same_bits(dtype, d):
-    """A call again, and a sequence of it alone, forward and backward."""
+    """A call again, forward and backward."""
     first = run(dtype, 6, 2, d, [130, 300, 65])
     again = run(dtype, 6, 2, d, [130, 300, 65])
     for name in first:
         assert torch.equal(first[name], again[name]), name
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_broadcast_inputs(dtype):
+    """One row as every row's gradient, one head as every key head: as if they were written out."""
+    rows, hq, hk, d = 333, 6, 3, 64
+    gen = torch.Generator().manual_seed(3)
+    q = normal(gen, rows, hq, d, dtype=dtype).cuda()
+    k, v = (normal(gen, rows, 1, d, dtype=dtype).cuda().expand(rows, hk, d) for _ in range(2))
+    d_o = normal(gen, 1, 1, d, dtype=dtype).cuda().expand(rows, hq, d)
+    announce(f"broadcast {dtype}")
+
+    def both(k, v, d_o):
+        o, dq = torch.empty_like(q), torch.empty_like(q)
+        dk, dv = (torch.empty(rows, hk, d, dtype=dtype, device="cuda") for _ in range(2))
+        lse = torch.empty(hq, rows, device="cuda")
+        scratch = torch.empty(mp.op_causal_attention_scratch_bytes(rows, hq, rows, hk, d),
+                              dtype=torch.uint8, device="cuda")
+        mp.op_causal_attention_fwd(q, k, v, o, lse, [0, 200], [190, 133])
+        mp.op_causal_attention_bwd(d_o, q, k, v, o, lse, [0, 200], [190, 133], dq, dk, dv, scratch)
+        return [t[r] for t in (o, dq, dk, dv) for r in (slice(0, 190), slice(200, 333))]
+    for a, b in zip(both(k, v, d_o), both(k.contiguous(), v.contiguous(), d_o.contiguous())):
+        assert torch.equal(a, b)
 
 
 def test_offsets_past_32_bits():
