@@ -877,12 +877,13 @@ def _lse(t, heads: int, rows: int, dev: int) -> Tuple[Optional[int], int]:
     import torch
     if t is None:
         return None, 0
-    if (t.dtype is not torch.float32 or t.dim() != 2 or t.shape[0] != heads or
-            t.shape[1] != rows or (rows > 1 and t.stride(1) != 1)):
+    stride = t.stride()
+    if (t.dtype is not torch.float32 or t.shape != (heads, rows) or
+            (rows > 1 and stride[1] != 1)):
         _bad("lse: fp32 [heads of q][rows], rows adjacent")
     if t.get_device() != dev:
         _bad("tensors on different devices")
-    return t.data_ptr(), t.stride(0) if heads > 1 else rows
+    return t.data_ptr(), stride[0] if heads > 1 else rows
 
 
 def _sequence_lists(seq_row, seq_len, key_row, key_len):
@@ -903,9 +904,10 @@ _ATTN_K = "k, v and their gradients: [key rows][key heads][head_dim] in the dtyp
 
 
 def _attn_shapes(q, k):
-    if len(q.shape) != 3 or len(k.shape) != 3:
+    of_q, of_k = q.shape, k.shape
+    if len(of_q) != 3 or len(of_k) != 3:
         _bad(_ATTN_Q)
-    return q.shape[0], k.shape[0], q.shape[2], q.dtype, q.get_device()
+    return of_q[0], of_q[1], of_k[0], of_q[2], q.dtype, q.get_device()
 
 
 def op_causal_attention_fwd(q, k, v, o, lse, seq_row, seq_len, key_row=None, key_len=None,
@@ -916,8 +918,8 @@ def op_causal_attention_fwd(q, k, v, o, lse, seq_row, seq_len, key_row=None, key
     together, so more keys are a prefix.  lse (fp32 [heads][rows], may be None) for the
     backward.  scale: head_dim ** -0.5 unless given.  Rows of no sequence are left as they
     were."""
-    rq, rk, d, dtype, dev = _attn_shapes(q, k)
-    p, ld = _lse(lse, q.shape[1], rq, dev)
+    rq, hq, rk, d, dtype, dev = _attn_shapes(q, k)
+    p, ld = _lse(lse, hq, rq, dev)
     _launch(load().mpipe_op_causal_attention_fwd, dev, stream, _code(dtype), d, rq, rk,
             _view(q, rq, d, dtype, dev, _ATTN_Q), _view(k, rk, d, dtype, dev, _ATTN_K),
             _view(v, rk, d, dtype, dev, _ATTN_K),
@@ -940,10 +942,10 @@ def op_causal_attention_bwd(d_o, q, k, v, o, lse, seq_row, seq_len, dq, dk, dv, 
     """Gradients of op_causal_attention_fwd from d_o, the gradient of o, and what the forward took
     and gave: dq, dk, dv overwritten in the sequences' rows (they may be columns of one product).
     scratch: op_causal_attention_scratch_bytes."""
-    rq, rk, d, dtype, dev = _attn_shapes(q, k)
+    rq, hq, rk, d, dtype, dev = _attn_shapes(q, k)
     if lse is None:
         _bad("the backward needs lse")
-    p, ld = _lse(lse, q.shape[1], rq, dev)
+    p, ld = _lse(lse, hq, rq, dev)
     _launch(load().mpipe_op_causal_attention_bwd, dev, stream, _code(dtype), d, rq, rk,
             _view(d_o, rq, d, dtype, dev, _ATTN_Q), _view(q, rq, d, dtype, dev, _ATTN_Q),
             _view(k, rk, d, dtype, dev, _ATTN_K), _view(v, rk, d, dtype, dev, _ATTN_K),
