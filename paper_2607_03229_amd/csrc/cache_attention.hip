@@ -470,14 +470,13 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
   }
 }
 
-// Joins the parts of one (sequence, query head), or of all query heads of a column block;
-// sequences without tokens get their outputs here.
+// Joins the parts of one (sequence, query head) with a block, or (ALL) of the query heads of a column
+// block with a wave each; sequences without tokens get their outputs here.
 template <class T, int DP, bool ALL>
 __global__ __launch_bounds__(256) void join_kernel(Args p) {
   constexpr int LANES = 256 / DP;   // threads to a column
   __shared__ int64_t sums[4];
   __shared__ int64_t before_s;
-  __shared__ float weight[MAX_BLOCKS], top[4], total[4], cols[256];
   const int tid = threadIdx.x, heads_v = p.at.heads * p.col_blocks, d = p.at.d;
   const int items = ALL ? heads_v : p.at.heads * p.group;   // of a sequence
   const int seq = blockIdx.x / items, item = blockIdx.x % items;
@@ -494,22 +493,49 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt;
   const int b0 = nt == 0 ? 0 : (int)quotient(u0, each), n = nt == 0 ? 0 : (int)quotient(u0 + nt - 1, each) - b0 + 1;
   if (n == 1) return;   // written by its block
-  for (int i0 = 0; i0 < count; ++i0) {
-    const int head = head_k * p.group + first + i0, h = first % QG + i0;
-    T* O = reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * head;
-    if (nt == 0) {
-      const float x = all_there ? 0.f : NAN;
-      for (int c = tid; c < d; c += 256) O[c] = (T)x;
-      if (p.lse && tid == 0) p.lse[head * p.ld_lse + seq] = all_there ? -INFINITY : NAN;
-      continue;
+  auto out_of = [&](int head) {
+    return reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * head;
+  };
+  // part i of head h of the column block: of block b0 + i; the first block's begins the head, the
+  // others' begin the block
+  auto part_of = [&](int i, int h) {
+    return p.part + ((int64_t)(2 * (b0 + i) + (i == 0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
+  };
+  const int head0 = head_k * p.group + first;
+  if (nt == 0) {
+    const float x = all_there ? 0.f : NAN;
+    for (int i = tid; i < count * d; i += 256) out_of(head0 + i / d)[i % d] = (T)x;
+    if (p.lse && tid < count) p.lse[(head0 + tid) * p.ld_lse + seq] = all_there ? -INFINITY : NAN;
+    return;
+  }
+  if constexpr (ALL) {
+    const int l = tid & 63;
+    for (int h = tid >> 6; h < count; h += 4) {
+      float m = -INFINITY, tot = 0.f, x[DP / 64];
+      for (int i = l; i < n; i += 64) m = fmaxf(m, part_of(i, h)[DP]);
+      const float M = warp_max(m), ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int j = 0; j < DP / 64; ++j) x[j] = 0.f;
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const float* part = part_of(i, h);
+        const float weight = exp2_any(part[DP] - ref);
+        tot += part[DP + 1] * weight;
+#pragma unroll
+        for (int j = 0; j < DP / 64; ++j) x[j] = fmaf(part[64 * j + l], weight, x[j]);
+      }
+      T* O = out_of(head0 + h);
+#pragma unroll
+      for (int j = 0; j < DP / 64; ++j)
+        if (64 * j + l < d) O[64 * j + l] = (T)(x[j] / tot);
+      if (p.lse && l == 0) p.lse[(head0 + h) * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
     }
-    // part i: of block b0 + i; the first block's begins the head, the others' begin the block
-    auto part_of = [&](int i) {
-      return p.part + ((int64_t)(2 * (b0 + i) + (i == 0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
-    };
+  } else {
+    __shared__ float weight[MAX_BLOCKS], top[4], total[4], cols[256];
+    const int h = first % QG;
     float m = -INFINITY;
     for (int i = tid; i < n; i += 256) {
-      weight[i] = part_of(i)[DP];
+      weight[i] = part_of(i, h)[DP];
       m = fmaxf(m, weight[i]);
     }
     m = warp_max(m);
@@ -519,7 +545,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
     float tot = 0.f;
     for (int i = tid; i < n; i += 256) {
       weight[i] = exp2_any(weight[i] - ref);
-      tot += part_of(i)[DP + 1] * weight[i];
+      tot += part_of(i, h)[DP + 1] * weight[i];
     }
     tot = warp_sum(tot);
     if (tid % 64 == 0) total[tid / 64] = tot;
@@ -528,18 +554,16 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
     const int c = tid % DP;
     float x = 0.f;
 #pragma unroll 8
-    for (int i = tid / DP; i < n; i += LANES) x = fmaf(part_of(i)[c], weight[i], x);
+    for (int i = tid / DP; i < n; i += LANES) x = fmaf(part_of(i, h)[c], weight[i], x);
     if constexpr (LANES > 1) {
       cols[tid] = x;
       __syncthreads();
-      if (tid < DP) {
+      if (tid >= DP) return;
 #pragma unroll
-        for (int i = 1; i < LANES; ++i) x += cols[i * DP + c];
-      }
+      for (int i = 1; i < LANES; ++i) x += cols[i * DP + c];
     }
-    if (tid < DP && c < d) O[c] = (T)(x / tot);
-    if (p.lse && tid == 0) p.lse[head * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
-    __syncthreads();
+    if (c < d) out_of(head0)[c] = (T)(x / tot);
+    if (p.lse && tid == 0) p.lse[head0 * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
   }
 }
 

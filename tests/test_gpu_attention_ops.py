@@ -543,8 +543,10 @@ def test_decode_many_sequences():
 
 @pytest.mark.parametrize("dtype,cache_dtype,hq,hk", [(BF, BF, 6, 3), (FP, "e4m3", 34, 2)])
 def test_decode_more_heads_than_blocks(dtype, cache_dtype, hq, hk):
-    """Most key heads lie in one block, some in two."""
-    decode(dtype, cache_dtype, hq, hk, 64, 16, [(i * 61) % 400 for i in range(360)])
+    """Most key heads lie in one block, some in two, those of one sequence in many."""
+    lens = [(i * 61) % 400 for i in range(360)]
+    lens[100] = 30000
+    decode(dtype, cache_dtype, hq, hk, 64, 16, lens)
 
 
 @pytest.mark.parametrize("layout", ["wide", "heads_first", "odd"])
