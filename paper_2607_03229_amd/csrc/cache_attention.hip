@@ -16,7 +16,7 @@
 //
 // Scores, maxima, sums and outputs are fp32; the weights of a bf16 query are rounded to bf16 (half a
 // step of 2^-8) for the matrix unit.  Measured on MI355X: 64 sequences of up to 16384, 32/8 heads of
-// 128, bf16, pages of 32: 410 us, 5.8 TB/s, and 9 us to join (first kernel 730); four of up to
+// 128, bf16, pages of 32: 410 us, 5.8 TB/s, and 7 us to join (first kernel 730); four of up to
 // 131072, 28/4 heads, e4m3: 98 us, 4.8 TB/s, and 8 (first 320); eight of up to 1000: 11 us, a chain
 // of loads (length, page, keys), and 5 (first 27).
 #include <type_traits>
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
       const float M = warp_max(m), ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) x[j] = 0.f;
-#pragma unroll 4
+#pragma unroll 16
       for (int i = 0; i < n; ++i) {
         const float* part = part_of(i, h);
         const float weight = exp2_any(part[DP] - ref);
@@ -575,11 +575,12 @@ hipError_t launch(Args& a, int64_t units, hipStream_t s) {
     hipLaunchKernelGGL((cache_attn_kernel<T, DP, F8, SMALL>), dim3(a.blocks), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  // A block joins one query head, or, where most find nothing to join, a column block's: those of a
-  // key head that lies in one block.  Measured on MI355X, us of the join, 28/4 heads of 128, one ->
-  // all: 256 sequences of up to 64 13.6 -> 3.8, of up to 512 16.3 -> 16.8; 100 of up to 30000 12 -> 22.
+  // A query head has a block of its own, or, where that is more blocks than run at once, a wave.
+  // Measured on MI355X, us of the join, 28/4 heads of 128, block -> wave: 256 sequences of up to 512
+  // 16.3 -> 7.1, 100 of up to 30000 12.6 -> 8.8, 64 of up to 1000 7.0 -> 6.5; 8 of up to 1000 5.7 -> 7.1,
+  // four of up to 131072 7.3 -> 17.
   const int columns = a.at.n_seq * a.at.heads * a.col_blocks;
-  if (columns >= 2 * a.blocks)
+  if (columns >= 256)
     hipLaunchKernelGGL((join_kernel<T, DP, true>), dim3(columns), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((join_kernel<T, DP, false>), dim3(a.at.n_seq * a.at.heads * a.group), dim3(256), 0, s, a);
