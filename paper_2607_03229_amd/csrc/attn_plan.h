@@ -47,5 +47,10 @@ mpipe_status cache_ok(const mpipe_kv_cache* c, std::string& why);
 bool cache_meets(const mpipe_kv_cache& c, const void* p, size_t bytes);
 bool cache_meets(const mpipe_kv_cache& c, const HeadView& v, int64_t rows, int esz);
 int64_t cache_page_values(const mpipe_kv_cache& c);   // of k or v, in one page
+// The attention over a cache takes a sequence's tokens in units; its units, of 0 .. 2^31 - 1 tokens.
+constexpr int kCacheUnit = 128;
+constexpr int cache_units(int tokens) {
+  return (int)(((uint32_t)tokens + kCacheUnit - 1) / kCacheUnit);
+}
 
 }  // namespace mpipe

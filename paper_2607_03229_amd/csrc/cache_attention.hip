@@ -27,6 +27,7 @@ namespace mpipe {
 namespace {
 
 constexpr int NW = 4, TILE = 32 * NW;   // waves of a block, tokens of a unit
+static_assert(TILE == kCacheUnit, "units");
 constexpr int QG = 16;                  // query heads of a column block
 constexpr int MAX_BLOCKS = 768;          // of any variant: three a CU
 
@@ -54,7 +55,7 @@ __device__ __forceinline__ int tokens_of(const Args& p, int s, bool& all) {
 }
 __device__ __forceinline__ int units_of(const Args& p, int s) {
   bool all;
-  return (tokens_of(p, s, all) + TILE - 1) / TILE;
+  return cache_units(tokens_of(p, s, all));
 }
 
 // Units before every sequence, by the whole block: thread t adds up a run of sequences.  Calls
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
 
   while (u < u_end) {
     bool all_there;
-    const int len = __builtin_amdgcn_readfirstlane(tokens_of(p, seq, all_there)), nt = (len + TILE - 1) / TILE;
+    const int len = __builtin_amdgcn_readfirstlane(tokens_of(p, seq, all_there)), nt = cache_units(len);
     if (nt == 0) {   // (a sequence without tokens has no units)
       ++seq;
       continue;
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
       if ((!BF && !F8) || d < DP || rows.last < 31) fetch_as(std::false_type(), std::false_type());
       else fetch_as(std::true_type(), std::true_type());
     };
-    // wave w's tokens of tile t
+    // wave w's tokens of tile t, of 0 .. tile1 - 1: below 2^31
     auto start = [&](int t) { return t * TILE + 32 * w; };
     auto there = [&](int t) { return t < tile1 && start(t) < len; };
     if (there(tile0)) {
@@ -293,6 +294,7 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
     for (int t = tile0; t < tile1; ++t) {
       const int k0 = start(t);
       if (k0 >= len) break;
+      const uint32_t ku = k0, end = len;   // (k0 plus a row may be 2^31 and more)
       const float scale_kt = F8 ? e8m0(scale_k) : 1.f, scale_vt = F8 ? e8m0(scale_v) : 1.f;
       f32x4 s[2];
 #pragma unroll
@@ -317,10 +319,10 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
           }
         }
       }
-      if (k0 + 32 > len) {   // rows past the last token: 0 times the last one again could be NaN
+      if (ku + 32 > end) {   // rows past the last token: 0 times the last one again could be NaN
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (k0 + (64 * i + l) / VS >= len) vr[i] = make_uint4(0, 0, 0, 0);
+          if (ku + (64 * i + l) / VS >= end) vr[i] = make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
       for (int kq = 0; kq < 2; ++kq)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = k0 + 16 * kq + 4 * g + e < len ? s[kq][e] * sl2 : -INFINITY;
+          const float x = ku + 16 * kq + 4 * g + e < end ? s[kq][e] * sl2 : -INFINITY;
           s[kq][e] = x;
           mx = fmaxf(mx, x);
         }
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   });
   __syncthreads();
   bool all_there;
-  const int len = tokens_of(p, seq, all_there), nt = (len + TILE - 1) / TILE;
+  const int len = tokens_of(p, seq, all_there), nt = cache_units(len);
   const int64_t each = units_each(units, p.blocks);
   const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt;
   const int b0 = nt == 0 ? 0 : (int)quotient(u0, each), n = nt == 0 ? 0 : (int)quotient(u0 + nt - 1, each) - b0 + 1;
