@@ -30,6 +30,13 @@ struct AttnItem {
 void attn_items(const std::vector<AttnSeq>& seqs, bool by_keys, int rows,
                 std::vector<AttnItem>& items);
 
+// Items of `blocks` blocks each to a launch, at least one (heads end at 65536): a grid has fewer than
+// 2^32 threads, and a block of causal attention at most kAttnThreads of them.
+constexpr int kAttnThreads = 512;
+constexpr int64_t attn_launch_items(int64_t blocks) {
+  return ((int64_t(1) << 32) / kAttnThreads - 1) / blocks;
+}
+
 // What one launch carries in its arguments: sequences from the front (four words each), items
 // from the back (a word: sequence in 8 bits, tile in 24).
 constexpr int kAttnWords = 900;

@@ -94,13 +94,13 @@ int general_sub(const CausalProblem& p, bool by_keys) {
   return std::max(1, std::min(8, (longest + 15) / 16));
 }
 
-// All items, as many to a launch as its arguments and 2^23 blocks hold.
+// All items, as many to a launch as its arguments and its grid hold.
 template <class Launch>
 hipError_t in_pieces(const CausalProblem& p, CausalArgs& a, bool by_keys, int rows,
                      int64_t blocks_per_item, Launch one) {
   std::vector<AttnItem> items;
   attn_items(p.seqs, by_keys, rows, items);
-  const int64_t most = (int64_t(1) << 23) / blocks_per_item;
+  const int64_t most = attn_launch_items(blocks_per_item);
   for (size_t at = 0; at < items.size();) {
     const int n = attn_pack(p.seqs, items, at, most, a.pool);
     if (hipError_t e = one(a, n)) return e;

@@ -471,12 +471,14 @@ __global__ __launch_bounds__(64 * NWV) void causal_parts_kernel(CausalArgs p) {
 }
 
 template <int DP, int NWV> hipError_t launch_dq(const CausalArgs& a, int items, hipStream_t s) {
+  static_assert(64 * NWV <= kAttnThreads, "threads of a grid");
   hipLaunchKernelGGL((causal_dq_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
                      dim3(64 * NWV), 0, s, a);
   return hipGetLastError();
 }
 template <int DP> hipError_t launch_dkdv(const CausalArgs& a, int items, hipStream_t s) {
   constexpr int NWV = causal_k_waves(DP);
+  static_assert(64 * NWV <= kAttnThreads, "threads of a grid");
   hipLaunchKernelGGL((causal_dkdv_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.parts),
                      dim3(64 * NWV), 0, s, a);
   if (a.parts > 1)

@@ -202,6 +202,7 @@ __global__ __launch_bounds__(64 * NWV, 2) void causal_fwd_kernel(CausalArgs p) {
 }
 
 template <int DP, int NWV> hipError_t launch(const CausalArgs& a, int items, hipStream_t s) {
+  static_assert(64 * NWV <= kAttnThreads, "threads of a grid");
   hipLaunchKernelGGL((causal_fwd_kernel<DP, NWV>), dim3((unsigned)items * a.heads_k * a.group),
                      dim3(64 * NWV), 0, s, a);
   return hipGetLastError();

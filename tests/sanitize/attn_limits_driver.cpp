@@ -28,10 +28,21 @@ void check_units() {
   }
 }
 
+// A grid's threads stay below 2^32 whatever an item's blocks, in launches as full as that allows.
+void check_launches() {
+  for (int64_t blocks : {int64_t(1), int64_t(28), int64_t(512), int64_t(65535), int64_t(65536), int64_t(8) * 65536}) {
+    const int64_t items = attn_launch_items(blocks);
+    expect(items >= 1, "an item", blocks);
+    expect(items * blocks * kAttnThreads < int64_t(1) << 32, "threads of a grid", blocks);
+    expect((items + 1) * blocks * kAttnThreads >= int64_t(1) << 32, "a full grid", blocks);
+  }
+}
+
 }  // namespace
 
 int main() {
   check_units();
+  check_launches();
   if (failures) return 1;
   std::printf("attention limits passed\n");
   return 0;

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2607_03229_amd as mp
+from tests import attn_ref as R
 from tests.gpu_util import announce
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +49,36 @@ def test_cache_of_as_many_tokens_as_a_length_counts(page):
         mean, size = ((count[..., None] * y).sum((0, 1)) / n for y in (x, x.abs()))
         assert ((o[s, 0] - mean).abs() <= 2.0 ** -8 * mean.abs() + 4096 * 2.0 ** -24 * size).all(), s
         assert abs(lse[0, s] - math.log(n)) <= 4096 * 2.0 ** -24 + 2.0 ** -22 * math.log(n), s
+
+
+def test_more_threads_than_a_grid_holds():
+    """65536 heads of 128 one-row sequences: blocks of 512 threads, 2^32 of them in one launch if it
+    took all items.  All heads are alike, so one is the reference: a row's output is its only value,
+    exactly, and the key head's gradients are 65536 times one head's, in sums of as many terms."""
+    n, hq, d = 128, 65536, 128
+    gen = torch.Generator().manual_seed(3)
+    x = [torch.randn(n, 1, d, generator=gen).to(BF) for _ in range(4)]
+    q, k, v, d_o = (t.cuda() for t in x)
+    wide = lambda t: t.expand(n, hq, d)
+    o = torch.full((n, hq, d), 7.0, dtype=BF, device="cuda")
+    lse = torch.full((hq, n), 7.0, device="cuda")
+    rows, lens = list(range(n)), [1] * n
+    announce("65536 heads of 128 sequences")
+    mp.op_causal_attention_fwd(wide(q), k, v, o, lse, rows, lens)
+    ref = R.attention(*x[:3], [(i, 1, i, 1) for i in range(n)], d ** -0.5, x[3], x[2])
+    assert torch.equal(o, wide(v))
+    for h in (0, 1, hq // 2, hq - 1):
+        R.check("lse", lse[h:h + 1], ref["lse"])
+    assert torch.equal(lse, lse[:1].expand(hq, n))
+    dq = torch.full_like(o, 7.0)
+    dk, dv = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    scratch = torch.empty(mp.op_causal_attention_scratch_bytes(n, hq, n, 1, d), dtype=torch.uint8,
+                          device="cuda")
+    mp.op_causal_attention_bwd(wide(d_o), wide(q), k, v, o, lse, rows, lens, dq, dk, dv, scratch)
+    for h in (0, 1, hq // 2, hq - 1):
+        R.check("dq", dq[:, h:h + 1], ref["dq"])
+    assert torch.equal(dq, dq[:, :1].expand(n, hq, d))
+    many = hq * 2.0 ** -24
+    for name, t in (("dk", dk), ("dv", dv)):
+        value, bound = ref[name]
+        R.check(name, t, (hq * value, hq * (bound + many * (value.abs() + bound))))
