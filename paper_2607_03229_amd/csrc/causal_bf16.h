@@ -183,14 +183,18 @@ struct Feed {
 // Copies from a buffer into LDS (lane l's 16 bytes to `to` + 16 l), under way until wait_copies.
 // An instruction of its own rather than the builtin: for the builtin's copies the compiler puts
 // a wait before every transposing read, whose LDS it cannot tell from theirs.  It writes no
-// register, and reads its own as it is issued.
+// register but m0, and reads its own as it is issued.  The compiler does not look into it for hazards:
+// gfx9 wants five wait states between a vector instruction that writes a scalar register (a lane's
+// read, as of a spilled one) and a memory instruction that reads it.  s_mov is one, s_nop 3 four.
 __device__ __forceinline__ void copy16(uint32_t to, uint32_t off, const buffer_t& from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(to), "v"(off), "s"(from) : "m0");
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds"
+               : "={m0}"(m0) : "s"(to), "v"(off), "s"(from));
 }
 __device__ __forceinline__ void copy4(uint32_t to, uint32_t off, const buffer_t& from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               :: "s"(to), "v"(off), "s"(from) : "m0");
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tbuffer_load_dword %2, %3, 0 offen lds"
+               : "={m0}"(m0) : "s"(to), "v"(off), "s"(from));
 }
 
 // Wave w of NWV waves copies its share of a pair of tiles (x, then y): wave instruction j = w,
