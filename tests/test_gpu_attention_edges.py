@@ -1,12 +1,19 @@
 """The first LLM layer's attention on the GPU where its other tests do not look: infinities pinned
-(attn_strict.py)."""
+(attn_strict.py), the blocks of eight waves of 128 wide heads at their edges."""
+import math
+import os
+import re
 
+import numpy as np
 import pytest
 import torch
 
+import paper_2607_03229_amd as mp
+from paper_2607_03229_amd import build as B
 from tests import attn_ref as R
 from tests import attn_strict as S
 from tests import test_gpu_attention_ops as G
+from tests.gpu_util import announce
 
 pytestmark = pytest.mark.gpu
 BF, FP = torch.bfloat16, torch.float32
@@ -38,3 +45,135 @@ def test_tokens_of_empty_sequences(dtype, cache_dtype):
 @pytest.mark.parametrize("prefix", [[-1, -40, -500], [100, -20, 0], [-129, -64, -33]], ids=str)
 def test_queries_without_keys(dtype, d, prefix):
     G.run(dtype, 4, 2, d, [60, 77, 330], prefix=prefix, gap=2)
+
+
+# ---- blocks of eight waves ------------------------------------------------------------------------
+
+def eight_waves(d, hq, lens):
+    """Whether causal_attention.hip gives a bf16 problem blocks of eight waves, two groups of which run a
+    phase apart: heads wider than 96, and more blocks of 256 queries than its threshold."""
+    text = open(os.path.join(B.CSRC, "causal_attention.hip")).read()
+    few = int(re.search(r"constexpr int64_t kFewBlocks = (\d+);", text).group(1))
+    assert "blocks += (q.q_len + 255) / 256 * p.q.heads" in text
+    assert "return blocks > kFewBlocks ? most : 4;" in text
+    return 96 < d <= 128 and sum(-(-n // 256) for n in lens) * hq > few
+
+
+def run8(hq, hk, d, lens, **kw):
+    assert eight_waves(d, hq, lens)
+    return G.run(BF, hq, hk, d, lens, **kw)
+
+
+@pytest.mark.parametrize("d", [104, 128])
+@pytest.mark.parametrize("lens,prefix", [
+    ([600, 300, 77], [-300, -290, 64]),      # blocks and waves without a key, a shifted diagonal
+    ([530, 257, 31], [1, 100, 700]),
+    ([256, 40, 513], [-255, -40, -1]),
+    ([260, 0, 290], [0, 50, -600])], ids=str)
+def test_eight_waves_prefixes(d, lens, prefix):
+    run8(28, 4, d, lens, prefix=prefix, gap=1)
+
+
+@pytest.mark.parametrize("lens", [[1, 2, 3], [31, 32, 33], [255, 256, 257], [63, 64, 65, 700]], ids=str)
+def test_eight_waves_lengths(lens):
+    run8(28, 4, 128, lens, gap=3)
+
+
+@pytest.mark.parametrize("layout", ["wide", "heads_first"])
+def test_eight_waves_layouts(layout):
+    run8(24, 8, 128, [300, 0, 270], gap=5, layout=layout)
+
+
+def test_eight_waves_many_launches():
+    run8(2, 1, 128, [1 + i % 9 for i in range(400)])
+
+
+def test_eight_waves_sharp_scores():
+    def sharpen(x, seqs):
+        x["q"] *= 8
+        x["k"] *= 8
+    run8(28, 4, 128, [300, 577], change=sharpen)
+
+
+def test_eight_waves_the_same_bits():
+    first, again = (run8(28, 4, 128, [600, 300], prefix=[-100, 70]) for _ in range(2))
+    for name in first:
+        assert torch.equal(first[name].nan_to_num(7.0), again[name].nan_to_num(7.0)), name
+
+
+@pytest.mark.parametrize("d", [104, 128])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_eight_waves_values_behind_the_mask(d, value):
+    """A bad key or value in the middle of a tile, which only later queries see; in the backward a
+    bad query or gradient too, which only counts for the keys up to itself."""
+    n, hq, hk, at = 570, 28, 4, 400
+    assert eight_waves(d, hq, [n])
+    gen = torch.Generator().manual_seed(3)
+    x = {s: G.normal(gen, n, h, d) for s, h in (("q", hq), ("k", hk), ("v", hk), ("d_o", hq))}
+    seqs, scale = [(0, n, 0, n)], d ** -0.5
+    clean = R.attention(x["q"], x["k"], x["v"], seqs, scale)
+    o = clean["o"][0].to(BF)
+    full = R.attention(x["q"], x["k"], x["v"], seqs, scale, x["d_o"], o)
+    lse = clean["lse"][0].float().cuda()
+    scratch = torch.empty(mp.op_causal_attention_scratch_bytes(n, hq, n, hk, d), dtype=torch.uint8,
+                          device="cuda")
+    for spoilt in ("k", "v", "q", "d_o"):
+        y = {s: t.clone() for s, t in x.items()}
+        y[spoilt][at] = value
+        g = {s: t.cuda() for s, t in y.items()}
+        announce(f"eight waves, masked {spoilt} {value} {d}")
+        if spoilt in "kv":
+            out, stats = torch.empty_like(g["q"]), torch.empty(hq, n, device="cuda")
+            mp.op_causal_attention_fwd(g["q"], g["k"], g["v"], out, stats, [0], [n])
+            R.check("o", out[:at], [t[:at] for t in clean["o"]])
+            R.check("lse", stats[:, :at], [t[:, :at] for t in clean["lse"]])
+            if spoilt == "v":
+                R.check("lse", stats, clean["lse"])
+                assert not torch.isfinite(out[at:].float()).any()
+        dq, dk, dv = (torch.empty_like(g[s]) for s in ("q", "k", "v"))
+        mp.op_causal_attention_bwd(g["d_o"], g["q"], g["k"], g["v"], o.cuda(), lse, [0], [n], dq, dk,
+                                   dv, scratch)
+        R.check("dq", dq[:at], [t[:at] for t in full["dq"]])
+        if spoilt in ("q", "d_o"):
+            R.check("dk", dk[at + 1:], [t[at + 1:] for t in full["dk"]])
+            R.check("dv", dv[at + 1:], [t[at + 1:] for t in full["dv"]])
+            R.check("dq", dq[at + 1:], [t[at + 1:] for t in full["dq"]])
+
+
+def test_eight_waves_captured():
+    """A training step in a graph, replayed with new inputs, eager work between the replays."""
+    hq, hk, d, rows = 28, 4, 128, 700
+    row, ln, krow, kln = (np.array(x) for x in ([0, 400], [400, 300], [0, 350], [350, 350]))
+    assert eight_waves(d, hq, [400, 300])
+    gen = torch.Generator().manual_seed(5)
+    q, k, v, d_o = (G.normal(gen, rows, h, d).cuda() for h in (hq, hk, hk, hq))
+    outs = [torch.empty_like(t) for t in (q, q, k, v)]
+    lse = torch.empty(hq, rows, device="cuda")
+    work = torch.empty(mp.op_causal_attention_scratch_bytes(rows, hq, rows, hk, d), dtype=torch.uint8,
+                       device="cuda")
+
+    def step():
+        keys = dict(key_row=krow, key_len=kln)
+        mp.op_causal_attention_fwd(q, k, v, outs[0], lse, row, ln, **keys)
+        mp.op_causal_attention_bwd(d_o, q, k, v, outs[0], lse, row, ln, *outs[1:], work, **keys)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        for t in (q, k, v, d_o):
+            t.copy_(torch.randn(t.shape, generator=gen))
+        both = []
+        for go in (graph.replay, step):
+            for t in (*outs, lse, work):
+                t.zero_()
+            go()
+            torch.cuda.synchronize()
+            both.append([t.clone() for t in (*outs, lse)])
+        for a, b in zip(*both):
+            assert torch.equal(a, b) and a.float().abs().sum() > 0, turn
