@@ -1,5 +1,6 @@
 """The first LLM layer's attention on the GPU where its other tests do not look: infinities pinned
-(attn_strict.py), the blocks of eight waves of 128 wide heads at their edges."""
+(attn_strict.py), the blocks of eight waves of 128 wide heads at their edges, key tiles in parts over
+several launches, far offsets in fp32, 8-bit values of every exponent, streams."""
 import math
 import os
 import re
@@ -177,3 +178,131 @@ def test_eight_waves_captured():
             both.append([t.clone() for t in (*outs, lse)])
         for a, b in zip(*both):
             assert torch.equal(a, b) and a.float().abs().sum() > 0, turn
+
+
+# ---- key tiles in parts, offsets, streams -----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,hq,d,gap", [(BF, 8, 128, 95), (FP, 32, 64, 35)])
+def test_parts_over_two_launches(dtype, hq, d, gap):
+    """200 sequences of one key tile each, more than a launch's arguments hold, in as many rows as
+    let two blocks share a key tile: both launches' parts use the same scratch, in turn."""
+    G.run(dtype, hq, 1, d, [5] * 200, gap=gap)
+
+
+def test_fp32_offsets_past_32_bits():
+    """fp32 rows so far apart that elements lie behind 2^32 bytes and 2^31 elements."""
+    rows, d = 1200, 64
+    stride = (2 ** 31 // rows // 8 + 64) * 8
+    gen = torch.Generator().manual_seed(9)
+    x = [G.normal(gen, 40, 1, d, dtype=FP) for _ in range(3)]
+    big = torch.empty(rows * stride, device="cuda")
+    views = [big.as_strided((rows, 1, d), (stride, d, 1), 64 * i) for i in range(8)]
+    for view, t in zip(views, x):
+        view[-40:] = t.cuda()
+    q, k, v, o, d_o, dq, dk, dv = views
+    d_o[-40:] = x[0].cuda()
+    lse = torch.empty(1, rows, device="cuda")
+    announce("fp32 offsets past 32 bits")
+    mp.op_causal_attention_fwd(q, k, v, o, lse, [rows - 40], [40])
+    scratch = torch.empty(mp.op_causal_attention_scratch_bytes(rows, 1, rows, 1, d),
+                          dtype=torch.uint8, device="cuda")
+    mp.op_causal_attention_bwd(d_o, q, k, v, o, lse, [rows - 40], [40], dq, dk, dv, scratch)
+    ref = R.attention(*x, [(0, 40, 0, 40)], 0.125, x[0], o[-40:].cpu())
+    R.check("o", o[-40:], ref["o"])
+    R.check("lse", lse[:, -40:], ref["lse"])
+    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        R.check(name, t[-40:], ref[name])
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (FP, 64)])
+def test_all_calls_on_another_stream(dtype, d):
+    """Inputs made on one stream, the calls on another that waits for it, by `stream` alone."""
+    n, hq, hk, page = 150, 8, 2, 16
+    gen = torch.Generator().manual_seed(13)
+    x = [G.normal(gen, n, h, d, dtype=dtype) for h in (hq, hk, hk, hq)]
+    host = [t.pin_memory() for t in x]
+    table, pages = G.make_table([n], page)
+    cache = G.make_cache(pages, hk, page, d, dtype)
+    pos, seq = G.all_rows([n])
+    s = torch.cuda.Stream()
+    q, k, v, d_o = (t.cuda(non_blocking=True) for t in host)
+    outs = [torch.empty_like(t) for t in (q, q, k, v)]
+    lse = torch.empty(hq, n, device="cuda")
+    back = [torch.empty_like(t) for t in (k, v)]
+    last, lens = torch.empty_like(q[:1]), torch.tensor([n], dtype=torch.int32, device="cuda")
+    work = [torch.empty(b, dtype=torch.uint8, device="cuda") for b in
+            (mp.op_causal_attention_scratch_bytes(n, hq, n, hk, d),
+             mp.op_cache_attention_scratch_bytes(1, hq, hk, d))]
+    s.wait_stream(torch.cuda.current_stream())
+    mp.op_causal_attention_fwd(q, k, v, outs[0], lse, [0], [n], stream=s)
+    mp.op_causal_attention_bwd(d_o, q, k, v, outs[0], lse, [0], [n], *outs[1:], work[0], stream=s)
+    mp.op_cache_write(cache, k, v, table, pos, seq=seq, stream=s)
+    mp.op_cache_read(cache, table, pos, *back, seq=seq, stream=s)
+    mp.op_cache_attention(cache, q[-1:], table, lens, last, work[1], stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    ref = R.attention(*x[:3], [(0, n, 0, n)], d ** -0.5, x[3], outs[0].cpu())
+    for name, t in zip(("o", "dq", "dk", "dv"), outs):
+        R.check(name, t, ref[name])
+    R.check("lse", lse, ref["lse"])
+    R.check("token", last, [t[-1:] for t in ref["o"]])
+    assert torch.equal(back[0].cpu(), x[1]) and torch.equal(back[1].cpu(), x[2])
+
+
+# ---- 8-bit values of every exponent ------------------------------------------------------------------
+
+def eight_bits(page):
+    """A sequence for every exponent that a write makes, whose one token holds every e4m3 code."""
+    n, d = 241, 256
+    code = torch.arange(256, dtype=torch.uint8)
+    k = torch.zeros(n, 1, page, d, dtype=torch.uint8)
+    k[:, 0, 0] = code
+    scale = torch.zeros(n, 1, page, dtype=torch.uint8)
+    scale[:, 0, 0] = torch.arange(7, 248)
+    magnitude = torch.tensor(R.e4m3_values() + [math.nan], dtype=torch.float64)
+    value = torch.cat([magnitude, -magnitude]) * torch.pow(2.0, torch.arange(-120.0, 121.0).double())[:, None]
+    table = torch.arange(n, dtype=torch.int32, device="cuda")[:, None]
+    return n, d, k, scale, value, table, torch.ones(n, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("page", [1, 32])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_values_of_every_exponent(dtype, page):
+    """One token has weight 1, so the output is its value: every e4m3 code at every exponent is exact in
+    bf16, below the normal range too; 256 * 2^120 and more is infinite in both types."""
+    n, d, v, scale, value, table, lens = eight_bits(page)
+    f8 = lambda t: t.view(torch.float8_e4m3fn).cuda()
+    k = torch.zeros_like(v)
+    cache = mp.KvCache(f8(k), f8(v), torch.full_like(scale, 127).cuda(), scale.cuda())
+    q = torch.randn(n, 2, d, generator=torch.Generator().manual_seed(0)).to(dtype).cuda()
+    o, lse = torch.empty_like(q), torch.empty(2, n, device="cuda")
+    scratch = torch.empty(mp.op_cache_attention_scratch_bytes(n, 2, 1, d), dtype=torch.uint8, device="cuda")
+    announce(f"values of every exponent {dtype} page {page}")
+    mp.op_cache_attention(cache, q, table, lens, o, scratch, lse=lse)
+    want = value.to(dtype)[:, None].expand(n, 2, d)
+    got = o.cpu()
+    assert torch.equal(got.isnan(), want.isnan())
+    wrong = (got != want) & ~want.isnan()
+    assert not wrong.any(), [(i, got[tuple(i)].item(), want[tuple(i)].item())
+                             for i in torch.nonzero(wrong)[:8].tolist()]
+    assert (lse == 0).all()
+
+
+@pytest.mark.parametrize("page", [1, 32])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_keys_of_every_exponent(dtype, page):
+    """Query head c is 1 / 2^e at component c, so its only score, and with it its lse, is scale times the
+    key's e4m3 code c: one product, and roundings of scale log2(e), of the score, of its logarithm and of ln 2."""
+    n, d, k, scale, value, table, lens = eight_bits(page)
+    gone = value.isnan() | (value.float().isinf())      # 0 times these would be no number
+    k[:, 0, 0][gone] = 0
+    value = torch.where(gone, 0.0, value)
+    f8 = lambda t: t.view(torch.float8_e4m3fn).cuda()
+    cache = mp.KvCache(f8(k), f8(k.clone()), scale.cuda(), scale.clone().cuda())
+    power = torch.pow(2.0, torch.arange(-120.0, 121.0))
+    q = (torch.eye(d) / power[:, None, None]).to(dtype).cuda()
+    o, lse = torch.empty_like(q), torch.empty(d, n, device="cuda")
+    scratch = torch.empty(mp.op_cache_attention_scratch_bytes(n, d, 1, d), dtype=torch.uint8, device="cuda")
+    announce(f"keys of every exponent {dtype} page {page}")
+    mp.op_cache_attention(cache, q, table, lens, o, scratch, lse=lse)
+    want = (value / power.double()[:, None] / 16).t()
+    R.check("lse", lse, (want, 8 * 2.0 ** -24 * want.abs()))
