@@ -602,7 +602,8 @@ int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 }  // namespace
 
-size_t cache_attention_scratch(int n_seq, int heads_q, int heads_k, int head_dim) {
+// (two parts a block, whatever the batch)
+size_t cache_attention_scratch(int head_dim) {
   return (size_t)2 * MAX_BLOCKS * QG * (padded(head_dim) + 2) * sizeof(float);
 }
 

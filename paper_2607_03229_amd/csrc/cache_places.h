@@ -11,15 +11,14 @@ constexpr int64_t kCacheNone = -1;   // a row that is left out
 constexpr int64_t kCacheBad = -2;    // a place outside the tables or the pool
 
 // n / d for n below 2^32 (d at most 2^17) by a product: n (2^49 / d rounded up) / 2^49, off by less
-// than n / 2^49 < 1 / d.  Larger n are divided.
+// than n / 2^49 < 1 / d.  (A launch's lanes end at 2^31, and a last block's beyond are some hundreds.)
 struct Divide {
   uint64_t mul;
-  uint32_t d;
   __device__ __forceinline__ int64_t quotient(int64_t n) const {
-    return n >> 32 ? n / d : (int64_t)(__umul64hi((uint64_t)n << 15, mul));
+    return (int64_t)__umul64hi((uint64_t)n << 15, mul);
   }
 };
-inline Divide divide_by(uint32_t d) { return {((uint64_t(1) << 49) + d - 1) / d, d}; }
+inline Divide divide_by(uint32_t d) { return {((uint64_t(1) << 49) + d - 1) / d}; }
 
 struct CachePlaces {
   const int32_t *table, *seq, *pos;

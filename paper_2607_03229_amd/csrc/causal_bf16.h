@@ -253,8 +253,8 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& s, int j) {
   for (int e = 0; e < 8; ++e) r[e] = (bf16)s[8 * j + e];
   return r;
 }
-// Order of a stretch of products whose operands come from LDS: `ahead` reads first, then with each
-// product the reads of one that is `ahead` reads later.  One wave of a SIMD reads at a time and a
+// Order of a stretch of products whose operands come from LDS, the first of them read before: with
+// each product the reads of one that is some reads later.  One wave of a SIMD reads at a time and a
 // read takes a few hundred cycles, so the compiler's own order, a few reads ahead, left the
 // matrix unit idle half of the time.
 template <int N, int READS> __device__ __forceinline__ void order_step() {
@@ -263,9 +263,6 @@ template <int N, int READS> __device__ __forceinline__ void order_step() {
     if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);   // LDS reads
     order_step<N - 1, READS>();
   }
-}
-template <int READS> __device__ __forceinline__ void order_reads() {
-  __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
 }
 
 template <int N> __device__ __forceinline__ bool finite16(const f32x16 (&acc)[N]) {
