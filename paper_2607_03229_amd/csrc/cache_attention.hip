@@ -472,15 +472,97 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
   }
 }
 
+// One query head's parts of n blocks from b0 on: part i is block b0 + i's; the first block's begins the
+// head, the others' begin the block.  h: the head's place in its column block.
+template <int DP> __device__ __forceinline__ const float* part_of(const Args& p, int b0, int i, int h) {
+  return p.part + ((int64_t)(2 * (b0 + i) + (i == 0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
+}
+
+// Joins them with a block.
+template <class T, int DP>
+__device__ __forceinline__ void join_by_block(const Args& p, int seq, int head, int h, int b0, int n) {
+  constexpr int LANES = 256 / DP;   // threads to a column
+  __shared__ float weight[MAX_BLOCKS], top[4], total[4], cols[256];
+  const int tid = threadIdx.x;
+  float m = -INFINITY;
+  for (int i = tid; i < n; i += 256) {
+    weight[i] = part_of<DP>(p, b0, i, h)[DP];
+    m = fmaxf(m, weight[i]);
+  }
+  m = warp_max(m);
+  if (tid % 64 == 0) top[tid / 64] = m;
+  __syncthreads();
+  const float M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), ref = M == -INFINITY ? 0.f : M;
+  float tot = 0.f;
+  for (int i = tid; i < n; i += 256) {
+    weight[i] = exp2_any(weight[i] - ref);
+    tot += part_of<DP>(p, b0, i, h)[DP + 1] * weight[i];
+  }
+  tot = warp_sum(tot);
+  if (tid % 64 == 0) total[tid / 64] = tot;
+  __syncthreads();
+  tot = total[0] + total[1] + total[2] + total[3];
+  const int c = tid % DP;
+  float x = 0.f;
+#pragma unroll 8
+  for (int i = tid / DP; i < n; i += LANES) x = fmaf(part_of<DP>(p, b0, i, h)[c], weight[i], x);
+  if constexpr (LANES > 1) {
+    cols[tid] = x;
+    __syncthreads();
+    if (tid >= DP) return;
+#pragma unroll
+    for (int i = 1; i < LANES; ++i) x += cols[i * DP + c];
+  }
+  if (c < p.at.d) reinterpret_cast<T*>(const_cast<void*>(p.o.p))[p.o.row * seq + p.o.head * head + c] = (T)(x / tot);
+  if (p.lse && tid == 0) p.lse[head * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
+}
+
 // Joins the parts of one (sequence, query head) with a block, or (ALL) of the query heads of a column
 // block with a wave each; sequences without tokens get their outputs here.
+//
+// A wave adds a head's parts one by one, and a column block has up to four heads for each, so (ALL)
+// heads of more than LONG parts get a block each all the same: those behind the column blocks'.  More
+// than LONG parts are LONG blocks at least that begin inside the head, one of which has a number that is a
+// multiple of LONG, so every such number is looked at.  Measured on MI355X, us of the join, heads of 128,
+// without these blocks -> with them: one sequence of 131072 tokens among 255 of 100, 16/1 heads, 108 -> 15
+// (beside 39 of the attention), among 63, 28/4 heads, 22 -> 8; 256 sequences of up to 512, 28/4 heads,
+// none of them long, 7.2 -> 7.2, and of up to 200, 8/8 heads, 5.6 -> 6.0.
+constexpr int LONG = 16;
+
 template <class T, int DP, bool ALL>
 __global__ __launch_bounds__(256) void join_kernel(Args p) {
-  constexpr int LANES = 256 / DP;   // threads to a column
   __shared__ int64_t sums[4];
   __shared__ int64_t before_s;
+  __shared__ int long_seq;
   const int tid = threadIdx.x, heads_v = p.at.heads * p.col_blocks, d = p.at.d;
   const int items = ALL ? heads_v : p.at.heads * p.group;   // of a sequence
+  const int of_long = ALL ? (int)blockIdx.x - p.at.n_seq * items : -1;
+  if (ALL && of_long >= 0) {
+    const int width = min(QG, p.group), b = (of_long / width + 1) * LONG, h = of_long % width;
+    if (tid == 0) long_seq = -1;
+    __syncthreads();
+    // the sequence that holds block b's first unit
+    const int64_t units = heads_v * scan_units(p, sums, [&](int s, int64_t before, int64_t all) {
+      const int64_t u = b * units_each(heads_v * all, p.blocks), lo = heads_v * before;
+      if (u >= lo && u < lo + (int64_t)heads_v * units_of(p, s)) {
+        long_seq = s;
+        before_s = lo;
+      }
+    });
+    __syncthreads();
+    const int seq = long_seq;
+    if (seq < 0) return;   // no such unit
+    const int nt = units_of(p, seq);
+    const int64_t each = units_each(units, p.blocks);
+    const int hv = (int)quotient(b * each - before_s, nt);
+    const int64_t u0 = before_s + (int64_t)hv * nt;
+    const int b0 = (int)quotient(u0, each), n = (int)quotient(u0 + nt - 1, each) - b0 + 1;
+    const int first = hv % p.col_blocks * QG;
+    // (the first such number inside the head joins it)
+    if (n <= LONG || b - LONG > b0 || b == b0 || first + h >= p.group) return;
+    join_by_block<T, DP>(p, seq, hv / p.col_blocks * p.group + first + h, h, b0, n);
+    return;
+  }
   const int seq = blockIdx.x / items, item = blockIdx.x % items;
   const int head_k = item / (ALL ? p.col_blocks : p.group);
   const int first = ALL ? item % p.col_blocks * QG : item % p.group;   // of the key head's
@@ -494,14 +576,9 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   const int64_t each = units_each(units, p.blocks);
   const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt;
   const int b0 = nt == 0 ? 0 : (int)quotient(u0, each), n = nt == 0 ? 0 : (int)quotient(u0 + nt - 1, each) - b0 + 1;
-  if (n == 1) return;   // written by its block
+  if (n == 1 || (ALL && n > LONG)) return;   // written by its block, or joined by those behind
   auto out_of = [&](int head) {
     return reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * head;
-  };
-  // part i of head h of the column block: of block b0 + i; the first block's begins the head, the
-  // others' begin the block
-  auto part_of = [&](int i, int h) {
-    return p.part + ((int64_t)(2 * (b0 + i) + (i == 0 ? 1 : 0)) * QG + h) * PartOf<DP>::ROW;
   };
   const int head0 = head_k * p.group + first;
   if (nt == 0) {
@@ -513,14 +590,14 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   if constexpr (ALL) {
     const int l = tid & 63;
     for (int h = tid >> 6; h < count; h += 4) {
-      float m = -INFINITY, tot = 0.f, x[DP / 64];
-      for (int i = l; i < n; i += 64) m = fmaxf(m, part_of(i, h)[DP]);
+      const float m = l < n ? part_of<DP>(p, b0, l, h)[DP] : -INFINITY;
       const float M = warp_max(m), ref = M == -INFINITY ? 0.f : M;
+      float tot = 0.f, x[DP / 64];
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) x[j] = 0.f;
-#pragma unroll 16
+#pragma unroll 8
       for (int i = 0; i < n; ++i) {
-        const float* part = part_of(i, h);
+        const float* part = part_of<DP>(p, b0, i, h);
         const float weight = exp2_any(part[DP] - ref);
         tot += part[DP + 1] * weight;
 #pragma unroll
@@ -533,39 +610,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
       if (p.lse && l == 0) p.lse[(head0 + h) * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
     }
   } else {
-    __shared__ float weight[MAX_BLOCKS], top[4], total[4], cols[256];
-    const int h = first % QG;
-    float m = -INFINITY;
-    for (int i = tid; i < n; i += 256) {
-      weight[i] = part_of(i, h)[DP];
-      m = fmaxf(m, weight[i]);
-    }
-    m = warp_max(m);
-    if (tid % 64 == 0) top[tid / 64] = m;
-    __syncthreads();
-    const float M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), ref = M == -INFINITY ? 0.f : M;
-    float tot = 0.f;
-    for (int i = tid; i < n; i += 256) {
-      weight[i] = exp2_any(weight[i] - ref);
-      tot += part_of(i, h)[DP + 1] * weight[i];
-    }
-    tot = warp_sum(tot);
-    if (tid % 64 == 0) total[tid / 64] = tot;
-    __syncthreads();
-    tot = total[0] + total[1] + total[2] + total[3];
-    const int c = tid % DP;
-    float x = 0.f;
-#pragma unroll 8
-    for (int i = tid / DP; i < n; i += LANES) x = fmaf(part_of(i, h)[c], weight[i], x);
-    if constexpr (LANES > 1) {
-      cols[tid] = x;
-      __syncthreads();
-      if (tid >= DP) return;
-#pragma unroll
-      for (int i = 1; i < LANES; ++i) x += cols[i * DP + c];
-    }
-    if (c < d) out_of(head0)[c] = (T)(x / tot);
-    if (p.lse && tid == 0) p.lse[head0 * p.ld_lse + seq] = (M + log2f(tot)) * kLn2;
+    join_by_block<T, DP>(p, seq, head0, first % QG, b0, n);
   }
 }
 
@@ -577,13 +622,14 @@ hipError_t launch(Args& a, int64_t units, hipStream_t s) {
     hipLaunchKernelGGL((cache_attn_kernel<T, DP, F8, SMALL>), dim3(a.blocks), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  // A query head has a block of its own, or, where that is more blocks than run at once, a wave.
+  // A query head has a block of its own, or, from 256 column blocks on (one for every CU), a wave.
   // Measured on MI355X, us of the join, 28/4 heads of 128, block -> wave: 256 sequences of up to 512
   // 16.3 -> 7.1, 100 of up to 30000 12.6 -> 8.8, 64 of up to 1000 7.0 -> 6.5; 8 of up to 1000 5.7 -> 7.1,
   // four of up to 131072 7.3 -> 17.
   const int columns = a.at.n_seq * a.at.heads * a.col_blocks;
   if (columns >= 256)
-    hipLaunchKernelGGL((join_kernel<T, DP, true>), dim3(columns), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((join_kernel<T, DP, true>),
+                       dim3(columns + (a.blocks - 1) / LONG * (a.group < QG ? a.group : QG)), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((join_kernel<T, DP, false>), dim3(a.at.n_seq * a.at.heads * a.group), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -1,6 +1,7 @@
 """The first LLM layer's attention on the GPU where its other tests do not look: infinities pinned
 (attn_strict.py), the blocks of eight waves of 128 wide heads at their edges, key tiles in parts over
-several launches, far offsets in fp32, 8-bit values of every exponent, streams."""
+several launches, far offsets in fp32, 8-bit values of every exponent, streams, long sequences among
+short ones."""
 import math
 import os
 import re
@@ -306,3 +307,48 @@ def test_keys_of_every_exponent(dtype, page):
     mp.op_cache_attention(cache, q, table, lens, o, scratch, lse=lse)
     want = (value / power.double()[:, None] / 16).t()
     R.check("lse", lse, (want, 8 * 2.0 ** -24 * want.abs()))
+
+
+# ---- one long sequence among many short ones ----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,cache_dtype,hq,hk,d", [
+    (BF, BF, 2, 1, 64), (BF, "e4m3", 7, 1, 128), (FP, FP, 3, 1, 64), (FP, "e4m3", 17, 1, 128),
+    (BF, BF, 34, 2, 64), (BF, BF, 4, 1, 256)], ids=str)
+def test_long_sequences_among_short_ones(dtype, cache_dtype, hq, hk, d):
+    """256 column blocks and more: a head's parts are joined by a wave up to 16 of them, by a block
+    beyond.  With one unit of 128 tokens a block, a sequence's parts are its units: 15 to 18, 32 to
+    34, at places that begin in every remainder of 16, neighbours too."""
+    for n in (15, 16, 17, 33):
+        lens = [(i * 29) % 128 for i in range(280)]
+        for at, more in ((0, 0), (1, 1), (101, 0), (150, 2), (279, 1)):
+            lens[at] = 128 * (n + more) - at % 3
+        G.decode(dtype, cache_dtype, hq, hk, d, 16, lens)
+
+
+def test_a_long_sequence_is_joined_by_many_blocks():
+    """256 sequences, one of which is long, take about as long as that one alone, as they read about as
+    much: its 16 query heads are joined by a block each.  (Joined by four waves they took 147 us for 53;
+    the bound lies between.)"""
+    page, hq, d, far = 16, 16, 128, 131072
+    gen = torch.Generator().manual_seed(0)
+
+    def call(lens):
+        table, pages = G.make_table(lens, page)
+        cache = mp.KvCache(*(torch.zeros(pages, 1, page, d, dtype=BF, device="cuda") for _ in range(2)))
+        q = G.normal(gen, len(lens), hq, d).cuda()
+        o, ln = torch.empty_like(q), torch.tensor(lens, dtype=torch.int32, device="cuda")
+        scratch = torch.empty(mp.op_cache_attention_scratch_bytes(len(lens), hq, 1, d), dtype=torch.uint8,
+                              device="cuda")
+        best = math.inf
+        for i in range(30):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(10):
+                mp.op_cache_attention(cache, q, table, ln, o, scratch)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) / 10)
+        return best
+
+    alone, among = call([far]), call([far] + [100] * 255)
+    assert among <= 1.8 * alone, (among, alone)
