@@ -1013,8 +1013,10 @@ def _row_ints(t, rows: int, dev: int, what: str) -> Optional[int]:
 
 def _cache_rows(cache, k, v, table, pos, seq, status):
     import torch
-    rows, d, dtype, dev = k.shape[0], cache.head_dim, k.dtype, cache.dev
     what = "k and v: [rows][heads][head_dim] of one dtype"
+    if k.dim() != 3:
+        _bad(what)
+    rows, d, dtype, dev = k.shape[0], cache.head_dim, k.dtype, cache.dev
     if pos is None:
         _bad("pos: int32 [rows]")
     return (rows, _code(dtype), _view(k, rows, d, dtype, dev, what),
@@ -1048,6 +1050,8 @@ def op_cache_attention(cache, q, table, lens, o, scratch, lse=None, scale: Optio
     its lens[s] (int32) tokens in the cache, the new one's own among them.  lse: fp32
     [heads][sequences], may be None.  scratch: op_cache_attention_scratch_bytes."""
     import torch
+    if q.dim() != 3:
+        _bad(_ATTN_Q)
     n, d, dtype, dev = q.shape[0], cache.head_dim, q.dtype, cache.dev
     at, ld, seqs, width = _table(table, dev)
     if seqs != n:
