@@ -9,7 +9,16 @@ from tests import attn_ref as R
 from tests.gpu_util import announce
 
 pytestmark = pytest.mark.gpu
-BF, FP = torch.bfloat16, torch.float32
+BF = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def float32_default():
+    """Other test modules change torch's default type as they are imported."""
+    old = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(old)
 
 
 @pytest.mark.parametrize("page", [16, 64])
