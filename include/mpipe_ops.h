@@ -265,7 +265,11 @@ mpipe_status mpipe_op_grad_clip(const mpipe_grad_tensor* grads, const mpipe_grad
  * A query that sees no key gets o = 0 and lse = -infinity, and gradients of 0.  A key that a
  * query does not see does not count for it, whatever its values.  Rows of no sequence keep what
  * they held in every output.  Scores, statistics and sums are fp32; in bf16 the weights and the
- * score gradients are rounded to bf16 (half a step, 2^-8 of the value at most) before their products.
+ * score gradients are rounded to bf16 (half a step, 2^-8 of the value at most) before their products,
+ * a weight on its way into a score gradient keeps 24 bits, the rest cut off, and a weight below fp32's
+ * normal range is 0.  (bf16 heads wider than 128, views whose address or strides are no multiples of
+ * 16 bytes and rows more than 2^23 elements apart go through fp32 products: slower, and nothing is
+ * rounded before the outputs.)
  * The same call gives the same bits.  Outputs are apart from every other buffer but each other's
  * columns of one product, side by side. */
 mpipe_status mpipe_op_causal_attention_fwd(int32_t dtype, int32_t head_dim, int64_t rows_q,
@@ -277,7 +281,8 @@ mpipe_status mpipe_op_causal_attention_fwd(int32_t dtype, int32_t head_dim, int6
                                            float* lse, int64_t ld_lse, void* hip_stream);
 
 /* Its backward: dq, dk, dv overwritten (a key that no query sees gets 0) from d_o, the gradient
- * of o, and the forward's inputs, o and lse.  lse itself has no gradient here.  The gradients of a
+ * of o, and the forward's inputs, o and lse.  The sum of d_o o that the score gradients are taken
+ * against is made from o as it is given, rounded to its type.  lse itself has no gradient here.  The gradients of a
  * key head are summed over the query heads of its group, in an order that the arguments fix.  scratch:
  * mpipe_op_causal_attention_scratch_bytes, aligned to 16 bytes, not kept. */
 mpipe_status mpipe_op_causal_attention_bwd(int32_t dtype, int32_t head_dim, int64_t rows_q,

@@ -1,10 +1,11 @@
 // Attention of one new token of every sequence over a paged cache (mpipe_op_cache_attention).
 //
-// Every key and value is read once, so HBM is the bound; the products (a group's query heads, up
-// to 16 at a time, against 16 keys) take a small part of the MFMA rate.  The work is one line of
-// units, TILE tokens of one (sequence, key head) each, sequences one behind the other; of U units
-// each block takes ceil(U / blocks) in turn, so that every block reads as much whatever the
-// lengths.  U comes from the device's lengths: every block adds them up itself, and nothing has to
+// Every key and value is read once for 16 query heads of its group, so HBM is the bound up to there (64
+// sequences of up to 8192, heads of 128 to one key head, bf16: 16 of them 47 us, 64 of them 131); the
+// products (up to 16 heads against 16 keys) take a small part of the bf16 MFMA rate, and half of the
+// fp32 one.  The work is one line of units, TILE tokens of one (sequence, key head) each, sequences one
+// behind the other; of U units each block takes ceil(U / blocks) in turn, so that every block reads as
+// much whatever the lengths.  U comes from the device's lengths: every block adds them up itself, and nothing has to
 // be known on the host.  A block that covers a head's whole length writes its output; otherwise
 // it leaves (maximum, sum, weighted values) of its part, and a second kernel joins a head's
 // parts in order.  A block has at most two such parts: where it starts and where it ends.
@@ -142,7 +143,8 @@ template <bool EXACT> __device__ __forceinline__ uint4 load_e4m3x16(const uint8_
 }
 
 // A bf16 wave's 32 rows of V in LDS: 16-byte chunk c of row R at c ^ mix(R), so that the transposing
-// reads (8 rows x 32 bytes at a time) and the writes of whole rows meet no bank twice.
+// reads (8 rows x 32 bytes at a time) and the writes of whole rows meet no bank twice.  (Values of 8 bits
+// are written two or four chunks a lane, which do meet: for 6 % of the time in bf16, 19 % in fp32.)
 template <int DP> __device__ __forceinline__ int mix(int row) {
   return DP == 64 ? (row >> 1 & 3) << 1 : (row & 7) << 1;
 }

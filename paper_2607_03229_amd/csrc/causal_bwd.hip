@@ -5,10 +5,13 @@
 // Scores, D and all sums are fp32; P and dS are rounded to bf16 (half a step of 2^-8) as operands of
 // their products, and P enters dS with 24 bits.
 //
-// Bound by the matrix unit: 6 d operations a pair in dQ and 8 d in dK and dV (a kernel of its own
-// for dQ: added to by many key tiles at once it would need atomics, or ordered turns).  Measured on
-// MI355X, eight sequences of up to 8192, 28/4 heads of 128: dQ 3.43 ms, 1.19 PFLOP/s of the pairs
-// that count; dK and dV 5.07 ms, 1.07 PFLOP/s (first kernels: 336 ms for both).
+// Bound by the matrix unit, at the clock that its power leaves: 6 d operations a pair in dQ and 8 d in
+// dK and dV (a kernel of its own for dQ: added to by many key tiles at once it would need atomics, or
+// ordered turns, which were not measured).  On MI355X, eight sequences of up to 8192, 28/4 heads of 128:
+// dQ 3.51 ms, 1.16 PFLOP/s of the pairs that count; dK and dV 5.14 ms, 1.06 PFLOP/s (first kernels: 336 ms
+// for both); the matrix unit busy for 62 and 58 % of the time at 1.75 of 2.4 GHz, no cycle lost to LDS
+// banks.  Short sequences wait for their first tiles instead: 64 of up to 700, 16 heads of 80, 162 and
+// 265 us, 18 and 19 % busy.
 #include <type_traits>
 
 #include "causal_bf16.h"

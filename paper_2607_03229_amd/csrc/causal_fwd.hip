@@ -9,11 +9,13 @@
 // from LDS by transposing reads: nothing is shuffled or written back between the products.  Scores,
 // m, sum and o are fp32; P is rounded to bf16 (half a step of 2^-8), as the matrix unit takes it.
 //
-// Bound by the matrix unit (4 d operations a pair).  Two waves share a SIMD and run a phase apart:
-// one's 2 KF + 4 DT products meet the other's 64 exponentials.  Tiles go global to LDS in copies
-// three tiles ahead.  Measured on MI355X: eight sequences of up to 8192, 28/4 heads of 128, 2.47 ms,
-// 1.11 PFLOP/s of the pairs that count (first kernel, fp32 products of 16 rows: 73 ms); 512 rows
-// after 32256, four sequences, 32/8 heads, 0.89 ms, 1.22 PFLOP/s; one sequence of 77 7 us.
+// Bound by the matrix unit (4 d operations a pair) and the vector unit beside it, at the clock that
+// their power leaves.  Two waves share a SIMD and run a phase apart: one's 2 KF + 4 DT products meet the
+// other's 64 exponentials.  Tiles go global to LDS in copies three tiles ahead.  Measured on MI355X:
+// eight sequences of up to 8192, 28/4 heads of 128, 2.52 ms, 1.08 PFLOP/s of the pairs that count (first
+// kernel, fp32 products of 16 rows: 73 ms), the matrix unit busy for 55 % of the time and the vector unit
+// for 50, at 1.65 to 1.8 of 2.4 GHz, no cycle lost to LDS banks; 512 rows after 32256, four sequences,
+// 32/8 heads, 0.92 ms, 1.19 PFLOP/s, 64 and 55 %; one sequence of 77 7 us.
 #include <type_traits>
 
 #include "causal_bf16.h"

@@ -13,10 +13,15 @@
 // so scores never leave their registers.  Values are widened to fp32 as they are read: bf16
 // products are then exact and weights are not rounded.
 //
-// Bound by the fp32 MFMA rate (157 TFLOP/s) and, below some 1000 rows, by one tile's chain of loads
-// and products.  Measured on MI355X, eight fp32 sequences of 2048, 8 heads of 64: forward 0.43 ms,
-// 81 TFLOP/s; backward 1.62 ms, 53 TFLOP/s of five products (seven are made); five of up to 333, 6
-// heads of 64: 12.7, 17.0 and 20.8 us.
+// Bound by the CU's path of loads: each wave takes the other side's rows from the caches itself, in both
+// forms, eight operations a byte.  Counted on MI355X, eight fp32 sequences of 2048, 8 heads of 64: that
+// path is busy for 93 % of the time in all three kernels, the matrix unit for 52, 51 and 44 % (forward
+// 0.43 ms, 81 of the 152 TFLOP/s that a large product reaches; backward 1.62 ms, 53 TFLOP/s of five
+// products, seven are made).  16/4 heads of 128: 96, 72 and 54 %, and 49, 38 and 37 %; the last two have
+// registers for one wave a SIMD.  Below some 1000 rows it is one tile's chain of loads and products: five
+// of up to 333, 6 heads of 64: 12.7, 17.0 and 20.8 us.  bf16 at width 256, where the backward spills
+// registers too: four of 2048, 8/2 heads of 256, forward 1.63 ms, backward 5.7 (heads of 128, on bf16
+// products, 0.06 and 0.19).
 //
 // A key that a query does not see has weight 0, but 0 times an infinity or a NaN of its value
 // would still reach the sum.  Only tiles that the diagonal cuts hold such pairs, and only an
