@@ -25,7 +25,7 @@ def float32_default():
 def test_cache_of_as_many_tokens_as_a_length_counts(page):
     """Tables of up to 2^31 - page tokens, all in the pages of one sequence of four.  Queries of 0
     weigh all tokens alike, so the output is the mean of the values: the weights' sums are whole
-    numbers, exact in fp32 up to 2^24, beyond which a wave's sum and the joins of at most 3072
+    numbers, exact in fp32 up to 2^24, beyond which a wave's sum and the joins of at most 4096
     waves round by 2^-24 each; one rounding to bf16."""
     d, width = 64, 2 ** 31 // page - 1
     gen = torch.Generator().manual_seed(page)
