@@ -93,6 +93,6 @@ struct CacheAttention {
   float* scratch = nullptr;
 };
 hipError_t cache_attention(const CacheAttention& p, hipStream_t s);
-size_t cache_attention_scratch(int head_dim);
+size_t cache_attention_scratch(int n_seq, int head_dim);
 
 }  // namespace mpipe

@@ -317,7 +317,7 @@ size_t mpipe_op_cache_attention_scratch_bytes(int32_t n_seq, int32_t heads_q, in
   if (n_seq < 0 || heads_q < 1 || heads_q > 65536 || heads_k < 1 || heads_q % heads_k ||
       !dim_ok(head_dim))
     return 0;
-  return cache_attention_scratch(head_dim);
+  return cache_attention_scratch(n_seq, head_dim);
 }
 
 mpipe_status mpipe_op_cache_attention(const mpipe_kv_cache* cache, int32_t dtype, int32_t n_seq,
@@ -352,7 +352,7 @@ mpipe_status mpipe_op_cache_attention(const mpipe_kv_cache* cache, int32_t dtype
       return invalid("ld_table must be at least the width");
     if ((int64_t)width * cache->page > INT32_MAX)
       return set_error(MPIPE_ERR_UNSUPPORTED, "a table of more than 2^31 - 1 tokens");
-    const size_t need = cache_attention_scratch(d);
+    const size_t need = cache_attention_scratch(n_seq, d);
     if (!scratch || scratch_bytes < need) return set_error(MPIPE_ERR_WORKSPACE, "scratch too small");
     if ((uintptr_t)scratch % 16) return invalid("scratch misaligned");
     const struct {

@@ -5,10 +5,13 @@
 // products (up to 16 heads against 16 keys) take a small part of the bf16 MFMA rate, and half of the
 // fp32 one.  The work is one line of units, TILE tokens of one (sequence, key head) each, sequences one
 // behind the other; of U units each block takes ceil(U / blocks) in turn, so that every block reads as
-// much whatever the lengths.  U comes from the device's lengths: every block adds them up itself, and nothing has to
-// be known on the host.  A block that covers a head's whole length writes its output; otherwise
-// it leaves (maximum, sum, weighted values) of its part, and a second kernel joins a head's
-// parts in order.  A block has at most two such parts: where it starts and where it ends.
+// much whatever the lengths.  U comes from the device's lengths: every block adds them up itself, and
+// nothing has to be known on the host.  A block that covers a head's whole length writes its output;
+// otherwise it leaves (maximum, sum, weighted values) of its part, and a second kernel joins a head's
+// parts in order.  A block has at most two such parts: where it starts and where it ends.  The second
+// kernel has blocks for every sequence, so it takes the units before one from the first, which leaves
+// them in scratch (16384 sequences of up to 100, 8/8 heads of 128: 0.18 ms of join beside 1.7, where it
+// took 10.5 with every block adding all lengths up again).
 //
 // In a block a wave takes 32 of a unit's tokens: S^T = K Q^T with a query head per column, so that
 // maxima and sums are lane exchanges within a column, and P^T is already the operand of
@@ -17,8 +20,8 @@
 //
 // Scores, maxima, sums and outputs are fp32; the weights of a bf16 query are rounded to bf16 (half a
 // step of 2^-8) for the matrix unit.  Measured on MI355X: 64 sequences of up to 16384, 32/8 heads of
-// 128, bf16, pages of 32: 410 us, 5.8 TB/s, and 7 us to join (first kernel 730); four of up to
-// 131072, 28/4 heads, e4m3: 98 us, 4.8 TB/s, and 8 (first 320); eight of up to 1000: 11 us, a chain
+// 128, bf16, pages of 32: 410 us, 5.8 TB/s, and 6 us to join (first kernel 730); four of up to
+// 131072, 28/4 heads, e4m3: 98 us, 4.8 TB/s, and 7 (first 320); eight of up to 1000: 11 us, a chain
 // of loads (length, page, keys), and 5 (first 27).
 #include <type_traits>
 
@@ -40,6 +43,7 @@ struct Args {
   const int32_t* lens;
   float* lse;
   float* part;      // [2 * blocks][QG][DP + 2]: weighted values, maximum, sum
+  int64_t* before;  // [n_seq + 1]: units before every sequence, and all, which one kernel leaves to the other
   int64_t ld_lse;
   float scale;
   int group, col_blocks, blocks;   // query heads per key head, in blocks of QG
@@ -60,7 +64,7 @@ __device__ __forceinline__ int units_of(const Args& p, int s) {
 }
 
 // Units before every sequence, by the whole block: thread t adds up a run of sequences.  Calls
-// `found(s, units before s)` on the threads whose run holds unit u.  Returns all units.
+// `found(s, units before s, all units)` for each, on the thread whose run holds it.  Returns all units.
 template <class Found>
 __device__ __forceinline__ int64_t scan_units(const Args& p, int64_t* sums, Found found) {
   const int t = threadIdx.x, n = p.at.n_seq, per = (n + 255) / 256;
@@ -205,6 +209,10 @@ __global__ __launch_bounds__(256, (blocks_per_cu(DP, F8, sizeof(T) == 2))) void 
     if (u0 >= lo && u0 < hi) {
       start_seq = s;
       start_before = lo;
+    }
+    if (blockIdx.x == 0) {
+      p.before[s] = before;
+      if (s == 0) p.before[p.at.n_seq] = all;
     }
   });
   __syncthreads();
@@ -527,37 +535,31 @@ __device__ __forceinline__ void join_by_block(const Args& p, int seq, int head, 
 // than LONG parts are LONG blocks at least that begin inside the head, one of which has a number that is a
 // multiple of LONG, so every such number is looked at.  Measured on MI355X, us of the join, heads of 128,
 // without these blocks -> with them: one sequence of 131072 tokens among 255 of 100, 16/1 heads, 108 -> 15
-// (beside 39 of the attention), among 63, 28/4 heads, 22 -> 8; 256 sequences of up to 512, 28/4 heads,
-// none of them long, 7.2 -> 7.2, and of up to 200, 8/8 heads, 5.6 -> 6.0.
+// (beside 39 of the attention), among 63, 28/4 heads, 22 -> 8.  With them 256 sequences of up to 512, 28/4
+// heads, none of them long, take 6.1 us, and of up to 200, 8/8 heads, 5.1.
 constexpr int LONG = 16;
 
 template <class T, int DP, bool ALL>
 __global__ __launch_bounds__(256) void join_kernel(Args p) {
-  __shared__ int64_t sums[4];
-  __shared__ int64_t before_s;
   __shared__ int long_seq;
   const int tid = threadIdx.x, heads_v = p.at.heads * p.col_blocks, d = p.at.d;
   const int items = ALL ? heads_v : p.at.heads * p.group;   // of a sequence
   const int of_long = ALL ? (int)blockIdx.x - p.at.n_seq * items : -1;
   if (ALL && of_long >= 0) {
     const int width = min(QG, p.group), b = (of_long / width + 1) * LONG, h = of_long % width;
+    const int64_t each = units_each(heads_v * p.before[p.at.n_seq], p.blocks), u = b * each;
     if (tid == 0) long_seq = -1;
     __syncthreads();
     // the sequence that holds block b's first unit
-    const int64_t units = heads_v * scan_units(p, sums, [&](int s, int64_t before, int64_t all) {
-      const int64_t u = b * units_each(heads_v * all, p.blocks), lo = heads_v * before;
-      if (u >= lo && u < lo + (int64_t)heads_v * units_of(p, s)) {
-        long_seq = s;
-        before_s = lo;
-      }
-    });
+    for (int s = tid; s < p.at.n_seq; s += 256)
+      if (heads_v * p.before[s] <= u && u < heads_v * p.before[s + 1]) long_seq = s;
     __syncthreads();
     const int seq = long_seq;
     if (seq < 0) return;   // no such unit
     const int nt = units_of(p, seq);
-    const int64_t each = units_each(units, p.blocks);
-    const int hv = (int)quotient(b * each - before_s, nt);
-    const int64_t u0 = before_s + (int64_t)hv * nt;
+    const int64_t seq_u0 = heads_v * p.before[seq];
+    const int hv = (int)quotient(u - seq_u0, nt);
+    const int64_t u0 = seq_u0 + (int64_t)hv * nt;
     const int b0 = (int)quotient(u0, each), n = (int)quotient(u0 + nt - 1, each) - b0 + 1;
     const int first = hv % p.col_blocks * QG;
     // (the first such number inside the head joins it)
@@ -569,15 +571,15 @@ __global__ __launch_bounds__(256) void join_kernel(Args p) {
   const int head_k = item / (ALL ? p.col_blocks : p.group);
   const int first = ALL ? item % p.col_blocks * QG : item % p.group;   // of the key head's
   const int count = ALL ? min(QG, p.group - first) : 1, col = first / QG;
-  const int64_t units = heads_v * scan_units(p, sums, [&](int s, int64_t before, int64_t) {
-    if (s == seq) before_s = heads_v * before;
-  });
-  __syncthreads();
   bool all_there;
   const int len = tokens_of(p, seq, all_there), nt = cache_units(len);
-  const int64_t each = units_each(units, p.blocks);
-  const int64_t u0 = before_s + (int64_t)(head_k * p.col_blocks + col) * nt;
-  const int b0 = nt == 0 ? 0 : (int)quotient(u0, each), n = nt == 0 ? 0 : (int)quotient(u0 + nt - 1, each) - b0 + 1;
+  int b0 = 0, n = 0;
+  if (nt > 0) {   // (without any unit nobody wrote `before`)
+    const int64_t each = units_each(heads_v * p.before[p.at.n_seq], p.blocks);
+    const int64_t u0 = heads_v * p.before[seq] + (int64_t)(head_k * p.col_blocks + col) * nt;
+    b0 = (int)quotient(u0, each);
+    n = (int)quotient(u0 + nt - 1, each) - b0 + 1;
+  }
   if (n == 1 || (ALL && n > LONG)) return;   // written by its block, or joined by those behind
   auto out_of = [&](int head) {
     return reinterpret_cast<T*>(const_cast<void*>(p.o.p)) + p.o.row * seq + p.o.head * head;
@@ -627,7 +629,7 @@ hipError_t launch(Args& a, int64_t units, hipStream_t s) {
   // A query head has a block of its own, or, from 256 column blocks on (one for every CU), a wave.
   // Measured on MI355X, us of the join, 28/4 heads of 128, block -> wave: 256 sequences of up to 512
   // 16.3 -> 7.1, 100 of up to 30000 12.6 -> 8.8, 64 of up to 1000 7.0 -> 6.5; 8 of up to 1000 5.7 -> 7.1,
-  // four of up to 131072 7.3 -> 17.
+  // four of up to 131072 7.3 -> 17.  (All of them some 1 us more than now: each block added the lengths up.)
   const int columns = a.at.n_seq * a.at.heads * a.col_blocks;
   if (columns >= 256)
     hipLaunchKernelGGL((join_kernel<T, DP, true>),
@@ -650,9 +652,13 @@ int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 }  // namespace
 
-// (two parts a block, whatever the batch)
-size_t cache_attention_scratch(int head_dim) {
+// two parts a block, and the units before every sequence; up to 4095 of them the size is one, so that
+// a batch may grow in it
+static size_t part_bytes(int head_dim) {
   return (size_t)2 * MAX_BLOCKS * QG * (padded(head_dim) + 2) * sizeof(float);
+}
+size_t cache_attention_scratch(int n_seq, int head_dim) {
+  return part_bytes(head_dim) + (n_seq < 4096 ? 4096 : (size_t)n_seq + 1) * sizeof(int64_t);
 }
 
 hipError_t cache_attention(const CacheAttention& p, hipStream_t s) {
@@ -667,6 +673,7 @@ hipError_t cache_attention(const CacheAttention& p, hipStream_t s) {
   a.lens = p.lens;
   a.lse = p.lse;
   a.part = p.scratch;
+  a.before = reinterpret_cast<int64_t*>((char*)p.scratch + part_bytes(p.cache.head_dim));
   a.ld_lse = p.ld_lse;
   a.scale = p.scale;
   a.group = p.q.heads / p.cache.heads;

@@ -36,3 +36,12 @@ def test_other_dimensions_refused(shape):
                  lambda: mp.op_causal_attention_fwd(x, good, good.clone(), good, None, [0], [10])):
         with pytest.raises(mp.MpipeError):
             call()
+
+def test_scratch_of_one_batch_serves_another():
+    """The size is one up to 4095 sequences."""
+    try:
+        mp.load()
+    except mp.MpipeError:
+        pytest.skip("libmpipe.so is not built")
+    size = {mp.op_cache_attention_scratch_bytes(n, 4, 2, 64) for n in (0, 1, 64, 4095)}
+    assert len(size) == 1 and mp.op_cache_attention_scratch_bytes(5000, 4, 2, 64) > size.pop()
